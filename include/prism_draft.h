@@ -38,7 +38,7 @@
  *   - Device memory: prism_create allocates the workspace, and
  *     prism_draft_load_shared / prism_draft_load_params allocate the weight
  *     arena (and the embedding tables, below) on their first call for a
- *     tensor group.  Drafting and verification calls allocate nothing.
+ *     tensor group.  Drafting, verification and cache calls allocate nothing.
  *   - One context is used by one host thread at a time.  Results are
  *     bit-identical across repeated calls with the same inputs.
  */
@@ -389,11 +389,171 @@ prism_status prism_verify_tree(prism_ctx *ctx, int32_t batch, int32_t n_nodes,
                                const int32_t *d_parent, int32_t *d_n_accepted,
                                int32_t *d_path, int32_t *d_next_token, void *stream);
 
+/* ---- Long-context draft cache ----------------------------------------------
+ * Calls that fill, read, summarise and shrink the paged cache of a prism_batch
+ * beside the drafting calls: rows appended with per-head norms and rotation,
+ * attention of one new token per sequence over the whole cache or over a list
+ * of its blocks, block summaries and the choice of blocks by them, and
+ * eviction by accumulated attention weight.  They need a context's shape and
+ * no weights, work on the device the context was created on (another current
+ * device is refused), and take prism_batch with d_tokens and d_features unused
+ * (NULL allowed).  Conventions of all of them:
+ *   - Rows (projections, queries, outputs), gains and summaries are in the
+ *     context dtype; sums, softmax statistics and slot weights are fp32 or
+ *     wider.  Matrix and pool pointers are 16-byte aligned; tensors are
+ *     contiguous and do not overlap unless stated.
+ *   - Slot weights are a pool beside the K and V pools,
+ *     [n_pool_blocks, n_kv_heads, kv_block_size] fp32: what each slot has
+ *     received of the attention, summed over the query heads of its KV head.
+ *   - n_new: slots behind the context that a call sees too (0, or 1 once the
+ *     new token's row has been appended): sequence b has n_b = L_b + n_new
+ *     visible slots, 0 .. n_b - 1.  n_b = 0 is allowed.
+ *   - max_len: an upper bound of every n_b known to the host, 1..capacity
+ *     (max_blocks_per_seq * kv_block_size); 0 = the capacity.  It sizes the
+ *     launches and the scratch.  A longer sequence is cut to it, and a
+ *     negative length taken as 0; both raise PRISM_ERR_CAPACITY in
+ *     prism_device_status.
+ *   - d_scratch: device memory of the caller's, at least prism_cache_scratch()
+ *     bytes, 16-byte aligned, written and read by the one call only (calls on
+ *     several streams, and captured graphs that may overlap, each need their
+ *     own).
+ *   - A block or slot that the block table or the pool does not hold is
+ *     skipped and raises PRISM_ERR_CAPACITY.
+ *   - n_pool_blocks * n_kv_heads * kv_block_size < 2^32 - 1. */
+
+/* New rows of the sequences, packed sequence by sequence: the fused
+ * projections [q heads ; k heads ; v heads] of each. */
+typedef struct {
+  const prism_batch *kv;
+  int32_t rows;                /* T >= 1                                     */
+  const int32_t *d_offsets;    /* [B + 1] sequence b owns rows d_offsets[b] ..
+                                  d_offsets[b+1] - 1 (any number, also none);
+                                  d_offsets[0] = 0, not decreasing,
+                                  d_offsets[B] <= T (the rows behind it are
+                                  left alone).  NULL: one row each, T = B    */
+  const int32_t *d_positions;  /* [B] RoPE position of each sequence's first
+                                  new row; NULL = L_b                        */
+  const void *d_qkv;           /* [T, (n_q_heads + 2 n_kv_heads) * d]        */
+  const void *d_q_gain;        /* [d] norm gain of the query heads; NULL =
+                                  no norm                                    */
+  const void *d_k_gain;        /* [d] the same of the key heads              */
+  void *d_q;                   /* [T, n_q_heads * d] queries out             */
+  float *d_weights;            /* slot weights, or NULL: 0 at the new slots  */
+} prism_cache_rows;
+
+/* Attention of one query row per sequence. */
+typedef struct {
+  const prism_batch *kv;
+  int32_t n_new, max_len;
+  const void *d_q;             /* [B, n_q_heads * d], rotated                */
+  const int32_t *d_blocks;     /* [B, n_kv_heads, n_blocks] the blocks (table
+                                  columns) that each sequence's KV head reads:
+                                  increasing, in 0 .. ceil(n_b / block) - 1,
+                                  then -1 (entries past max_blocks_per_seq
+                                  are not read).  NULL = every block         */
+  int32_t n_blocks;            /* >= 1 (with d_blocks)                       */
+  float *d_weights;            /* slot weights, or NULL: the weight that each
+                                  visible slot receives is added             */
+  void *d_out;                 /* [B, n_q_heads * d]                         */
+  float *d_lse;                /* [B, n_q_heads] log of the sum of exp(q.k /
+                                  sqrt(d)), or NULL                          */
+  void *d_scratch;
+  uint64_t scratch_bytes;
+} prism_cache_attention;
+
+/* Choice of the blocks that one query row per sequence reads. */
+typedef struct {
+  const prism_batch *kv;
+  int32_t n_new, max_len;
+  const void *d_q;             /* [B, n_q_heads * d], rotated                */
+  const void *d_summary;       /* prism_cache_summarize                      */
+  int32_t n_blocks;            /* blocks to choose, >= 1                     */
+  int32_t n_first, n_last;     /* always chosen: the first and the last ones;
+                                  n_first + n_last <= n_blocks               */
+  int32_t *d_blocks;           /* [B, n_kv_heads, n_blocks] chosen blocks in
+                                  increasing order, then -1                  */
+  void *d_scratch;
+  uint64_t scratch_bytes;
+} prism_cache_selection;
+
+/* Eviction: which slots stay, and where they go. */
+typedef struct {
+  const prism_batch *kv;       /* all L_b slots are candidates               */
+  int32_t max_len;
+  const int32_t *d_new_table;  /* [B, max_blocks_per_seq] the blocks that
+                                  receive the kept slots (the first
+                                  ceil(n_keep / kv_block_size) columns): of
+                                  the same pool, each used once, and none of
+                                  them in the first ceil(L_b / block) columns
+                                  of any sequence's block table              */
+  float *d_weights;            /* slot weights                               */
+  int32_t n_keep;              /* slots kept per sequence and KV head, 1 ..
+                                  capacity                                   */
+  int32_t n_first, n_recent;   /* always kept: the first and the last slots;
+                                  n_first + n_recent <= n_keep               */
+  int32_t *d_kept;             /* [B, n_kv_heads, n_keep] old slot of each new
+                                  slot, increasing, then -1                  */
+  int32_t *d_new_lens;         /* [B] min(n_keep, L_b)                       */
+  void *d_scratch;
+  uint64_t scratch_bytes;
+} prism_cache_eviction;
+
+/* Scratch bytes of one call over up to `batch` sequences: attention, the same
+ * with slot weights, selection, eviction.  max_len as in the call; for
+ * attention over a block list min(n_blocks, max_blocks_per_seq) *
+ * kv_block_size (whichever max_len the call has). */
+enum { PRISM_CACHE_ATTEND = 0, PRISM_CACHE_ATTEND_WEIGHTS = 1, PRISM_CACHE_SELECT = 2,
+       PRISM_CACHE_EVICT = 3 };
+prism_status prism_cache_scratch(prism_ctx *ctx, int32_t call, int32_t batch, int32_t max_len,
+                                 uint64_t *bytes);
+
+/* Append rows to the cache.  Row i of sequence b (its i-th new one) takes slot
+ * L_b + i and position p = d_positions[b] + i.  Every query and key head x is
+ * normalised, x / sqrt(mean(x^2) + rms_eps) * gain (where its gain is given),
+ * and rotated, (x_i, x_{i + d/2}) by the angle p * rope_theta^(-2i/d), in one
+ * pass; one rounding to the context dtype at the end.  Keys and values go to
+ * the cache, queries to d_q.  A malformed d_offsets raises
+ * PRISM_ERR_INVALID_ARG in prism_device_status and appends nothing. */
+prism_status prism_cache_append(prism_ctx *ctx, const prism_cache_rows *io, void *stream);
+
+/* out = softmax(q K^T / sqrt(d)) V over the visible slots of each sequence
+ * (GQA: query head h reads KV head h / (n_q_heads / n_kv_heads)), split over
+ * the cache's length and joined.  A sequence that sees nothing, or whose every
+ * score is -inf, gives zeros and a log-sum of -inf.  With d_weights no block
+ * may belong to two sequences of the call.  An entry of d_blocks that is out
+ * of range or not increasing is skipped and raises PRISM_ERR_INVALID_ARG in
+ * prism_device_status. */
+prism_status prism_cache_attend(prism_ctx *ctx, const prism_cache_attention *io, void *stream);
+
+/* Summaries of cache blocks: d_summary[block, head, 0 / 1, :] = the minimum /
+ * maximum of each channel over the block's visible keys (NaN passed over),
+ * [n_pool_blocks, n_kv_heads, 2, d] in the context dtype.  span > 0: only the
+ * blocks that hold the last span visible slots (those that changed since the
+ * last call); 0: every block. */
+prism_status prism_cache_summarize(prism_ctx *ctx, const prism_batch *kv, int32_t n_new,
+                                   int32_t span, void *d_summary, void *stream);
+
+/* The blocks of largest score for each sequence and KV head.  A block's score
+ * is the largest, over the query heads of the KV head, of sum_c q_c * (q_c >=
+ * 0 ? max_c : min_c), which bounds q.k over the block's keys; the sum is taken
+ * in fp64 and rounded to fp32.  Larger scores first, NaN after every number,
+ * ties to the lowest block. */
+prism_status prism_cache_select(prism_ctx *ctx, const prism_cache_selection *io, void *stream);
+
+/* Keep the n_keep slots of largest accumulated weight of each sequence and KV
+ * head (NaN after every number, ties to the lowest slot), and copy their keys,
+ * values and weights, in slot order, to the blocks of d_new_table.  The old
+ * blocks are left as they are, and so are the slots of the new ones behind
+ * d_new_lens[b].  Keys keep the rotation of their old positions: continue with
+ * explicit positions (prism_cache_append, prism_draft_step). */
+prism_status prism_cache_evict(prism_ctx *ctx, const prism_cache_eviction *io, void *stream);
+
 /* Synchronize `stream` and report device-side flags raised since the last
  * call, the first that applies of: PRISM_ERR_NONFINITE (a row whose logits
  * are all NaN, or a NaN tree score: the tokens of such a row are
  * unspecified and may lie outside 0..V-1; other rows are unaffected),
- * PRISM_ERR_INVALID_ARG (malformed catch-up offsets or tree-scoring rows),
+ * PRISM_ERR_INVALID_ARG (malformed catch-up offsets, tree-scoring rows, cache
+ * offsets or block lists),
  * PRISM_ERR_CAPACITY
  * (block table / pool / slot out of range), PRISM_ERR_INVALID_ARG (token id
  * out of range), else PRISM_OK.  Clears the flags. */

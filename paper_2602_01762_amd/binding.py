@@ -23,6 +23,8 @@ EXPORTS = ("prism_create", "prism_destroy", "prism_last_error", "prism_draft_loa
            "prism_draft_tree", "prism_score_tree", "prism_verify_chain",
            "prism_verify_chain_static",
            "prism_verify_tree",
+           "prism_cache_scratch", "prism_cache_append", "prism_cache_attend",
+           "prism_cache_summarize", "prism_cache_select", "prism_cache_evict",
            "prism_device_status",
            "prism_profile_enable", "prism_profile_read", "prism_profile_pairs",
            "prism_graph_cache")
@@ -70,6 +72,30 @@ class prism_tree_out(ctypes.Structure):
                 ("d_cand_score", c_vp), ("d_frontier", c_vp), ("d_logits", c_vp)]
 
 
+class prism_cache_rows(ctypes.Structure):
+    _fields_ = [("kv", ctypes.POINTER(prism_batch)), ("rows", c_i32), ("d_offsets", c_vp),
+                ("d_positions", c_vp), ("d_qkv", c_vp), ("d_q_gain", c_vp), ("d_k_gain", c_vp),
+                ("d_q", c_vp), ("d_weights", c_vp)]
+
+
+class prism_cache_attention(ctypes.Structure):
+    _fields_ = [("kv", ctypes.POINTER(prism_batch)), ("n_new", c_i32), ("max_len", c_i32),
+                ("d_q", c_vp), ("d_blocks", c_vp), ("n_blocks", c_i32), ("d_weights", c_vp),
+                ("d_out", c_vp), ("d_lse", c_vp), ("d_scratch", c_vp), ("scratch_bytes", c_u64)]
+
+
+class prism_cache_selection(ctypes.Structure):
+    _fields_ = [("kv", ctypes.POINTER(prism_batch)), ("n_new", c_i32), ("max_len", c_i32),
+                ("d_q", c_vp), ("d_summary", c_vp), ("n_blocks", c_i32), ("n_first", c_i32),
+                ("n_last", c_i32), ("d_blocks", c_vp), ("d_scratch", c_vp), ("scratch_bytes", c_u64)]
+
+
+class prism_cache_eviction(ctypes.Structure):
+    _fields_ = [("kv", ctypes.POINTER(prism_batch)), ("max_len", c_i32), ("d_new_table", c_vp),
+                ("d_weights", c_vp), ("n_keep", c_i32), ("n_first", c_i32), ("n_recent", c_i32),
+                ("d_kept", c_vp), ("d_new_lens", c_vp), ("d_scratch", c_vp), ("scratch_bytes", c_u64)]
+
+
 class PrismError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__("%s: %s" % (STATUS.get(status, status), msg))
@@ -110,6 +136,12 @@ def lib():
                                                 c_vp, c_vp, c_vp, c_vp]
         L.prism_verify_tree.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
                                         c_vp]
+        L.prism_cache_scratch.argtypes = [c_vp, c_i32, c_i32, c_i32, P(c_u64)]
+        L.prism_cache_append.argtypes = [c_vp, P(prism_cache_rows), c_vp]
+        L.prism_cache_attend.argtypes = [c_vp, P(prism_cache_attention), c_vp]
+        L.prism_cache_summarize.argtypes = [c_vp, P(prism_batch), c_i32, c_i32, c_vp, c_vp]
+        L.prism_cache_select.argtypes = [c_vp, P(prism_cache_selection), c_vp]
+        L.prism_cache_evict.argtypes = [c_vp, P(prism_cache_eviction), c_vp]
         L.prism_device_status.argtypes = [c_vp, c_vp]
         L.prism_profile_enable.argtypes = [c_vp, c_i32]
         L.prism_profile_read.argtypes = [c_vp, P(c_f32), P(c_i32)]
@@ -231,6 +263,37 @@ def prism_verify_tree(ctx, batch: int, n_nodes: int, target_logits, tokens, pare
     _check(lib().prism_verify_tree(ctx, batch, n_nodes, ptr(target_logits), ptr(tokens),
                                    ptr(parent), ptr(n_accepted), ptr(path), ptr(next_token),
                                    cur_stream() if stream is None else stream), ctx)
+
+
+PRISM_CACHE_ATTEND, PRISM_CACHE_ATTEND_WEIGHTS, PRISM_CACHE_SELECT, PRISM_CACHE_EVICT = range(4)
+
+
+def prism_cache_scratch(ctx, call: int, batch: int, max_len: int = 0) -> int:
+    """Scratch bytes of a PRISM_CACHE_* call."""
+    n = c_u64()
+    _check(lib().prism_cache_scratch(ctx, call, batch, max_len, ctypes.byref(n)), ctx)
+    return n.value
+
+
+def prism_cache_append(ctx, io: prism_cache_rows, stream=None):
+    _check(lib().prism_cache_append(ctx, ctypes.byref(io), cur_stream() if stream is None else stream), ctx)
+
+
+def prism_cache_attend(ctx, io: prism_cache_attention, stream=None):
+    _check(lib().prism_cache_attend(ctx, ctypes.byref(io), cur_stream() if stream is None else stream), ctx)
+
+
+def prism_cache_summarize(ctx, kv: prism_batch, n_new: int, span: int, summary, stream=None):
+    _check(lib().prism_cache_summarize(ctx, ctypes.byref(kv), n_new, span, ptr(summary),
+                                       cur_stream() if stream is None else stream), ctx)
+
+
+def prism_cache_select(ctx, io: prism_cache_selection, stream=None):
+    _check(lib().prism_cache_select(ctx, ctypes.byref(io), cur_stream() if stream is None else stream), ctx)
+
+
+def prism_cache_evict(ctx, io: prism_cache_eviction, stream=None):
+    _check(lib().prism_cache_evict(ctx, ctypes.byref(io), cur_stream() if stream is None else stream), ctx)
 
 
 def prism_device_status(ctx, stream=None) -> int:

@@ -1,0 +1,618 @@
+// Long-context draft cache: rows appended to the paged cache with per-head
+// norms and rotation, attention of one token per sequence over the whole cache
+// or a list of its blocks (with the weight that every slot receives), block
+// summaries and the selection of blocks by them, and eviction by accumulated
+// weight.
+//
+// Pools are [block, KV head, slot in block, d]: row (block, head, slot) of a
+// pool seen as [rows, d] has a 32-bit index (the runtime refuses larger pools).
+#include "device.h"
+#include "rotation.h"
+
+namespace prism {
+
+constexpr uint32_t NO_ROW = 0xffffffffu;   // a slot without storage
+
+// Slots of sequence b that a call sees: its context plus n_new, at most
+// max_len.  A negative length counts as none; a longer one is cut.  Both flag.
+__device__ __forceinline__ int visible_slots(const CacheView &v, int b, uint32_t *err) {
+  const long n = (long)v.kv.ctx_lens[b] + v.n_new;
+  if (n < 0 || n > v.max_len) {
+    if ((threadIdx.x & 63) == 0) atomicOr(err, ERRF_CAPACITY);
+    return n < 0 ? 0 : v.max_len;
+  }
+  return (int)n;
+}
+// Pool row of slot s of table column `bi` of sequence b, KV head j.
+__device__ __forceinline__ uint32_t pool_row(const CacheView &v, const int32_t *table, int b, int j,
+                                             int bi, int s, uint32_t *err) {
+  const int blk = bi < v.kv.mbps ? table[(size_t)b * v.kv.mbps + bi] : -1;
+  if (blk < 0 || blk >= v.kv.n_blocks) {
+    atomicOr(err, ERRF_CAPACITY);
+    return NO_ROW;
+  }
+  return ((uint32_t)blk * v.nkv + j) * v.kv.bs + s;
+}
+
+// 8 values of a row <-> fp32
+template <typename T>
+__device__ __forceinline__ void load8f(const T *p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    const u32x4 r = *(const u32x4 *)p;
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else {
+    const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = a[i];
+      x[4 + i] = b[i];
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8f(T *p, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = f2bf(x[2 * i]) | (f2bf(x[2 * i + 1]) << 16);
+    *(u32x4 *)p = r;
+  } else {
+    *(f32x4 *)p = f32x4{x[0], x[1], x[2], x[3]};
+    *(f32x4 *)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+  }
+}
+
+// ---------------------------------------------------------------- append
+// One lane group of d / 16 lanes per head: lane i holds dims 8i .. 8i+7 and
+// their rotation partners d/2 + 8i ...  The angles of a row are the same for
+// all its heads: d / 2 threads of the workgroup compute them once.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_cache_append(CacheAppend a) {
+  constexpr int LPH = D / 16, HPW = 64 / LPH;      // lanes per head, heads per wave
+  const int r = blockIdx.x, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
+  __shared__ float cs[D / 2], sn[D / 2];
+  const int nh = a.nq + 2 * a.v.nkv;
+  const int h = (blockIdx.y * (blockDim.x >> 6) + wave) * HPW + lane / LPH, li = lane % LPH;
+  const bool has = h < nh;
+  float x1[8], x2[8];
+  const T *row = (const T *)a.qkv + ((size_t)r * nh + (has ? h : 0)) * D + 8 * li;
+  load8f<T>(row, x1);
+  load8f<T>(row + D / 2, x2);
+  // sequence of the row, at most 64 of them: one lane per sequence
+  int b = r, at = 0;
+  if (a.offsets) {
+    const int B = a.v.kv.n_seq;
+    const int lo = lane < B ? a.offsets[lane] : 0, hi = lane < B ? a.offsets[lane + 1] : 0x7fffffff;
+    const bool bad = lane < B && (hi < lo || hi > a.rows || (lane == 0 && lo != 0));
+    if (__ballot(bad)) {                            // the same in every wave of every workgroup
+      if (tid == 0 && r == 0) atomicOr(a.err, ERRF_ROWS);
+      return;
+    }
+    b = __popcll(__ballot(lane < B && hi <= r));
+    if (b >= B) return;                             // a row behind the last sequence
+    at = r - __builtin_amdgcn_readlane(lo, __builtin_amdgcn_readfirstlane(b));
+  }
+  const int L = a.v.kv.ctx_lens[b];
+  const int pos0 = a.positions ? a.positions[b] : L;
+  for (int i = tid; i < D / 2; i += blockDim.x)
+    rotation_cos_sin((double)((long)pos0 + at) * a.inv_freq[i], cs[i], sn[i]);
+  __syncthreads();
+  if (!has) return;
+  const bool is_q = h < a.nq, is_v = h >= a.nq + a.v.nkv;
+  if (!is_v) {
+    const T *gain = (const T *)(is_q ? a.q_gain : a.k_gain);
+    if (gain) {
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss += x1[i] * x1[i] + x2[i] * x2[i];
+#pragma unroll
+      for (int m = 1; m < LPH; m *= 2) ss += __shfl_xor(ss, m, 64);
+      const float rs = 1.0f / sqrtf(ss / (float)D + a.eps);
+      float g1[8], g2[8];
+      load8f<T>(gain + 8 * li, g1);
+      load8f<T>(gain + D / 2 + 8 * li, g2);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x1[i] *= rs * g1[i];
+        x2[i] *= rs * g2[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float c = cs[8 * li + i], s = sn[8 * li + i], u = x1[i], w = x2[i];
+      x1[i] = u * c - w * s;
+      x2[i] = w * c + u * s;
+    }
+  }
+  if (is_q) {
+    T *o = (T *)a.q + ((size_t)r * a.nq + h) * D + 8 * li;
+    store8f<T>(o, x1);
+    store8f<T>(o + D / 2, x2);
+    return;
+  }
+  const int j = is_v ? h - a.nq - a.v.nkv : h - a.nq;
+  const long t = (long)L + at;
+  uint32_t prow = NO_ROW;
+  if (L < 0 || t >= (long)a.v.kv.mbps * a.v.kv.bs) {
+    atomicOr(a.err, ERRF_CAPACITY);
+  } else {
+    const int bi = slot_block(a.v.kv, (int)t);
+    prow = pool_row(a.v, a.v.kv.block_table, b, j, bi, slot_in_block(a.v.kv, (int)t, bi), a.err);
+  }
+  if (prow == NO_ROW) return;
+  T *o = (T *)(is_v ? a.v.kv.v_pool : a.v.kv.k_pool) + (size_t)prow * D + 8 * li;
+  store8f<T>(o, x1);
+  store8f<T>(o + D / 2, x2);
+  if (a.weights && is_v && li == 0) a.weights[prow] = 0.f;
+}
+
+template <typename T>
+static void append_d(const CacheAppend &a, int d, hipStream_t s) {
+  const int hpw = 64 / (d / 16), nh = a.nq + 2 * a.v.nkv;
+  const int nw = min(4, (nh + hpw - 1) / hpw);
+  const dim3 g(a.rows, (nh + nw * hpw - 1) / (nw * hpw)), t(64 * nw);
+  if (d == 32) hipLaunchKernelGGL((k_cache_append<T, 32>), g, t, 0, s, a);
+  else if (d == 64) hipLaunchKernelGGL((k_cache_append<T, 64>), g, t, 0, s, a);
+  else if (d == 128) hipLaunchKernelGGL((k_cache_append<T, 128>), g, t, 0, s, a);
+  else hipLaunchKernelGGL((k_cache_append<T, 256>), g, t, 0, s, a);
+}
+void launch_cache_append(bool bf16, const CacheAppend &a, int d, hipStream_t s) {
+  if (bf16) append_d<bf16_t>(a, d, s);
+  else append_d<float>(a, d, s);
+}
+
+// ---------------------------------------------------------------- attention
+// A call walks sequence b's "places" p: slot p, or with a block list slot p %
+// bs of block list[p / bs].  Workgroup (chunk c, KV head j, sequence b) takes
+// chunk places and leaves, for each of the g query heads, the maximum, the sum
+// and the unnormalised output of its softmax in base 2; the join adds the
+// chunks in order, so the result does not depend on scheduling.
+
+// Pool row of place p, or NO_ROW (nothing visible there).
+__device__ __forceinline__ uint32_t place_row(const CacheAttend &a, int b, int j, int n, int p) {
+  const CacheView &v = a.v;
+  int bi = slot_block(v.kv, p);
+  const int s = slot_in_block(v.kv, p, bi);
+  if (a.blocks) {
+    const int32_t *list = a.blocks + ((size_t)b * v.nkv + j) * a.n_list;
+    const int id = list[bi], prev = bi > 0 ? list[bi - 1] : -1;
+    if (id == -1) return NO_ROW;
+    if (id < 0 || id <= prev || (long)id * v.kv.bs >= n) {
+      atomicOr(a.err, ERRF_ROWS);
+      return NO_ROW;
+    }
+    bi = id;
+  }
+  if ((long)bi * v.kv.bs + s >= n) return NO_ROW;
+  return pool_row(v, v.kv.block_table, b, j, bi, s, a.err);
+}
+
+constexpr int CACHE_MAXG = 8;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// Plain form of the attention: a lane group of d / 8 lanes per slot keeps its
+// own softmax state; the groups of the wave are merged at the end.
+template <typename T, int D>
+__global__ __launch_bounds__(64) void k_cache_attend(CacheAttend a) {
+  constexpr int LPR = D / 8, RPI = 64 / LPR;       // lanes per row, rows per step
+  const int c = blockIdx.z, j = blockIdx.x, b = blockIdx.y, lane = threadIdx.x;
+  const int grp = lane / LPR, li = lane % LPR, g = a.g;
+  const int n = visible_slots(a.v, b, a.err);
+  const int places = a.blocks ? a.span : min(n, a.span);
+  const int p0 = c * a.chunk, p1 = min(places, p0 + a.chunk);
+  if (p0 >= places) return;
+  float q[CACHE_MAXG][8], o[CACHE_MAXG][8], m[CACHE_MAXG], l[CACHE_MAXG];
+#pragma unroll
+  for (int h = 0; h < CACHE_MAXG; ++h) {
+    if (h < g) load8f<T>((const T *)a.q + ((size_t)b * a.nq + j * g + h) * D + 8 * li, q[h]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      q[h][i] = h < g ? q[h][i] * a.scale : 0.f;
+      o[h][i] = 0.f;
+    }
+    m[h] = -INFINITY;
+    l[h] = 0.f;
+  }
+  for (int t = p0; t < p1; t += RPI) {
+    const int p = t + grp;
+    const uint32_t row = p < p1 ? place_row(a, b, j, n, p) : NO_ROW;
+    float k[8], w[8];
+    if (row != NO_ROW) {
+      load8f<T>((const T *)a.v.kv.k_pool + (size_t)row * D + 8 * li, k);
+      load8f<T>((const T *)a.v.kv.v_pool + (size_t)row * D + 8 * li, w);
+    }
+#pragma unroll
+    for (int h = 0; h < CACHE_MAXG; ++h)
+      if (h < g) {
+        float s = 0.f;
+        if (row != NO_ROW) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s += q[h][i] * k[i];
+        }
+#pragma unroll
+        for (int x = 1; x < LPR; x *= 2) s += __shfl_xor(s, x, 64);
+        if (row == NO_ROW) s = -INFINITY;
+        if (a.scores && li == 0 && p < p1) a.scores[((size_t)b * a.nq + j * g + h) * a.span + p] = s;
+        const float mn = s != s ? s : fmaxf(m[h], s);   // a NaN score reaches the sum
+        if (row != NO_ROW && !(s == -INFINITY)) {
+          const float al = m[h] == -INFINITY ? 0.f : exp2f(m[h] - mn), e = exp2f(s - mn);
+          l[h] = l[h] * al + e;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[h][i] = o[h][i] * al + e * w[i];
+          m[h] = mn;
+        }
+      }
+  }
+#pragma unroll
+  for (int h = 0; h < CACHE_MAXG; ++h)
+    if (h < g) {
+      float M = m[h];
+#pragma unroll
+      for (int x = LPR; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x, 64));
+      const float w = m[h] == -INFINITY ? 0.f : exp2f(m[h] - M);
+      float ls = l[h] * w;
+#pragma unroll
+      for (int x = LPR; x < 64; x *= 2) ls += __shfl_xor(ls, x, 64);
+      float ov[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ov[i] = m[h] == -INFINITY ? 0.f : o[h][i] * w;
+#pragma unroll
+        for (int x = LPR; x < 64; x *= 2) ov[i] += __shfl_xor(ov[i], x, 64);
+      }
+      const size_t pi = ((size_t)b * a.nq + j * g + h) * a.nch + c;
+      if (grp == 0) store8f<float>(a.po + pi * D + 8 * li, ov);
+      if (lane == 0) {
+        a.pm[pi] = M;
+        a.pl[pi] = ls;
+      }
+    }
+}
+
+// Join of the chunks of one (sequence, query head): every chunk's sum and
+// output weighted by 2^(its maximum - the largest one).
+template <typename T>
+__global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, d = a.d;
+  __shared__ float sh[8];
+  const int n = visible_slots(a.v, b, a.err);
+  const int places = a.blocks ? a.span : min(n, a.span);
+  const int nch = (places + a.chunk - 1) / a.chunk;
+  const size_t base = ((size_t)b * a.nq + h) * a.nch;
+  float m = -INFINITY;
+  for (int c = tid; c < nch; c += 256) m = fmaxf(m, a.pm[base + c]);
+  const float M = block_max<4>(m, sh);
+  float ls = 0.f;
+  for (int c = tid; c < nch; c += 256) {
+    const float mc = a.pm[base + c];
+    ls += mc == -INFINITY ? 0.f : a.pl[base + c] * exp2f(mc - M);
+  }
+  const float l = block_sum<4>(ls, sh);
+  if (tid < d) {
+    float o = 0.f;
+    for (int c = 0; c < nch; ++c) {
+      const float mc = a.pm[base + c];
+      if (mc != -INFINITY) o += a.po[(base + c) * d + tid] * exp2f(mc - M);
+    }
+    Ty<T>::st((T *)a.out, ((size_t)b * a.nq + h) * d + tid, l == 0.f ? 0.f : o / l);
+  }
+  if (tid == 0) {
+    const float lse = l == 0.f ? -INFINITY : M + log2f(l);
+    if (a.lse) a.lse[(size_t)b * a.nq + h] = lse * LN2;
+    if (a.lse2) a.lse2[(size_t)b * a.nq + h] = lse;
+  }
+}
+
+// Weight of every visible slot: the sum of its probabilities over the g heads
+// of its KV head, added to the slot's accumulated weight (one thread owns it).
+__global__ __launch_bounds__(256) void k_cache_weigh(CacheAttend a) {
+  const int j = blockIdx.y, b = blockIdx.z, g = a.g;
+  const int n = visible_slots(a.v, b, a.err);
+  const int places = a.blocks ? a.span : min(n, a.span);
+  const int p = blockIdx.x * 256 + threadIdx.x;
+  if (p >= places) return;
+  const uint32_t row = place_row(a, b, j, n, p);
+  if (row == NO_ROW) return;
+  float w = 0.f;
+  for (int h = 0; h < g; ++h) {
+    const size_t hi = (size_t)b * a.nq + j * g + h;
+    const float lse = a.lse2[hi];
+    if (lse != -INFINITY) w += exp2f(a.scores[hi * a.span + p] - lse);
+  }
+  a.weights[row] += w;
+}
+
+template <typename T>
+static void attend_d(const CacheAttend &a, hipStream_t s) {
+  const dim3 g(a.v.nkv, a.v.kv.n_seq, a.nch);
+  if (a.d == 32) hipLaunchKernelGGL((k_cache_attend<T, 32>), g, dim3(64), 0, s, a);
+  else if (a.d == 64) hipLaunchKernelGGL((k_cache_attend<T, 64>), g, dim3(64), 0, s, a);
+  else if (a.d == 128) hipLaunchKernelGGL((k_cache_attend<T, 128>), g, dim3(64), 0, s, a);
+  else hipLaunchKernelGGL((k_cache_attend<T, 256>), g, dim3(64), 0, s, a);
+  hipLaunchKernelGGL(k_cache_join<T>, dim3(a.nq, a.v.kv.n_seq), dim3(256), 0, s, a);
+  if (a.weights)
+    hipLaunchKernelGGL(k_cache_weigh, dim3((a.span + 255) / 256, a.v.nkv, a.v.kv.n_seq), dim3(256), 0, s, a);
+}
+void launch_cache_attend(bool bf16, const CacheAttend &a, hipStream_t s) {
+  if (bf16) attend_d<bf16_t>(a, s);
+  else attend_d<float>(a, s);
+}
+
+// ---------------------------------------------------------------- summaries
+// Channelwise minimum and maximum of the keys of one block and KV head: one
+// wave per (table column, KV head, sequence).  fminf and fmaxf pass over NaN.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_cache_summarize(CacheSummarize a) {
+  constexpr int LPR = D / 8, RPI = 64 / LPR;
+  const int lane = threadIdx.x & 63, j = blockIdx.y, b = blockIdx.z, bs = a.v.kv.bs;
+  const int grp = lane / LPR, li = lane % LPR;
+  const int n = visible_slots(a.v, b, a.err);
+  const int nblk = (int)(((long)n + bs - 1) / bs);
+  const int first = a.span > 0 && a.span < n ? (n - a.span) / bs : 0;
+  const int bi = first + blockIdx.x * 4 + wave_id();
+  if (bi >= nblk) return;
+  const uint32_t row = pool_row(a.v, a.v.kv.block_table, b, j, bi, 0, a.err);
+  if (row == NO_ROW) return;
+  const int held = min(bs, n - bi * bs);
+  float lo[8], hi[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo[i] = INFINITY;
+    hi[i] = -INFINITY;
+  }
+  for (int s = grp; s < held; s += RPI) {
+    float k[8];
+    load8f<T>((const T *)a.v.kv.k_pool + (size_t)(row + s) * D + 8 * li, k);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      lo[i] = fminf(lo[i], k[i]);
+      hi[i] = fmaxf(hi[i], k[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int x = LPR; x < 64; x *= 2) {
+      lo[i] = fminf(lo[i], __shfl_xor(lo[i], x, 64));
+      hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], x, 64));
+    }
+  if (grp == 0) {
+    T *o = (T *)a.summary + (size_t)(row / bs) * 2 * D + 8 * li;
+    store8f<T>(o, lo);
+    store8f<T>(o + D, hi);
+  }
+}
+
+template <typename T>
+static void summarize_d(const CacheSummarize &a, int d, hipStream_t s) {
+  const dim3 g((a.columns + 3) / 4, a.v.nkv, a.v.kv.n_seq);
+  if (d == 32) hipLaunchKernelGGL((k_cache_summarize<T, 32>), g, dim3(256), 0, s, a);
+  else if (d == 64) hipLaunchKernelGGL((k_cache_summarize<T, 64>), g, dim3(256), 0, s, a);
+  else if (d == 128) hipLaunchKernelGGL((k_cache_summarize<T, 128>), g, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_cache_summarize<T, 256>), g, dim3(256), 0, s, a);
+}
+void launch_cache_summarize(bool bf16, const CacheSummarize &a, int d, hipStream_t s) {
+  if (bf16) summarize_d<bf16_t>(a, d, s);
+  else summarize_d<float>(a, d, s);
+}
+
+// ---------------------------------------------------------------- choice
+// Order key of a choice's candidate: larger value first, NaN after every
+// number, forced candidates before all.
+constexpr uint32_t KEY_FORCED = 0xffffffffu;
+__device__ __forceinline__ uint32_t choice_key(float v) { return (uint32_t)(cand_key(v, 0) >> 32); }
+
+// Scores of the blocks: for every query head of the group the sum over the
+// channels of q_c * (q_c >= 0 ? max_c : min_c), an upper bound of q.k over the
+// block's keys; the block's score is the largest of them.  Products of stored
+// values are exact in fp64 and their sum is as good as exact, so the order of
+// the blocks does not depend on the order of the sum.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_cache_score(CacheSelect a) {
+  constexpr int LPR = D / 8, RPI = 64 / LPR;
+  const int lane = threadIdx.x & 63, j = blockIdx.y, b = blockIdx.z, bs = a.v.kv.bs, g = a.g;
+  const int grp = lane / LPR, li = lane % LPR;
+  const int n = visible_slots(a.v, b, a.err);
+  const int nblk = (int)(((long)n + bs - 1) / bs);
+  const int bi = (blockIdx.x * 4 + wave_id()) * RPI + grp;
+  if (bi - grp >= nblk) return;                     // whole waves
+  const bool held = bi < nblk;
+  const uint32_t row = held ? pool_row(a.v, a.v.kv.block_table, b, j, bi, 0, a.err) : NO_ROW;
+  float lo[8] = {}, hi[8] = {};
+  if (row != NO_ROW) {
+    const T *p = (const T *)a.summary + (size_t)(row / bs) * 2 * D + 8 * li;
+    load8f<T>(p, lo);
+    load8f<T>(p + D, hi);
+  }
+  float best = -INFINITY;
+  for (int h = 0; h < g; ++h) {
+    float q[8];
+    load8f<T>((const T *)a.q + ((size_t)b * a.nq + j * g + h) * D + 8 * li, q);
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += (double)q[i] * (double)(q[i] >= 0.f ? hi[i] : lo[i]);
+#pragma unroll
+    for (int x = 1; x < LPR; x *= 2) s += __shfl_xor(s, x, 64);
+    const float f = (float)s;
+    best = f > best || f != f ? f : best;           // NaN stays
+  }
+  if (held && li == 0) {
+    const bool forced = bi < a.n_first || bi >= nblk - a.n_last;
+    a.keys[((size_t)b * a.v.nkv + j) * a.columns + bi] =
+        row == NO_ROW ? 0u : forced ? KEY_FORCED : choice_key(best);
+  }
+}
+
+// The n_take candidates of largest key of one (sequence, KV head), ties to
+// the lowest index, in index order, then -1.  Radix descent over digits of 11,
+// 11 and 10 bits with an LDS histogram finds the key of the last one taken;
+// each wave then owns a run of candidates, so a prefix over the waves gives
+// every taken one its place.
+constexpr int CHOOSE_T = 1024, CHOOSE_W = CHOOSE_T / 64;
+__global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
+  const int j = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
+  __shared__ uint32_t hist[2048];
+  __shared__ uint32_t wsum[CHOOSE_W], wgt[CHOOSE_W], weq[CHOOSE_W];
+  __shared__ uint32_t s_digit, s_above;
+  const int n_vis = visible_slots(a.v, b, a.err);
+  const int bs = a.per_block ? a.v.kv.bs : 1;
+  const int n = (int)(((long)n_vis + bs - 1) / bs);
+  const size_t u = (size_t)b * a.v.nkv + j;
+  const uint32_t *keys = a.keys + u * a.ld_keys;
+  int32_t *out = a.out + u * a.n_take;
+  if (a.lens && j == 0 && tid == 0) a.lens[b] = min(n, a.n_take);
+  if (n <= a.n_take) {
+    for (int i = tid; i < a.n_take; i += CHOOSE_T) out[i] = i < n ? i : -1;
+    return;
+  }
+  uint32_t prefix = 0, mask = 0, need = a.n_take;
+  const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
+  for (int p = 0; p < 3; ++p) {
+    for (int i = tid; i < 2048; i += CHOOSE_T) hist[i] = 0;
+    __syncthreads();
+    const uint32_t dm = (1u << bits[p]) - 1;
+    for (int i = tid; i < n; i += CHOOSE_T) {
+      const uint32_t k = keys[i];
+      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shifts[p]) & dm], 1u);
+    }
+    __syncthreads();
+    // thread t owns digits 2t, 2t + 1; counts of the digits above it
+    const uint32_t h0 = hist[2 * tid], h1 = hist[2 * tid + 1];
+    uint32_t suf = h0 + h1;                         // inclusive suffix sum over the wave
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+      const uint32_t v = __shfl_down(suf, x, 64);
+      if (lane + x < 64) suf += v;
+    }
+    if (lane == 0) wsum[wave] = suf;
+    __syncthreads();
+    uint32_t above = suf - h0 - h1;
+    for (int w = wave + 1; w < CHOOSE_W; ++w) above += wsum[w];
+    if (above < need && above + h1 >= need) {
+      s_digit = 2 * tid + 1;
+      s_above = above;
+    } else if (above + h1 < need && above + h1 + h0 >= need) {
+      s_digit = 2 * tid;
+      s_above = above + h1;
+    }
+    __syncthreads();
+    prefix |= s_digit << shifts[p];
+    mask |= dm << shifts[p];
+    need -= s_above;
+    __syncthreads();
+  }
+  // taken: key > prefix, and the first `need` of those equal to it
+  const int per = ((n + CHOOSE_T - 1) / CHOOSE_T) * 64;   // candidates of one wave
+  const int i0 = wave * per, i1 = min(n, i0 + per);
+  uint32_t gt = 0, eq = 0;
+  for (int i = i0; i < i1; i += 64) {
+    const uint32_t k = i + lane < i1 ? keys[i + lane] : 0u;
+    gt += __popcll(__ballot(i + lane < i1 && k > prefix));
+    eq += __popcll(__ballot(i + lane < i1 && k == prefix));
+  }
+  if (lane == 0) {
+    wgt[wave] = gt;
+    weq[wave] = eq;
+  }
+  __syncthreads();
+  uint32_t eq0 = 0, at = 0;
+  for (int w = 0; w < wave; ++w) {
+    eq0 += weq[w];
+    at += wgt[w];
+  }
+  at += min(eq0, need);
+  const uint64_t below = (1ull << lane) - 1;
+  for (int i = i0; i < i1; i += 64) {
+    const bool in = i + lane < i1;
+    const uint32_t k = in ? keys[i + lane] : 0u;
+    const uint64_t me = __ballot(in && k == prefix);
+    const bool take = in && (k > prefix || (k == prefix && eq0 + __popcll(me & below) < need));
+    const uint64_t mt = __ballot(take);
+    if (take) out[at + __popcll(mt & below)] = i + lane;
+    at += __popcll(mt);
+    eq0 += __popcll(me);
+  }
+}
+
+template <typename T>
+static void score_d(const CacheSelect &a, int d, hipStream_t s) {
+  const int rpi = 64 / (d / 8);
+  const dim3 g((a.columns + 4 * rpi - 1) / (4 * rpi), a.v.nkv, a.v.kv.n_seq);
+  if (d == 32) hipLaunchKernelGGL((k_cache_score<T, 32>), g, dim3(256), 0, s, a);
+  else if (d == 64) hipLaunchKernelGGL((k_cache_score<T, 64>), g, dim3(256), 0, s, a);
+  else if (d == 128) hipLaunchKernelGGL((k_cache_score<T, 128>), g, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_cache_score<T, 256>), g, dim3(256), 0, s, a);
+}
+void launch_cache_select(bool bf16, const CacheSelect &a, int d, hipStream_t s) {
+  if (bf16) score_d<bf16_t>(a, d, s);
+  else score_d<float>(a, d, s);
+  CacheChoose c{a.v, a.keys, a.columns, 1, a.n_take, a.out, nullptr, a.err};
+  hipLaunchKernelGGL(k_cache_choose, dim3(a.v.nkv, a.v.kv.n_seq), dim3(CHOOSE_T), 0, s, c);
+}
+
+// ---------------------------------------------------------------- eviction
+// Order keys of the slots of one sequence and KV head.
+__global__ __launch_bounds__(256) void k_cache_keys(CacheEvict a) {
+  const int t = blockIdx.x * 256 + threadIdx.x, j = blockIdx.y, b = blockIdx.z;
+  const int n = visible_slots(a.v, b, a.err);
+  if (t >= n) return;
+  const int bi = slot_block(a.v.kv, t);
+  const uint32_t row = pool_row(a.v, a.v.kv.block_table, b, j, bi, slot_in_block(a.v.kv, t, bi), a.err);
+  const bool forced = t < a.n_first || t >= n - a.n_recent;
+  a.keys[((size_t)b * a.v.nkv + j) * a.ld_keys + t] =
+      row == NO_ROW ? 0u : forced ? KEY_FORCED : choice_key(a.weights[row]);
+}
+
+// Keys, values and weight of the kept slots to the new blocks: a lane group
+// of d / 8 lanes per slot.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_cache_copy(CacheEvict a) {
+  constexpr int LPR = D / 8, RPI = 64 / LPR;
+  const int lane = threadIdx.x & 63, j = blockIdx.y, b = blockIdx.z;
+  const int i = (blockIdx.x * 4 + wave_id()) * RPI + lane / LPR, li = lane % LPR;
+  if (i >= a.n_keep) return;
+  const int t = a.kept[((size_t)b * a.v.nkv + j) * a.n_keep + i];
+  if (t < 0) return;
+  const int sb = slot_block(a.v.kv, t), db = slot_block(a.v.kv, i);
+  const uint32_t src = pool_row(a.v, a.v.kv.block_table, b, j, sb, slot_in_block(a.v.kv, t, sb), a.err);
+  const uint32_t dst = pool_row(a.v, a.new_table, b, j, db, slot_in_block(a.v.kv, i, db), a.err);
+  if (src == NO_ROW || dst == NO_ROW) return;
+  constexpr int U = sizeof(T) / 2;                 // 16-byte pieces per lane
+  const size_t so = (size_t)src * D + 8 * li, to = (size_t)dst * D + 8 * li;
+  u32x4 k[U], v[U];
+#pragma unroll
+  for (int x = 0; x < U; ++x) {
+    k[x] = ((const u32x4 *)((const T *)a.v.kv.k_pool + so))[x];
+    v[x] = ((const u32x4 *)((const T *)a.v.kv.v_pool + so))[x];
+  }
+#pragma unroll
+  for (int x = 0; x < U; ++x) {
+    ((u32x4 *)((T *)a.v.kv.k_pool + to))[x] = k[x];
+    ((u32x4 *)((T *)a.v.kv.v_pool + to))[x] = v[x];
+  }
+  if (li == 0) a.weights[dst] = a.weights[src];
+}
+
+template <typename T>
+static void copy_d(const CacheEvict &a, int d, hipStream_t s) {
+  const int rpi = 64 / (d / 8);
+  const dim3 g((a.n_keep + 4 * rpi - 1) / (4 * rpi), a.v.nkv, a.v.kv.n_seq);
+  if (d == 32) hipLaunchKernelGGL((k_cache_copy<T, 32>), g, dim3(256), 0, s, a);
+  else if (d == 64) hipLaunchKernelGGL((k_cache_copy<T, 64>), g, dim3(256), 0, s, a);
+  else if (d == 128) hipLaunchKernelGGL((k_cache_copy<T, 128>), g, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_cache_copy<T, 256>), g, dim3(256), 0, s, a);
+}
+void launch_cache_evict(bool bf16, const CacheEvict &a, int d, hipStream_t s) {
+  hipLaunchKernelGGL(k_cache_keys, dim3((a.v.max_len + 255) / 256, a.v.nkv, a.v.kv.n_seq), dim3(256), 0, s, a);
+  CacheChoose c{a.v, a.keys, a.ld_keys, 0, a.n_keep, a.kept, a.new_lens, a.err};
+  hipLaunchKernelGGL(k_cache_choose, dim3(a.v.nkv, a.v.kv.n_seq), dim3(CHOOSE_T), 0, s, c);
+  if (bf16) copy_d<bf16_t>(a, d, s);
+  else copy_d<float>(a, d, s);
+}
+
+}  // namespace prism

@@ -356,4 +356,21 @@ inline long attention_partial_rows(int rows_max, int grp, int grp2, int nkv, int
   return most;
 }
 
+// Attention over the long-context cache: places per workgroup (one wave) and
+// workgroups per (sequence, KV head), for `units` pairs of a sequence and a KV
+// head of up to `span` places.
+constexpr int CACHE_TILE = 64;          // a chunk is a multiple of this
+constexpr int CACHE_WAVES = 4096;       // waves aimed at: two rounds of 8 per CU
+constexpr int CACHE_MAX_CHUNK = 1024;   // bounds the tail of a ragged batch
+struct CachePlan {
+  int chunk, nch;
+};
+inline CachePlan cache_plan(int units, int span) {
+  const long want = units >= CACHE_WAVES ? 1 : CACHE_WAVES / units;
+  long chunk = (span + want - 1) / want;
+  chunk = (chunk + CACHE_TILE - 1) / CACHE_TILE * CACHE_TILE;
+  if (chunk > CACHE_MAX_CHUNK) chunk = CACHE_MAX_CHUNK;
+  return {(int)chunk, (int)((span + chunk - 1) / chunk)};
+}
+
 }  // namespace prism

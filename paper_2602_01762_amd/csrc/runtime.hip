@@ -1469,6 +1469,249 @@ prism_status prism_graph_cache(const prism_ctx *c, int32_t *n_graphs, int32_t *c
   return PRISM_OK;
 }
 
+// ---- long-context draft cache
+static prism_status check_cache(prism_ctx *c, const prism_batch *b) {
+  if (!b) return fail(c, PRISM_ERR_INVALID_ARG, "kv is NULL");
+  if (b->batch < 1 || b->batch > c->cfg.max_batch)
+    return fail(c, PRISM_ERR_INVALID_ARG, "batch %d out of 1..%d", b->batch, c->cfg.max_batch);
+  if (!b->d_ctx_lens || !b->d_k_pool || !b->d_v_pool || !b->d_block_table || b->n_pool_blocks < 1)
+    return fail(c, PRISM_ERR_INVALID_ARG, "incomplete KV description");
+  if (((uintptr_t)b->d_k_pool | (uintptr_t)b->d_v_pool) & 15)
+    return fail(c, PRISM_ERR_INVALID_ARG, "KV pools must be 16-byte aligned");
+  if ((double)b->n_pool_blocks * c->nkv * c->cfg.kv_block_size >= 4294967295.0)
+    return fail(c, PRISM_ERR_SHAPE, "KV pools of 2^32 rows or more");
+  int dev = -1;
+  HIPCHK(c, hipGetDevice(&dev));
+  if (dev != c->dev)
+    return fail(c, PRISM_ERR_INVALID_ARG, "current device %d, but the context is on device %d", dev, c->dev);
+  return PRISM_OK;
+}
+static prism_status check_rows(prism_ctx *c, const void *p, const char *what) {
+  if (!p) return fail(c, PRISM_ERR_INVALID_ARG, "%s is NULL", what);
+  if ((uintptr_t)p & 15) return fail(c, PRISM_ERR_INVALID_ARG, "%s must be 16-byte aligned", what);
+  return PRISM_OK;
+}
+// max_len of a call: 0 = the capacity
+static prism_status check_len(prism_ctx *c, int32_t n_new, int32_t max_len, int *out) {
+  if (n_new < 0 || n_new > c->max_slots)
+    return fail(c, PRISM_ERR_INVALID_ARG, "n_new %d out of 0..%d", n_new, c->max_slots);
+  if (max_len < 0 || max_len > c->max_slots)
+    return fail(c, PRISM_ERR_INVALID_ARG, "max_len %d out of 0..%d", max_len, c->max_slots);
+  *out = max_len ? max_len : c->max_slots;
+  return PRISM_OK;
+}
+static size_t cache_scratch(const prism_ctx *c, int call, int B, int span) {
+  const size_t pad = 255;
+  if (call == PRISM_CACHE_SELECT)
+    return (size_t)B * c->nkv * ((span + c->cfg.kv_block_size - 1) / c->cfg.kv_block_size) * 4;
+  if (call == PRISM_CACHE_EVICT) return (size_t)B * c->nkv * span * 4;
+  const CachePlan p = cache_plan(B * c->nkv, span);
+  const size_t parts = (size_t)B * c->nq * p.nch;
+  size_t n = ((parts * 4 + pad) & ~pad) * 2 + ((parts * c->d * 4 + pad) & ~pad);
+  if (call == PRISM_CACHE_ATTEND_WEIGHTS)
+    n += (((size_t)B * c->nq * 4 + pad) & ~pad) + (size_t)B * c->nq * span * 4;
+  return n;
+}
+static prism_status check_scratch(prism_ctx *c, const void *p, uint64_t bytes, size_t need) {
+  if (!p || ((uintptr_t)p & 15)) return fail(c, PRISM_ERR_INVALID_ARG, "d_scratch is NULL or not 16-byte aligned");
+  if (bytes < need)
+    return fail(c, PRISM_ERR_INVALID_ARG, "scratch of %llu bytes, %zu needed", (unsigned long long)bytes, need);
+  return PRISM_OK;
+}
+static CacheView cache_view(const prism_ctx *c, const prism_batch *b, int n_new, int max_len) {
+  CacheView v;
+  v.kv = kv_of(c, b);
+  v.nkv = c->nkv;
+  v.n_new = n_new;
+  v.max_len = max_len;
+  return v;
+}
+#define CHECK(call)                   \
+  do {                                \
+    const prism_status st_ = (call);  \
+    if (st_) return st_;              \
+  } while (0)
+
+prism_status prism_cache_scratch(prism_ctx *c, int32_t call, int32_t batch, int32_t max_len,
+                                 uint64_t *bytes) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  if (!bytes) return fail(c, PRISM_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = 0;
+  if (call < PRISM_CACHE_ATTEND || call > PRISM_CACHE_EVICT)
+    return fail(c, PRISM_ERR_INVALID_ARG, "call %d", call);
+  if (batch < 1 || batch > c->cfg.max_batch)
+    return fail(c, PRISM_ERR_INVALID_ARG, "batch %d out of 1..%d", batch, c->cfg.max_batch);
+  int len = 0;
+  CHECK(check_len(c, 0, max_len, &len));
+  *bytes = cache_scratch(c, call, batch, len);
+  return PRISM_OK;
+}
+
+prism_status prism_cache_append(prism_ctx *c, const prism_cache_rows *io, void *stream) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  if (!io) return fail(c, PRISM_ERR_INVALID_ARG, "io is NULL");
+  CHECK(check_cache(c, io->kv));
+  if (io->rows < 1) return fail(c, PRISM_ERR_INVALID_ARG, "rows %d", io->rows);
+  if (!io->d_offsets && io->rows != io->kv->batch)
+    return fail(c, PRISM_ERR_INVALID_ARG, "%d rows without offsets for a batch of %d", io->rows, io->kv->batch);
+  CHECK(check_rows(c, io->d_qkv, "d_qkv"));
+  CHECK(check_rows(c, io->d_q, "d_q"));
+  if (((uintptr_t)io->d_q_gain | (uintptr_t)io->d_k_gain) & 15)
+    return fail(c, PRISM_ERR_INVALID_ARG, "gains must be 16-byte aligned");
+  CacheAppend a{};
+  a.v = cache_view(c, io->kv, 0, c->max_slots);
+  a.rows = io->rows;
+  a.nq = c->nq;
+  a.offsets = io->d_offsets;
+  a.positions = io->d_positions;
+  a.qkv = io->d_qkv;
+  a.q_gain = io->d_q_gain;
+  a.k_gain = io->d_k_gain;
+  a.q = io->d_q;
+  a.weights = io->d_weights;
+  a.inv_freq = c->inv_freq;
+  a.eps = c->cfg.rms_eps;
+  a.err = c->err;
+  launch_cache_append(c->bf16, a, c->d, (hipStream_t)stream);
+  HIPCHK(c, hipGetLastError());
+  return PRISM_OK;
+}
+
+prism_status prism_cache_attend(prism_ctx *c, const prism_cache_attention *io, void *stream) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  if (!io) return fail(c, PRISM_ERR_INVALID_ARG, "io is NULL");
+  CHECK(check_cache(c, io->kv));
+  int len = 0;
+  CHECK(check_len(c, io->n_new, io->max_len, &len));
+  CHECK(check_rows(c, io->d_q, "d_q"));
+  CHECK(check_rows(c, io->d_out, "d_out"));
+  if (io->d_blocks && io->n_blocks < 1)
+    return fail(c, PRISM_ERR_INVALID_ARG, "n_blocks %d", io->n_blocks);
+  const int B = io->kv->batch;
+  const int span = io->d_blocks ? std::min(io->n_blocks, c->cfg.max_blocks_per_seq) * c->cfg.kv_block_size : len;
+  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes,
+                      cache_scratch(c, io->d_weights ? PRISM_CACHE_ATTEND_WEIGHTS : PRISM_CACHE_ATTEND, B, span)));
+  const CachePlan p = cache_plan(B * c->nkv, span);
+  CacheAttend a{};
+  a.v = cache_view(c, io->kv, io->n_new, len);
+  a.nq = c->nq;
+  a.g = c->nq / c->nkv;
+  a.d = c->d;
+  a.q = io->d_q;
+  a.blocks = io->d_blocks;
+  a.n_list = io->n_blocks;
+  a.span = span;
+  a.chunk = p.chunk;
+  a.nch = p.nch;
+  a.scale = 1.4426950408889634f / sqrtf((float)c->d);
+  const size_t parts = (size_t)B * c->nq * p.nch;
+  char *ws = (char *)io->d_scratch;
+  carve(ws, (void **)&a.pm, parts * 4);
+  carve(ws, (void **)&a.pl, parts * 4);
+  carve(ws, (void **)&a.po, parts * c->d * 4);
+  if (io->d_weights) {
+    carve(ws, (void **)&a.lse2, (size_t)B * c->nq * 4);
+    a.scores = (float *)ws;
+  }
+  a.out = io->d_out;
+  a.lse = io->d_lse;
+  a.weights = io->d_weights;
+  a.err = c->err;
+  launch_cache_attend(c->bf16, a, (hipStream_t)stream);
+  HIPCHK(c, hipGetLastError());
+  return PRISM_OK;
+}
+
+prism_status prism_cache_summarize(prism_ctx *c, const prism_batch *kv, int32_t n_new, int32_t span,
+                                   void *d_summary, void *stream) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  CHECK(check_cache(c, kv));
+  int len = 0;
+  CHECK(check_len(c, n_new, 0, &len));
+  if (span < 0) return fail(c, PRISM_ERR_INVALID_ARG, "span %d", span);
+  CHECK(check_rows(c, d_summary, "d_summary"));
+  CacheSummarize a{};
+  a.v = cache_view(c, kv, n_new, len);
+  a.span = span;
+  const int bs = c->cfg.kv_block_size;
+  a.columns = c->cfg.max_blocks_per_seq;
+  if (span > 0) a.columns = (int)std::min((long)a.columns, ((long)span + bs - 1) / bs + 1);
+  a.summary = d_summary;
+  a.err = c->err;
+  launch_cache_summarize(c->bf16, a, c->d, (hipStream_t)stream);
+  HIPCHK(c, hipGetLastError());
+  return PRISM_OK;
+}
+
+prism_status prism_cache_select(prism_ctx *c, const prism_cache_selection *io, void *stream) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  if (!io) return fail(c, PRISM_ERR_INVALID_ARG, "io is NULL");
+  CHECK(check_cache(c, io->kv));
+  int len = 0;
+  CHECK(check_len(c, io->n_new, io->max_len, &len));
+  CHECK(check_rows(c, io->d_q, "d_q"));
+  CHECK(check_rows(c, io->d_summary, "d_summary"));
+  if (!io->d_blocks) return fail(c, PRISM_ERR_INVALID_ARG, "d_blocks is NULL");
+  if (io->n_blocks < 1) return fail(c, PRISM_ERR_INVALID_ARG, "n_blocks %d", io->n_blocks);
+  if (io->n_first < 0 || io->n_last < 0 || (long)io->n_first + io->n_last > io->n_blocks)
+    return fail(c, PRISM_ERR_INVALID_ARG, "n_first %d and n_last %d of n_blocks %d", io->n_first, io->n_last,
+                io->n_blocks);
+  const int B = io->kv->batch;
+  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, cache_scratch(c, PRISM_CACHE_SELECT, B, len)));
+  CacheSelect a{};
+  a.v = cache_view(c, io->kv, io->n_new, len);
+  a.nq = c->nq;
+  a.g = c->nq / c->nkv;
+  a.q = io->d_q;
+  a.summary = io->d_summary;
+  a.n_take = io->n_blocks;
+  a.n_first = io->n_first;
+  a.n_last = io->n_last;
+  a.columns = (len + c->cfg.kv_block_size - 1) / c->cfg.kv_block_size;
+  a.keys = (uint32_t *)io->d_scratch;
+  a.out = io->d_blocks;
+  a.err = c->err;
+  launch_cache_select(c->bf16, a, c->d, (hipStream_t)stream);
+  HIPCHK(c, hipGetLastError());
+  return PRISM_OK;
+}
+
+prism_status prism_cache_evict(prism_ctx *c, const prism_cache_eviction *io, void *stream) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  if (!io) return fail(c, PRISM_ERR_INVALID_ARG, "io is NULL");
+  CHECK(check_cache(c, io->kv));
+  int len = 0;
+  CHECK(check_len(c, 0, io->max_len, &len));
+  if (!io->d_new_table || !io->d_weights || !io->d_kept || !io->d_new_lens)
+    return fail(c, PRISM_ERR_INVALID_ARG, "NULL pointer in eviction");
+  if (io->d_new_table == io->kv->d_block_table)
+    return fail(c, PRISM_ERR_INVALID_ARG, "d_new_table is the batch's block table");
+  if (io->d_new_lens == io->kv->d_ctx_lens)
+    return fail(c, PRISM_ERR_INVALID_ARG, "d_new_lens are the batch's lengths");
+  if (io->n_keep < 1 || io->n_keep > c->max_slots)
+    return fail(c, PRISM_ERR_INVALID_ARG, "n_keep %d out of 1..%d", io->n_keep, c->max_slots);
+  if (io->n_first < 0 || io->n_recent < 0 || (long)io->n_first + io->n_recent > io->n_keep)
+    return fail(c, PRISM_ERR_INVALID_ARG, "n_first %d and n_recent %d of n_keep %d", io->n_first, io->n_recent,
+                io->n_keep);
+  const int B = io->kv->batch;
+  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, cache_scratch(c, PRISM_CACHE_EVICT, B, len)));
+  CacheEvict a{};
+  a.v = cache_view(c, io->kv, 0, len);
+  a.new_table = io->d_new_table;
+  a.weights = io->d_weights;
+  a.n_keep = io->n_keep;
+  a.n_first = io->n_first;
+  a.n_recent = io->n_recent;
+  a.ld_keys = len;
+  a.keys = (uint32_t *)io->d_scratch;
+  a.kept = io->d_kept;
+  a.new_lens = io->d_new_lens;
+  a.err = c->err;
+  launch_cache_evict(c->bf16, a, c->d, (hipStream_t)stream);
+  HIPCHK(c, hipGetLastError());
+  return PRISM_OK;
+}
+
 prism_status prism_device_status(prism_ctx *c, void *stream) {
   if (!c) return PRISM_ERR_INVALID_ARG;
   HIPCHK(c, hipStreamSynchronize((hipStream_t)stream));
@@ -1478,7 +1721,7 @@ prism_status prism_device_status(prism_ctx *c, void *stream) {
   if (flags & ERRF_NONFINITE)
     return fail(c, PRISM_ERR_NONFINITE, "NaN logits or tree scores (NaN in a feature row or a weight)");
   if (flags & ERRF_ROWS)
-    return fail(c, PRISM_ERR_INVALID_ARG, "malformed catch-up offsets or tree-scoring rows");
+    return fail(c, PRISM_ERR_INVALID_ARG, "malformed catch-up offsets, tree-scoring rows, cache offsets or block lists");
   if (flags & ERRF_CAPACITY) return fail(c, PRISM_ERR_CAPACITY, "KV slot, block or pool out of range");
   if (flags & ERRF_TOKEN) return fail(c, PRISM_ERR_INVALID_ARG, "token id out of range");
   return PRISM_OK;

@@ -5,6 +5,7 @@ into the HIP library.  Nothing here computes any part of the drafting path.
 """
 from __future__ import annotations
 
+import ctypes
 from typing import Optional, Sequence
 
 import torch
@@ -241,6 +242,189 @@ class Drafter:
         io.d_logits = B.ptr(out["logits"])
         B.prism_draft_step(self.ctx, k, io)
         return out
+
+    # long-context draft cache ---------------------------------------------------
+    def _expect(self, t, name: str, shape, dtype, optional=False):
+        """A contiguous tensor of this shape and type on the context's device."""
+        if t is None and optional:
+            return
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a tensor" % name)
+        if t.dtype != dtype:
+            raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+        if t.device != self.device:
+            raise ValueError("%s is on %s, the context on %s" % (name, t.device, self.device))
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+
+    def _pool(self, kv):
+        c = self.cfg
+        return int(kv.n_pool_blocks), c.n_kv_heads, c.kv_block_size
+
+    @property
+    def _dtype(self):
+        return torch.bfloat16 if self.cfg.dtype == B.PRISM_BF16 else torch.float32
+
+    def _scratch(self, call: int, batch: int, max_len: int):
+        n = B.prism_cache_scratch(self.ctx, call, batch, max_len)
+        return torch.empty(n, dtype=torch.uint8, device=self.device)
+
+    def cache(self, lens, k_pool, v_pool, block_table) -> B.prism_batch:
+        """The sequences of a cache call: lens [B] int32 slots held, pools
+        [blocks, n_kv_heads, kv_block_size, head_dim], block_table
+        [B, max_blocks_per_seq] int32.  Keeps the tensors alive."""
+        c = self.cfg
+        nb = int(lens.shape[0])
+        self._expect(lens, "lens", (nb,), torch.int32)
+        for name, t in (("k_pool", k_pool), ("v_pool", v_pool)):
+            self._expect(t, name, (k_pool.shape[0], c.n_kv_heads, c.kv_block_size, c.head_dim), self._dtype)
+        self._expect(block_table, "block_table", (nb, c.max_blocks_per_seq), torch.int32)
+        kv = B.prism_batch()
+        kv.batch = nb
+        kv.d_ctx_lens = B.ptr(lens)
+        kv.d_k_pool = B.ptr(k_pool)
+        kv.d_v_pool = B.ptr(v_pool)
+        kv.d_block_table = B.ptr(block_table)
+        kv.n_pool_blocks = int(k_pool.shape[0])
+        kv.tensors = (lens, k_pool, v_pool, block_table)
+        return kv
+
+    def cache_append(self, kv, qkv, q_gain=None, k_gain=None, offsets=None, positions=None,
+                     weights=None, out=None):
+        """Normalise, rotate and append rows: qkv [T, (n_q + 2 n_kv) * d] of
+        the sequences in order (rows offsets[b] .. offsets[b+1] - 1; None: one
+        row each) at positions[b] (None: lens[b]) and the slots behind each
+        context.  Returns the queries [T, n_q, d]."""
+        c, dt = self.cfg, self._dtype
+        T = int(qkv.shape[0])
+        self._expect(qkv, "qkv", (T, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim), dt)
+        for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
+            self._expect(t, name, (c.head_dim,), dt, optional=True)
+        self._expect(offsets, "offsets", (kv.batch + 1,), torch.int32, optional=True)
+        self._expect(positions, "positions", (kv.batch,), torch.int32, optional=True)
+        self._expect(weights, "weights", self._pool(kv), torch.float32, optional=True)
+        if out is None:
+            out = torch.empty((T, c.n_q_heads, c.head_dim), dtype=dt, device=self.device)
+        self._expect(out, "out", (T, c.n_q_heads, c.head_dim), dt)
+        io = B.prism_cache_rows()
+        io.kv = ctypes.pointer(kv)
+        io.rows = T
+        io.d_offsets = B.ptr(offsets)
+        io.d_positions = B.ptr(positions)
+        io.d_qkv = B.ptr(qkv)
+        io.d_q_gain = B.ptr(q_gain)
+        io.d_k_gain = B.ptr(k_gain)
+        io.d_q = B.ptr(out)
+        io.d_weights = B.ptr(weights)
+        B.prism_cache_append(self.ctx, io)
+        return out
+
+    def cache_attend(self, kv, q, n_new: int = 0, max_len: int = 0, blocks=None, weights=None,
+                     lse: bool = False, out=None):
+        """Attention of one query row per sequence, q [B, n_q, d], over its
+        cache or over blocks [B, n_kv, n] of it; adds what every slot receives
+        to weights.  Returns out [B, n_q, d] and, if asked for, lse [B, n_q]."""
+        c, dt, nb = self.cfg, self._dtype, int(kv.batch)
+        self._expect(q, "q", (nb, c.n_q_heads, c.head_dim), dt)
+        span = max_len
+        n_blocks = 0
+        if blocks is not None:
+            n_blocks = int(blocks.shape[-1])
+            self._expect(blocks, "blocks", (nb, c.n_kv_heads, n_blocks), torch.int32)
+            if n_blocks < 1:
+                raise ValueError("blocks has no entry")
+            span = min(n_blocks, c.max_blocks_per_seq) * c.kv_block_size
+        self._expect(weights, "weights", self._pool(kv), torch.float32, optional=True)
+        if out is None:
+            out = torch.empty((nb, c.n_q_heads, c.head_dim), dtype=dt, device=self.device)
+        self._expect(out, "out", (nb, c.n_q_heads, c.head_dim), dt)
+        res = {"out": out,
+               "lse": (torch.empty((nb, c.n_q_heads), dtype=torch.float32, device=self.device)
+                       if lse else None)}
+        call = B.PRISM_CACHE_ATTEND if weights is None else B.PRISM_CACHE_ATTEND_WEIGHTS
+        scratch = self._scratch(call, nb, span)
+        io = B.prism_cache_attention()
+        io.kv = ctypes.pointer(kv)
+        io.n_new = n_new
+        io.max_len = max_len
+        io.d_q = B.ptr(q)
+        io.d_blocks = B.ptr(blocks)
+        io.n_blocks = n_blocks
+        io.d_weights = B.ptr(weights)
+        io.d_out = B.ptr(out)
+        io.d_lse = B.ptr(res["lse"])
+        io.d_scratch = B.ptr(scratch)
+        io.scratch_bytes = scratch.numel()
+        B.prism_cache_attend(self.ctx, io)
+        return res
+
+    def summary_buffer(self, kv):
+        """A summary pool [blocks, n_kv, 2, d] for cache_summarize."""
+        n, h, _ = self._pool(kv)
+        return torch.zeros((n, h, 2, self.cfg.head_dim), dtype=self._dtype, device=self.device)
+
+    def cache_summarize(self, kv, summary, n_new: int = 0, span: int = 0):
+        """Write the key minima and maxima of the blocks that hold the last
+        span slots (0: of every block) into summary [blocks, n_kv, 2, d]."""
+        n, h, _ = self._pool(kv)
+        self._expect(summary, "summary", (n, h, 2, self.cfg.head_dim), self._dtype)
+        B.prism_cache_summarize(self.ctx, kv, n_new, span, summary)
+        return summary
+
+    def cache_select(self, kv, q, summary, n_blocks: int, n_first: int = 0, n_last: int = 0,
+                     n_new: int = 0, max_len: int = 0, out=None):
+        """The n_blocks blocks of largest score bound for each sequence and KV
+        head, [B, n_kv, n_blocks] int32: increasing, then -1."""
+        c, nb = self.cfg, int(kv.batch)
+        n, h, _ = self._pool(kv)
+        self._expect(q, "q", (nb, c.n_q_heads, c.head_dim), self._dtype)
+        self._expect(summary, "summary", (n, h, 2, c.head_dim), self._dtype)
+        if out is None:
+            out = torch.empty((nb, h, max(n_blocks, 0)), dtype=torch.int32, device=self.device)
+        self._expect(out, "out", (nb, h, n_blocks), torch.int32)
+        scratch = self._scratch(B.PRISM_CACHE_SELECT, nb, max_len)
+        io = B.prism_cache_selection()
+        io.kv = ctypes.pointer(kv)
+        io.n_new = n_new
+        io.max_len = max_len
+        io.d_q = B.ptr(q)
+        io.d_summary = B.ptr(summary)
+        io.n_blocks = n_blocks
+        io.n_first = n_first
+        io.n_last = n_last
+        io.d_blocks = B.ptr(out)
+        io.d_scratch = B.ptr(scratch)
+        io.scratch_bytes = scratch.numel()
+        B.prism_cache_select(self.ctx, io)
+        return out
+
+    def cache_evict(self, kv, new_table, weights, n_keep: int, n_first: int = 0, n_recent: int = 0,
+                    max_len: int = 0):
+        """Copy the n_keep slots of largest weight to the blocks of new_table
+        [B, max_blocks_per_seq].  Returns kept [B, n_kv, n_keep] (old slots)
+        and lens [B], the lengths of the new cache."""
+        c, nb = self.cfg, int(kv.batch)
+        self._expect(new_table, "new_table", (nb, c.max_blocks_per_seq), torch.int32)
+        self._expect(weights, "weights", self._pool(kv), torch.float32)
+        i32 = dict(dtype=torch.int32, device=self.device)
+        res = {"kept": torch.empty((nb, c.n_kv_heads, max(n_keep, 0)), **i32), "lens": torch.empty(nb, **i32)}
+        scratch = self._scratch(B.PRISM_CACHE_EVICT, nb, max_len)
+        io = B.prism_cache_eviction()
+        io.kv = ctypes.pointer(kv)
+        io.max_len = max_len
+        io.d_new_table = B.ptr(new_table)
+        io.d_weights = B.ptr(weights)
+        io.n_keep = n_keep
+        io.n_first = n_first
+        io.n_recent = n_recent
+        io.d_kept = B.ptr(res["kept"])
+        io.d_new_lens = B.ptr(res["lens"])
+        io.d_scratch = B.ptr(scratch)
+        io.scratch_bytes = scratch.numel()
+        B.prism_cache_evict(self.ctx, io)
+        return res
 
     def device_status(self) -> int:
         return B.prism_device_status(self.ctx)
