@@ -195,9 +195,9 @@ __device__ __forceinline__ uint32_t place_row(const CacheAttend &a, int b, int j
 constexpr int CACHE_MAXG = 8;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-// Plain form of the attention: a lane group of d / 8 lanes per slot keeps its
-// own softmax state; the groups of the wave are merged at the end.
-template <typename T, int D>
+// fp32 caches: a lane group of d / 8 lanes per slot keeps its own softmax
+// state; the groups of the wave are merged at the end.
+template <int D>
 __global__ __launch_bounds__(64) void k_cache_attend(CacheAttend a) {
   constexpr int LPR = D / 8, RPI = 64 / LPR;       // lanes per row, rows per step
   const int c = blockIdx.z, j = blockIdx.x, b = blockIdx.y, lane = threadIdx.x;
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(64) void k_cache_attend(CacheAttend a) {
   float q[CACHE_MAXG][8], o[CACHE_MAXG][8], m[CACHE_MAXG], l[CACHE_MAXG];
 #pragma unroll
   for (int h = 0; h < CACHE_MAXG; ++h) {
-    if (h < g) load8f<T>((const T *)a.q + ((size_t)b * a.nq + j * g + h) * D + 8 * li, q[h]);
+    if (h < g) load8f<float>((const float *)a.q + ((size_t)b * a.nq + j * g + h) * D + 8 * li, q[h]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       q[h][i] = h < g ? q[h][i] * a.scale : 0.f;
@@ -223,8 +223,8 @@ __global__ __launch_bounds__(64) void k_cache_attend(CacheAttend a) {
     const uint32_t row = p < p1 ? place_row(a, b, j, n, p) : NO_ROW;
     float k[8], w[8];
     if (row != NO_ROW) {
-      load8f<T>((const T *)a.v.kv.k_pool + (size_t)row * D + 8 * li, k);
-      load8f<T>((const T *)a.v.kv.v_pool + (size_t)row * D + 8 * li, w);
+      load8f<float>((const float *)a.v.kv.k_pool + (size_t)row * D + 8 * li, k);
+      load8f<float>((const float *)a.v.kv.v_pool + (size_t)row * D + 8 * li, w);
     }
 #pragma unroll
     for (int h = 0; h < CACHE_MAXG; ++h)
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(64) void k_cache_attend(CacheAttend a) {
 #pragma unroll
         for (int x = 1; x < LPR; x *= 2) s += __shfl_xor(s, x, 64);
         if (row == NO_ROW) s = -INFINITY;
-        if (a.scores && li == 0 && p < p1) a.scores[((size_t)b * a.nq + j * g + h) * a.span + p] = s;
+        if (a.scores && li == 0 && p < p1) a.scores[((size_t)b * a.nq + j * g + h) * a.ld_scores + p] = s;
         const float mn = s != s ? s : fmaxf(m[h], s);   // a NaN score reaches the sum
         if (row != NO_ROW && !(s == -INFINITY)) {
           const float al = m[h] == -INFINITY ? 0.f : exp2f(m[h] - mn), e = exp2f(s - mn);
@@ -274,73 +274,315 @@ __global__ __launch_bounds__(64) void k_cache_attend(CacheAttend a) {
     }
 }
 
-// Join of the chunks of one (sequence, query head): every chunk's sum and
-// output weighted by 2^(its maximum - the largest one).
+// The same on the matrix cores, for bf16 caches.  A wave takes tiles of TS
+// places.  K and V rows are loaded whole, D / 8 lanes per row, so that every
+// cache line is requested once, into registers, and pass through LDS into
+// operand order: the scores are MFMAs of 16 slots x 16 heads (K rows as A, the
+// queries as B), the outputs MFMAs of 16 dims x 16 heads (V transposed by the
+// LDS read as A, the probabilities, straight from the score layout, as B).
+// Each lane then holds one head's softmax state and output, so nothing is
+// exchanged but the maximum and the sum over the four lane rows.  The next
+// tile's rows are in flight while one is computed, and the block-table
+// entries of the one after it.
+//   In LDS the 16-byte pieces of row s are permuted by s, so that both the
+// A-operand reads (16 rows, one piece) and the transposing reads (4 rows, half
+// pieces of 16 dims) spread over all banks.
+//   Probabilities are multiplied as a pair of bf16 (value and remainder,
+// 2^-16), so that the output keeps the accuracy of its own rounding.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+template <int D>
+struct MfmaTile {
+  static constexpr int TS = D >= 256 ? 16 : D >= 128 ? 32 : 64;   // places per tile
+  static constexpr int LPR = D / 8, RPI = 64 / LPR, NI = TS / RPI;
+  __device__ static int swz(int s) {
+    return D >= 128 ? s & 15 : D == 64 ? (s >> 1) & 7 : (s >> 2) & 3;
+  }
+  // byte of 16-byte piece c of row s
+  __device__ static int at(int s, int c) { return (s * LPR + (c ^ swz(s))) * 16; }
+};
+
+template <int D>
+__global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
+  using M = MfmaTile<D>;
+  constexpr int TS = M::TS, LPR = M::LPR, RPI = M::RPI, NI = M::NI;
+  constexpr int NS = TS / 16, NK = D / 32, ND = D / 16;
+  __shared__ __attribute__((aligned(16))) char s_k[TS * D * 2], s_v[TS * D * 2];
+  const int c = blockIdx.z, j = blockIdx.x, b = blockIdx.y, lane = threadIdx.x, g = a.g;
+  const int col = lane & 15, q4 = lane >> 4, grp = lane / LPR, li = lane % LPR;
+  const int n = visible_slots(a.v, b, a.err);
+  const int places = a.blocks ? a.span : min(n, a.span);
+  const int p0 = c * a.chunk, p1 = min(places, p0 + a.chunk);
+  if (p0 >= places && !(a.nch == 1)) return;
+
+  const KvArgs &kv = a.v.kv;
+  const int32_t *table = kv.block_table + (size_t)b * kv.mbps;
+  const int32_t *list = a.blocks ? a.blocks + ((size_t)b * a.v.nkv + j) * a.n_list : nullptr;
+  // this lane's place of the tile at t: table column (dense) or list entry
+  // and its predecessor, in the order in which they are looked up
+  auto place = [&](int t) { return t + lane; };
+  auto ids = [&](int t, int &id, int &prev) {
+    const int p = min(place(t), p1 - 1);
+    const int bi = slot_block(kv, p);
+    if (list) {
+      id = list[bi];
+      prev = bi > 0 ? list[bi - 1] : -1;
+    } else {
+      id = bi;
+      prev = -1;
+    }
+  };
+  // the table entry of id (0 where there is none, so that the load is always made)
+  auto entry = [&](int id) { return table[id >= 0 && id < kv.mbps ? id : 0]; };
+  auto row_of = [&](int t, int id, int prev, int blk) -> uint32_t {
+    const int p = place(t);
+    const int s = p - slot_block(kv, p) * kv.bs;
+    if (lane >= TS || p >= p1 || id == -1) return NO_ROW;
+    if (list && (id < 0 || id <= prev || (long)id * kv.bs >= n)) {
+      atomicOr(a.err, ERRF_ROWS);
+      return NO_ROW;
+    }
+    if ((long)id * kv.bs + s >= n) return NO_ROW;
+    if (blk < 0 || blk >= kv.n_blocks) {
+      atomicOr(a.err, ERRF_CAPACITY);
+      return NO_ROW;
+    }
+    return ((uint32_t)blk * a.v.nkv + j) * kv.bs + s;
+  };
+  u32x4 kr[NI], vr[NI];
+  auto load = [&](uint32_t row) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const uint32_t r = __shfl(row, i * RPI + grp, 64);
+      const size_t o = (size_t)(r == NO_ROW ? 0 : r) * D + 8 * li;   // a masked place reads row 0
+      kr[i] = *(const u32x4 *)((const bf16_t *)kv.k_pool + o);
+      vr[i] = *(const u32x4 *)((const bf16_t *)kv.v_pool + o);
+    }
+  };
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x4 o[ND];
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (p0 < places) {
+    // lookups of the first two tiles, and the queries
+    int id0, pv0, id1, pv1, id2, pv2;
+    ids(p0, id0, pv0);
+    ids(p0 + TS, id1, pv1);
+    ids(p0 + 2 * TS, id2, pv2);
+    u32x4 qf[NK];
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk)
+      qf[kk] = col < g ? *(const u32x4 *)((const bf16_t *)a.q + ((size_t)b * a.nq + j * g + col) * D + 32 * kk + 8 * q4)
+                       : u32x4{0, 0, 0, 0};
+    const int e0 = entry(id0);
+    int e1 = entry(id1);
+    uint32_t row = row_of(p0, id0, pv0, e0);
+    load(row);
+    for (int t = p0; t < p1; t += TS) {
+      const uint64_t mask = __ballot(row != NO_ROW);   // lanes TS .. 63 hold none
+      constexpr uint64_t FULL = TS == 64 ? ~0ull : (1ull << (TS & 63)) - 1;
+      // rows to LDS; V rows of masked places as zeros (a NaN there must not
+      // meet a probability of 0)
+      if (mask != FULL) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+          if (!((mask >> (i * RPI + grp)) & 1)) vr[i] = u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        *(u32x4 *)(s_k + M::at(i * RPI + grp, li)) = kr[i];
+        *(u32x4 *)(s_v + M::at(i * RPI + grp, li)) = vr[i];
+      }
+      // the next tile's rows, the lookups of the one after it
+      if (t + TS < p1) {
+        row = row_of(t + TS, id1, pv1, e1);
+        id1 = id2;
+        pv1 = pv2;
+        e1 = entry(id1);
+        ids(t + 3 * TS, id2, pv2);
+        load(row);
+      }
+      wave_lds_sync();
+      // scores S[slot 16 st + 4 q4 + i][head col]
+      f32x4 sc[NS];
+#pragma unroll
+      for (int st = 0; st < NS; ++st) {
+        sc[st] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk)
+          sc[st] = Ty<bf16_t>::mma(*(const u32x4 *)(s_k + M::at(16 * st + col, 4 * kk + q4)), qf[kk], sc[st]);
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sc[st][i] = ((mask >> (16 * st + 4 * q4 + i)) & 1) ? sc[st][i] * a.scale : -INFINITY;
+          mx = fmaxf(mx, sc[st][i]);
+        }
+      if (a.scores && col < g) {
+        float *ps = a.scores + ((size_t)b * a.nq + j * g + col) * a.ld_scores + t + 4 * q4;
+#pragma unroll
+        for (int st = 0; st < NS; ++st) *(f32x4 *)(ps + 16 * st) = sc[st];
+      }
+      mx = fmaxf(mx, xor16_f(mx));
+      mx = fmaxf(mx, xor32_f(mx));
+      const float mn = fmaxf(m_run, mx);
+      // nothing but -inf so far: subtract 0, so that every p is 0 (a NaN score
+      // still makes its p, and with it the sum and the output, NaN)
+      const float ms = mn == -INFINITY ? 0.f : mn;
+      const float al = __builtin_amdgcn_exp2f(m_run - ms);
+      m_run = mn;
+      float ls = 0.f;
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sc[st][i] = __builtin_amdgcn_exp2f(sc[st][i] - ms);
+          ls += sc[st][i];
+        }
+      ls += xor16_f(ls);
+      ls += xor32_f(ls);
+      l_run = l_run * al + ls;
+      if (__ballot(al != 1.f)) {
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) o[dt] *= al;
+      }
+      s16x4 ph[NS], pl[NS];
+#pragma unroll
+      for (int st = 0; st < NS; ++st) {
+        const uint32_t h0 = pack_bf16(sc[st][0], sc[st][1]), h1 = pack_bf16(sc[st][2], sc[st][3]);
+        const uint32_t l0 = pack_bf16(sc[st][0] - __uint_as_float(h0 << 16), sc[st][1] - __uint_as_float(h0 & 0xffff0000u));
+        const uint32_t l1 = pack_bf16(sc[st][2] - __uint_as_float(h1 << 16), sc[st][3] - __uint_as_float(h1 & 0xffff0000u));
+        ph[st] = __builtin_bit_cast(s16x4, uint2{h0, h1});
+        pl[st] = __builtin_bit_cast(s16x4, uint2{l0, l1});
+      }
+      // O[dim 16 dt + 4 q4 + i][head col]
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+          const int r = 16 * st + 4 * q4 + (col >> 2);
+          const char *pv = s_v + M::at(r, 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
+          const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv);
+          o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, ph[st], o[dt], 0, 0, 0);
+          o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pl[st], o[dt], 0, 0, 0);
+        }
+      wave_lds_sync();                                 // reads done before the next tile's writes
+    }
+  }
+  if (col >= g) return;
+  const size_t hi = (size_t)b * a.nq + j * g + col;
+  if (a.nch == 1 && !a.weights) {                      // no join follows
+    const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+      *(uint2 *)((bf16_t *)a.out + hi * D + 16 * dt + 4 * q4) =
+          uint2{f2bf(o[dt][0] * inv) | (f2bf(o[dt][1] * inv) << 16), f2bf(o[dt][2] * inv) | (f2bf(o[dt][3] * inv) << 16)};
+    if (a.lse && q4 == 0) a.lse[hi] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
+    return;
+  }
+  const size_t pi = hi * a.nch + c;
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(a.po + pi * D + 16 * dt + 4 * q4) = o[dt];
+  if (q4 == 0) {
+    a.pm[pi] = m_run;
+    a.pl[pi] = l_run;
+  }
+}
+
+// Log-sum in base 2 of head hi's chunks, from every lane of a wave: M and the
+// sum l of 2^(m_c - M) l_c.
+__device__ __forceinline__ void join_stats(const CacheAttend &a, size_t hi, int nch, float &M, float &l) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY;
+  for (int c = lane; c < nch; c += 64) m = fmaxf(m, a.pm[hi * a.nch + c]);
+  M = wave_max(m);
+  M = M == -INFINITY ? 0.f : M;
+  float s = 0.f;
+  for (int c = lane; c < nch; c += 64) s += a.pl[hi * a.nch + c] * exp2f(a.pm[hi * a.nch + c] - M);
+  l = wave_sum(s);
+}
+
+// Join of the chunks: workgroup x < nq adds the outputs of query head x, every
+// chunk weighted by 2^(its maximum - the largest one), in an order that only
+// the sizes set.  The others (with slot weights) take JOIN_P places of one KV
+// head each: the sum over its g heads of 2^(score - log-sum) is added to the
+// place's slot, which one thread owns.
+constexpr int JOIN_P = 1024;
 template <typename T>
 __global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, d = a.d;
-  __shared__ float sh[8];
+  const int b = blockIdx.y, tid = threadIdx.x, wave = wave_id(), d = a.d;
   const int n = visible_slots(a.v, b, a.err);
   const int places = a.blocks ? a.span : min(n, a.span);
   const int nch = (places + a.chunk - 1) / a.chunk;
-  const size_t base = ((size_t)b * a.nq + h) * a.nch;
-  float m = -INFINITY;
-  for (int c = tid; c < nch; c += 256) m = fmaxf(m, a.pm[base + c]);
-  const float M = block_max<4>(m, sh);
-  float ls = 0.f;
-  for (int c = tid; c < nch; c += 256) {
-    const float mc = a.pm[base + c];
-    ls += mc == -INFINITY ? 0.f : a.pl[base + c] * exp2f(mc - M);
-  }
-  const float l = block_sum<4>(ls, sh);
-  if (tid < d) {
-    float o = 0.f;
-    for (int c = 0; c < nch; ++c) {
-      const float mc = a.pm[base + c];
-      if (mc != -INFINITY) o += a.po[(base + c) * d + tid] * exp2f(mc - M);
+  if ((int)blockIdx.x < a.nq) {
+    const int h = blockIdx.x;
+    const size_t hi = (size_t)b * a.nq + h;
+    __shared__ float red[256 * 4];
+    float M, l;
+    join_stats(a, hi, nch, M, l);                      // every wave for itself
+    // thread = (4 dims, chunk group)
+    const int q = d / 4, G = 256 / q, x = tid % q, grp = tid / q;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int c = grp; c < nch; c += G)
+      o += *(const f32x4 *)(a.po + (hi * a.nch + c) * d + 4 * x) * exp2f(a.pm[hi * a.nch + c] - M);
+    *(f32x4 *)(red + 4 * tid) = o;
+    __syncthreads();
+    if (grp == 0) {
+      for (int y = 1; y < G; ++y) o += *(const f32x4 *)(red + 4 * (y * q + x));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) Ty<T>::st((T *)a.out, hi * d + 4 * x + i, l == 0.f ? 0.f : o[i] / l);
     }
-    Ty<T>::st((T *)a.out, ((size_t)b * a.nq + h) * d + tid, l == 0.f ? 0.f : o / l);
+    if (tid == 0 && a.lse) a.lse[hi] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
+    return;
   }
-  if (tid == 0) {
-    const float lse = l == 0.f ? -INFINITY : M + log2f(l);
-    if (a.lse) a.lse[(size_t)b * a.nq + h] = lse * LN2;
-    if (a.lse2) a.lse2[(size_t)b * a.nq + h] = lse;
+  const int w = blockIdx.x - a.nq, j = w % a.v.nkv, g = a.g;
+  const int t0 = w / a.v.nkv * JOIN_P;
+  if (t0 >= places) return;
+  __shared__ float lse[CACHE_MAXG];
+  for (int h = wave; h < g; h += 4) {
+    float M, l;
+    join_stats(a, (size_t)b * a.nq + j * g + h, nch, M, l);
+    if ((tid & 63) == 0) lse[h] = l == 0.f ? INFINITY : M + log2f(l);   // nothing seen: every weight 0
+  }
+  __syncthreads();
+  for (int p = t0 + tid; p < min(places, t0 + JOIN_P); p += 256) {
+    const uint32_t row = place_row(a, b, j, n, p);
+    if (row == NO_ROW) continue;
+    float s = 0.f;
+    for (int h = 0; h < g; ++h) s += exp2f(a.scores[((size_t)b * a.nq + j * g + h) * a.ld_scores + p] - lse[h]);
+    a.weights[row] += s;
   }
 }
 
-// Weight of every visible slot: the sum of its probabilities over the g heads
-// of its KV head, added to the slot's accumulated weight (one thread owns it).
-__global__ __launch_bounds__(256) void k_cache_weigh(CacheAttend a) {
-  const int j = blockIdx.y, b = blockIdx.z, g = a.g;
-  const int n = visible_slots(a.v, b, a.err);
-  const int places = a.blocks ? a.span : min(n, a.span);
-  const int p = blockIdx.x * 256 + threadIdx.x;
-  if (p >= places) return;
-  const uint32_t row = place_row(a, b, j, n, p);
-  if (row == NO_ROW) return;
-  float w = 0.f;
-  for (int h = 0; h < g; ++h) {
-    const size_t hi = (size_t)b * a.nq + j * g + h;
-    const float lse = a.lse2[hi];
-    if (lse != -INFINITY) w += exp2f(a.scores[hi * a.span + p] - lse);
-  }
-  a.weights[row] += w;
-}
-
-template <typename T>
-static void attend_d(const CacheAttend &a, hipStream_t s) {
-  const dim3 g(a.v.nkv, a.v.kv.n_seq, a.nch);
-  if (a.d == 32) hipLaunchKernelGGL((k_cache_attend<T, 32>), g, dim3(64), 0, s, a);
-  else if (a.d == 64) hipLaunchKernelGGL((k_cache_attend<T, 64>), g, dim3(64), 0, s, a);
-  else if (a.d == 128) hipLaunchKernelGGL((k_cache_attend<T, 128>), g, dim3(64), 0, s, a);
-  else hipLaunchKernelGGL((k_cache_attend<T, 256>), g, dim3(64), 0, s, a);
-  hipLaunchKernelGGL(k_cache_join<T>, dim3(a.nq, a.v.kv.n_seq), dim3(256), 0, s, a);
-  if (a.weights)
-    hipLaunchKernelGGL(k_cache_weigh, dim3((a.span + 255) / 256, a.v.nkv, a.v.kv.n_seq), dim3(256), 0, s, a);
+static void join(bool bf16, const CacheAttend &a, hipStream_t s) {
+  const dim3 g(a.nq + (a.weights ? a.v.nkv * ((a.span + JOIN_P - 1) / JOIN_P) : 0), a.v.kv.n_seq);
+  if (bf16) hipLaunchKernelGGL(k_cache_join<bf16_t>, g, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_cache_join<float>, g, dim3(256), 0, s, a);
 }
 void launch_cache_attend(bool bf16, const CacheAttend &a, hipStream_t s) {
-  if (bf16) attend_d<bf16_t>(a, s);
-  else attend_d<float>(a, s);
+  const dim3 g(a.v.nkv, a.v.kv.n_seq, a.nch), t(64);
+  if (bf16) {
+    if (a.d == 32) hipLaunchKernelGGL((k_cache_attend_mfma<32>), g, t, 0, s, a);
+    else if (a.d == 64) hipLaunchKernelGGL((k_cache_attend_mfma<64>), g, t, 0, s, a);
+    else if (a.d == 128) hipLaunchKernelGGL((k_cache_attend_mfma<128>), g, t, 0, s, a);
+    else hipLaunchKernelGGL((k_cache_attend_mfma<256>), g, t, 0, s, a);
+    if (a.nch > 1 || a.weights) join(true, a, s);
+    return;
+  }
+  if (a.d == 32) hipLaunchKernelGGL((k_cache_attend<32>), g, t, 0, s, a);
+  else if (a.d == 64) hipLaunchKernelGGL((k_cache_attend<64>), g, t, 0, s, a);
+  else if (a.d == 128) hipLaunchKernelGGL((k_cache_attend<128>), g, t, 0, s, a);
+  else hipLaunchKernelGGL((k_cache_attend<256>), g, t, 0, s, a);
+  join(false, a, s);
 }
 
 // ---------------------------------------------------------------- summaries

@@ -386,11 +386,11 @@ struct CacheAttend {
   const void *q;                        // [B, nq, d]
   const int32_t *blocks; int n_list;    // [B, nkv, n_list] or NULL
   int span;                             // places per sequence: max_len, or all of a list's first
-                                        // mbps entries (row length of scores)
+                                        // mbps entries
   int chunk, nch;                       // places per workgroup, workgroups per (sequence, KV head)
   float scale;                          // log2(e) / sqrt(d)
   float *pm, *pl, *po;                  // partials [B, nq, nch] / [.., d]
-  float *scores, *lse2;                 // [B, nq, span] / [B, nq] in base 2 (weights only)
+  float *scores; int ld_scores;         // [B, nq, ld_scores] in base 2 (weights only)
   void *out; float *lse;                // [B, nq, d] / [B, nq] or NULL
   float *weights;                       // slot weights, or NULL
   uint32_t *err;

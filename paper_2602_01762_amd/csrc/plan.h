@@ -365,6 +365,8 @@ constexpr int CACHE_MAX_CHUNK = 1024;   // bounds the tail of a ragged batch
 struct CachePlan {
   int chunk, nch;
 };
+// row length of the scores kept for the slot weights: whole tiles
+inline int cache_score_row(int span) { return (span + CACHE_TILE - 1) / CACHE_TILE * CACHE_TILE; }
 inline CachePlan cache_plan(int units, int span) {
   const long want = units >= CACHE_WAVES ? 1 : CACHE_WAVES / units;
   long chunk = (span + want - 1) / want;

@@ -1509,7 +1509,7 @@ static size_t cache_scratch(const prism_ctx *c, int call, int B, int span) {
   const size_t parts = (size_t)B * c->nq * p.nch;
   size_t n = ((parts * 4 + pad) & ~pad) * 2 + ((parts * c->d * 4 + pad) & ~pad);
   if (call == PRISM_CACHE_ATTEND_WEIGHTS)
-    n += (((size_t)B * c->nq * 4 + pad) & ~pad) + (size_t)B * c->nq * span * 4;
+    n += (size_t)B * c->nq * cache_score_row(span) * 4;
   return n;
 }
 static prism_status check_scratch(prism_ctx *c, const void *p, uint64_t bytes, size_t need) {
@@ -1609,10 +1609,8 @@ prism_status prism_cache_attend(prism_ctx *c, const prism_cache_attention *io, v
   carve(ws, (void **)&a.pm, parts * 4);
   carve(ws, (void **)&a.pl, parts * 4);
   carve(ws, (void **)&a.po, parts * c->d * 4);
-  if (io->d_weights) {
-    carve(ws, (void **)&a.lse2, (size_t)B * c->nq * 4);
-    a.scores = (float *)ws;
-  }
+  a.scores = io->d_weights ? (float *)ws : nullptr;
+  a.ld_scores = cache_score_row(span);
   a.out = io->d_out;
   a.lse = io->d_lse;
   a.weights = io->d_weights;
