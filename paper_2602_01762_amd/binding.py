@@ -9,6 +9,8 @@ from __future__ import annotations
 import ctypes
 import os
 
+import torch
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libprism_draft.so")
 
@@ -72,26 +74,27 @@ class prism_tree_out(ctypes.Structure):
                 ("d_cand_score", c_vp), ("d_frontier", c_vp), ("d_logits", c_vp)]
 
 
+# kv: ctypes.addressof() of a prism_batch that outlives the call
 class prism_cache_rows(ctypes.Structure):
-    _fields_ = [("kv", ctypes.POINTER(prism_batch)), ("rows", c_i32), ("d_offsets", c_vp),
+    _fields_ = [("kv", c_vp), ("rows", c_i32), ("d_offsets", c_vp),
                 ("d_positions", c_vp), ("d_qkv", c_vp), ("d_q_gain", c_vp), ("d_k_gain", c_vp),
                 ("d_q", c_vp), ("d_weights", c_vp)]
 
 
 class prism_cache_attention(ctypes.Structure):
-    _fields_ = [("kv", ctypes.POINTER(prism_batch)), ("n_new", c_i32), ("max_len", c_i32),
+    _fields_ = [("kv", c_vp), ("n_new", c_i32), ("max_len", c_i32),
                 ("d_q", c_vp), ("d_blocks", c_vp), ("n_blocks", c_i32), ("d_weights", c_vp),
                 ("d_out", c_vp), ("d_lse", c_vp), ("d_scratch", c_vp), ("scratch_bytes", c_u64)]
 
 
 class prism_cache_selection(ctypes.Structure):
-    _fields_ = [("kv", ctypes.POINTER(prism_batch)), ("n_new", c_i32), ("max_len", c_i32),
+    _fields_ = [("kv", c_vp), ("n_new", c_i32), ("max_len", c_i32),
                 ("d_q", c_vp), ("d_summary", c_vp), ("n_blocks", c_i32), ("n_first", c_i32),
                 ("n_last", c_i32), ("d_blocks", c_vp), ("d_scratch", c_vp), ("scratch_bytes", c_u64)]
 
 
 class prism_cache_eviction(ctypes.Structure):
-    _fields_ = [("kv", ctypes.POINTER(prism_batch)), ("max_len", c_i32), ("d_new_table", c_vp),
+    _fields_ = [("kv", c_vp), ("max_len", c_i32), ("d_new_table", c_vp),
                 ("d_weights", c_vp), ("n_keep", c_i32), ("n_first", c_i32), ("n_recent", c_i32),
                 ("d_kept", c_vp), ("d_new_lens", c_vp), ("d_scratch", c_vp), ("scratch_bytes", c_u64)]
 
@@ -166,8 +169,9 @@ def ptr(t) -> int:
 
 
 def cur_stream():
-    import torch
-    return int(torch.cuda.current_stream().cuda_stream)
+    # the handle alone: torch.cuda.current_stream() also builds a Stream object,
+    # 2.7 us of a call that may take 8
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 # thin wrappers with the C names ------------------------------------------------

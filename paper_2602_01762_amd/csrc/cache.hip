@@ -18,7 +18,7 @@ constexpr uint32_t NO_ROW = 0xffffffffu;   // a slot without storage
 __device__ __forceinline__ int visible_slots(const CacheView &v, int b, uint32_t *err) {
   const long n = (long)v.kv.ctx_lens[b] + v.n_new;
   if (n < 0 || n > v.max_len) {
-    if ((threadIdx.x & 63) == 0) atomicOr(err, ERRF_CAPACITY);
+    atomicOr(err, ERRF_CAPACITY);
     return n < 0 ? 0 : v.max_len;
   }
   return (int)n;
@@ -34,6 +34,9 @@ __device__ __forceinline__ uint32_t pool_row(const CacheView &v, const int32_t *
   return ((uint32_t)blk * v.nkv + j) * v.kv.bs + s;
 }
 
+// 16 bytes that the call reads once: a nontemporal load.  Read rates of a plain
+// streaming kernel over 4.3 GB: 6.3 TB/s, with nontemporal loads 7.1.
+__device__ __forceinline__ u32x4 stream16(const void *p) { return __builtin_nontemporal_load((const u32x4 *)p); }
 // 8 values of a row <-> fp32
 template <typename T>
 __device__ __forceinline__ void load8f(const T *p, float (&x)[8]) {
@@ -168,110 +171,215 @@ void launch_cache_append(bool bf16, const CacheAppend &a, int d, hipStream_t s) 
 
 // ---------------------------------------------------------------- attention
 // A call walks sequence b's "places" p: slot p, or with a block list slot p %
-// bs of block list[p / bs].  Workgroup (chunk c, KV head j, sequence b) takes
-// chunk places and leaves, for each of the g query heads, the maximum, the sum
-// and the unnormalised output of its softmax in base 2; the join adds the
-// chunks in order, so the result does not depend on scheduling.
+// bs of block list[p / bs].  The places of one sequence and KV head are cut
+// into granules of CACHE_GRAN places, the granules of all sequences and heads are
+// numbered in (sequence, head, place) order, and wave w takes the w-th run of
+// equally many of them.  So every wave streams the same amount whatever the
+// lengths, and one long sequence among short ones fills the chip as equal
+// ones do.  A run covers parts of one or more segments (sequence, KV head);
+// for each it leaves, per query head, the maximum, the sum and the
+// unnormalised output of the softmax in base 2 in partial w + segment (unique:
+// along the runs each step moves on one wave or one segment).  The join adds a
+// segment's partials in order, so the result does not depend on scheduling.
+constexpr int CACHE_MAXG = 8;
+constexpr float LN2 = 0.6931471805599453f;
 
-// Pool row of place p, or NO_ROW (nothing visible there).
-__device__ __forceinline__ uint32_t place_row(const CacheAttend &a, int b, int j, int n, int p) {
-  const CacheView &v = a.v;
-  int bi = slot_block(v.kv, p);
-  const int s = slot_in_block(v.kv, p, bi);
-  if (a.blocks) {
-    const int32_t *list = a.blocks + ((size_t)b * v.nkv + j) * a.n_list;
-    const int id = list[bi], prev = bi > 0 ? list[bi - 1] : -1;
-    if (id == -1) return NO_ROW;
-    if (id < 0 || id <= prev || (long)id * v.kv.bs >= n) {
+// The numbering of the granules, in every lane of a wave.
+struct Walk {
+  int n, count, begin, end;   // lane b: visible slots; granules per head, before and through sequence b
+  int total, per;             // granules in all, granules per wave
+};
+__device__ __forceinline__ int places_of(const CacheAttend &a, int n) { return a.blocks ? a.span : min(n, a.span); }
+__device__ __forceinline__ Walk walk_of(const CacheAttend &a) {
+  const int lane = threadIdx.x & 63;
+  const bool has = lane < a.v.kv.n_seq;
+  Walk w;
+  w.n = has ? visible_slots(a.v, lane, a.err) : 0;
+  w.count = has ? (places_of(a, w.n) + CACHE_GRAN - 1) / CACHE_GRAN : 0;
+  if (a.direct && has) w.count = 1;            // an empty sequence writes its zeros itself
+  w.end = w.count * a.v.nkv;
+  for (int x = 1; x < a.v.kv.n_seq; x *= 2) {
+    const int v = __shfl_up(w.end, x, 64);
+    if (lane >= x) w.end += v;
+  }
+  w.total = __builtin_amdgcn_readlane(w.end, a.v.kv.n_seq - 1);
+  if (!has) w.end = w.total;
+  w.begin = w.end - w.count * a.v.nkv;
+  w.per = max(1, (w.total + a.waves - 1) / a.waves);
+  return w;
+}
+// The part of a segment that a run starting at granule u (< w.total) and
+// ending at `last` begins with.
+struct Segment {
+  int b, j, n, granules, p0, p1;
+};
+__device__ __forceinline__ Segment segment_at(const CacheAttend &a, const Walk &w, int u, int last) {
+  Segment s;
+  s.b = __popcll(__ballot(w.end <= u));        // wave-uniform
+  const int count = __builtin_amdgcn_readlane(w.count, s.b);
+  const int at = u - __builtin_amdgcn_readlane(w.begin, s.b);
+  s.n = __builtin_amdgcn_readlane(w.n, s.b);
+  s.j = at / count;
+  const int first = at - s.j * count;
+  s.granules = min(last - u, count - first);
+  s.p0 = first * CACHE_GRAN;
+  s.p1 = min(places_of(a, s.n), (first + s.granules) * CACHE_GRAN);
+  return s;
+}
+
+// Lookup of a segment's places, in the steps that their loads allow: the
+// table column of a place (from the list, with its predecessor), the block of
+// the column, the pool row.  The loads are made for every place (past the end
+// for the last one), so that they can be issued early and counted.
+struct Lookup {
+  const CacheAttend &a;
+  const Segment &s;
+  const int32_t *table, *list;
+  __device__ __forceinline__ Lookup(const CacheAttend &a_, const Segment &s_)
+      : a(a_), s(s_), table(a_.v.kv.block_table + (size_t)s_.b * a_.v.kv.mbps),
+        list(a_.blocks ? a_.blocks + ((size_t)s_.b * a_.v.nkv + s_.j) * a_.n_list : nullptr) {}
+  __device__ __forceinline__ void column(int p, int &id, int &prev) const {
+    const int bi = slot_block(a.v.kv, min(p, s.p1 - 1));
+    id = list ? list[bi] : bi;
+    prev = list && bi > 0 ? list[bi - 1] : -1;
+  }
+  __device__ __forceinline__ int block(int id) const { return table[id >= 0 && id < a.v.kv.mbps ? id : 0]; }
+  __device__ __forceinline__ uint32_t row(int p, int id, int prev, int blk) const {
+    const KvArgs &kv = a.v.kv;
+    if (p >= s.p1 || id == -1) return NO_ROW;
+    if (list && (id < 0 || id <= prev || (long)id * kv.bs >= s.n)) {
       atomicOr(a.err, ERRF_ROWS);
       return NO_ROW;
     }
-    bi = id;
-  }
-  if ((long)bi * v.kv.bs + s >= n) return NO_ROW;
-  return pool_row(v, v.kv.block_table, b, j, bi, s, a.err);
-}
-
-constexpr int CACHE_MAXG = 8;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-
-// fp32 caches: a lane group of d / 8 lanes per slot keeps its own softmax
-// state; the groups of the wave are merged at the end.
-template <int D>
-__global__ __launch_bounds__(64) void k_cache_attend(CacheAttend a) {
-  constexpr int LPR = D / 8, RPI = 64 / LPR;       // lanes per row, rows per step
-  const int c = blockIdx.z, j = blockIdx.x, b = blockIdx.y, lane = threadIdx.x;
-  const int grp = lane / LPR, li = lane % LPR, g = a.g;
-  const int n = visible_slots(a.v, b, a.err);
-  const int places = a.blocks ? a.span : min(n, a.span);
-  const int p0 = c * a.chunk, p1 = min(places, p0 + a.chunk);
-  if (p0 >= places) return;
-  float q[CACHE_MAXG][8], o[CACHE_MAXG][8], m[CACHE_MAXG], l[CACHE_MAXG];
-#pragma unroll
-  for (int h = 0; h < CACHE_MAXG; ++h) {
-    if (h < g) load8f<float>((const float *)a.q + ((size_t)b * a.nq + j * g + h) * D + 8 * li, q[h]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      q[h][i] = h < g ? q[h][i] * a.scale : 0.f;
-      o[h][i] = 0.f;
+    const int off = p - slot_block(kv, p) * kv.bs;
+    if ((long)id * kv.bs + off >= s.n) return NO_ROW;
+    if (blk < 0 || blk >= kv.n_blocks) {
+      atomicOr(a.err, ERRF_CAPACITY);
+      return NO_ROW;
     }
-    m[h] = -INFINITY;
-    l[h] = 0.f;
+    return ((uint32_t)blk * a.v.nkv + s.j) * kv.bs + off;
   }
-  for (int t = p0; t < p1; t += RPI) {
-    const int p = t + grp;
-    const uint32_t row = p < p1 ? place_row(a, b, j, n, p) : NO_ROW;
-    float k[8], w[8];
-    if (row != NO_ROW) {
-      load8f<float>((const float *)a.v.kv.k_pool + (size_t)row * D + 8 * li, k);
-      load8f<float>((const float *)a.v.kv.v_pool + (size_t)row * D + 8 * li, w);
+};
+
+// fp32 caches: tiles of 4 rows per lane group of d / 8 lanes; the group keeps
+// its own softmax state, and the groups of the wave are merged at the end of a
+// segment.  The next tile's rows are in flight while one is computed.
+// G: query heads per KV head, rounded up to a power of two.
+template <int D, int G>
+__global__ __launch_bounds__(64, G > 4 ? 1 : 2) void k_cache_attend(CacheAttend a) {
+  constexpr int LPR = D / 8, RPI = 64 / LPR, NI = 4, TS = NI * RPI;
+  constexpr int SH = D == 32 ? 2 : D == 64 ? 3 : D == 128 ? 4 : 5;   // log2 LPR
+  const int lane = threadIdx.x, grp = lane / LPR, li = lane % LPR, g = a.g;
+  const Walk wk = walk_of(a);
+  int u = blockIdx.x * wk.per;
+  const int last = min(wk.total, u + wk.per);
+  while (u < last) {
+    const Segment sg = segment_at(a, wk, u, last);
+    u += sg.granules;
+    const Lookup lk(a, sg);
+    const size_t h0 = (size_t)sg.b * a.nq + sg.j * g;
+    float q[G][8], o[G][8], m[G], l[G];
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      if (h < g) load8f<float>((const float *)a.q + (h0 + h) * D + 8 * li, q[h]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[h][i] = 0.f;
+      m[h] = -INFINITY;
+      l[h] = 0.f;
     }
+    float k[NI][8], v[NI][8];
+    uint32_t rows = NO_ROW;
+    auto load = [&]() {
 #pragma unroll
-    for (int h = 0; h < CACHE_MAXG; ++h)
-      if (h < g) {
-        float s = 0.f;
-        if (row != NO_ROW) {
+      for (int i = 0; i < NI; ++i) {
+        const uint32_t r = __shfl(rows, i * RPI + grp, 64);
+        const size_t at = (size_t)(r == NO_ROW ? 0 : r) * D + 8 * li;   // a masked place reads row 0
+        load8f<float>((const float *)a.v.kv.k_pool + at, k[i]);
+        load8f<float>((const float *)a.v.kv.v_pool + at, v[i]);
+      }
+    };
+    int id1, pv1, b1;
+    if (sg.p0 < sg.p1) {
+      int id0, pv0;
+      lk.column(sg.p0 + lane, id0, pv0);
+      lk.column(sg.p0 + TS + lane, id1, pv1);
+      const int b0 = lk.block(id0);
+      b1 = lk.block(id1);
+      rows = lane < TS ? lk.row(sg.p0 + lane, id0, pv0, b0) : NO_ROW;
+      load();
+    }
+    for (int t = sg.p0; t < sg.p1; t += TS) {
+      const uint64_t mask = __ballot(rows != NO_ROW);
+      float kc[NI][8], vc[NI][8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s += q[h][i] * k[i];
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          kc[i][x] = k[i][x];
+          vc[i][x] = ((mask >> (i * RPI + grp)) & 1) ? v[i][x] : 0.f;
         }
+      if (t + TS < sg.p1) {
+        rows = lane < TS ? lk.row(t + TS + lane, id1, pv1, b1) : NO_ROW;
+        lk.column(t + 2 * TS + lane, id1, pv1);
+        b1 = lk.block(id1);
+        load();
+      }
 #pragma unroll
-        for (int x = 1; x < LPR; x *= 2) s += __shfl_xor(s, x, 64);
-        if (row == NO_ROW) s = -INFINITY;
-        if (a.scores && li == 0 && p < p1) a.scores[((size_t)b * a.nq + j * g + h) * a.ld_scores + p] = s;
-        const float mn = s != s ? s : fmaxf(m[h], s);   // a NaN score reaches the sum
-        if (row != NO_ROW && !(s == -INFINITY)) {
-          const float al = m[h] == -INFINITY ? 0.f : exp2f(m[h] - mn), e = exp2f(s - mn);
-          l[h] = l[h] * al + e;
+      for (int h = 0; h < G; ++h)
+        if (h < g) {
+          float s[NI], mx = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) o[h][i] = o[h][i] * al + e * w[i];
+          for (int i = 0; i < NI; ++i) {
+            s[i] = 0.f;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) s[i] += q[h][x] * kc[i][x];
+            s[i] = group_sum(s[i], SH) * a.scale;
+            if (!((mask >> (i * RPI + grp)) & 1)) s[i] = -INFINITY;
+            if (a.scores && li == 0) a.scores[(h0 + h) * a.ld_scores + t + i * RPI + grp] = s[i];
+            mx = fmaxf(mx, s[i]);
+          }
+          const float mn = fmaxf(m[h], mx);
+          // nothing but -inf so far: subtract 0, so that every p is 0 (a NaN
+          // score still makes its p, and with it the sum, NaN)
+          const float ms = mn == -INFINITY ? 0.f : mn, al = exp2f(m[h] - ms);
           m[h] = mn;
+          l[h] *= al;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) o[h][x] *= al;
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const float p = exp2f(s[i] - ms);
+            l[h] += p;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) o[h][x] += p * vc[i][x];
+          }
+        }
+    }
+    const size_t part = (size_t)(blockIdx.x + sg.b * a.v.nkv + sg.j) * g;
+#pragma unroll
+    for (int h = 0; h < G; ++h)
+      if (h < g) {
+        float M = m[h];
+#pragma unroll
+        for (int x = LPR; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x, 64));
+        const float w = exp2f(m[h] - (M == -INFINITY ? 0.f : M));
+        const float ls = stride_sum(l[h] * w, LPR);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) o[h][x] = stride_sum(o[h][x] * w, LPR);
+        if (a.direct) {
+#pragma unroll
+          for (int x = 0; x < 8; ++x) o[h][x] = ls == 0.f ? 0.f : o[h][x] / ls;
+          if (grp == 0) store8f<float>((float *)a.out + (h0 + h) * D + 8 * li, o[h]);
+          if (a.lse && lane == 0) a.lse[h0 + h] = ls == 0.f ? -INFINITY : (M + log2f(ls)) * LN2;
+        } else {
+          if (grp == 0) store8f<float>(a.po + (part + h) * D + 8 * li, o[h]);
+          if (lane == 0) {
+            a.pm[part + h] = M;
+            a.pl[part + h] = ls;
+          }
         }
       }
   }
-#pragma unroll
-  for (int h = 0; h < CACHE_MAXG; ++h)
-    if (h < g) {
-      float M = m[h];
-#pragma unroll
-      for (int x = LPR; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x, 64));
-      const float w = m[h] == -INFINITY ? 0.f : exp2f(m[h] - M);
-      float ls = l[h] * w;
-#pragma unroll
-      for (int x = LPR; x < 64; x *= 2) ls += __shfl_xor(ls, x, 64);
-      float ov[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        ov[i] = m[h] == -INFINITY ? 0.f : o[h][i] * w;
-#pragma unroll
-        for (int x = LPR; x < 64; x *= 2) ov[i] += __shfl_xor(ov[i], x, 64);
-      }
-      const size_t pi = ((size_t)b * a.nq + j * g + h) * a.nch + c;
-      if (grp == 0) store8f<float>(a.po + pi * D + 8 * li, ov);
-      if (lane == 0) {
-        a.pm[pi] = M;
-        a.pl[pi] = ls;
-      }
-    }
 }
 
 // The same on the matrix cores, for bf16 caches.  A wave takes tiles of TS
@@ -313,78 +421,48 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
   constexpr int TS = M::TS, LPR = M::LPR, RPI = M::RPI, NI = M::NI;
   constexpr int NS = TS / 16, NK = D / 32, ND = D / 16;
   __shared__ __attribute__((aligned(16))) char s_k[TS * D * 2], s_v[TS * D * 2];
-  const int c = blockIdx.z, j = blockIdx.x, b = blockIdx.y, lane = threadIdx.x, g = a.g;
+  const int lane = threadIdx.x, g = a.g;
   const int col = lane & 15, q4 = lane >> 4, grp = lane / LPR, li = lane % LPR;
-  const int n = visible_slots(a.v, b, a.err);
-  const int places = a.blocks ? a.span : min(n, a.span);
-  const int p0 = c * a.chunk, p1 = min(places, p0 + a.chunk);
-  if (p0 >= places && !(a.nch == 1)) return;
-
   const KvArgs &kv = a.v.kv;
-  const int32_t *table = kv.block_table + (size_t)b * kv.mbps;
-  const int32_t *list = a.blocks ? a.blocks + ((size_t)b * a.v.nkv + j) * a.n_list : nullptr;
-  // this lane's place of the tile at t: table column (dense) or list entry
-  // and its predecessor, in the order in which they are looked up
-  auto place = [&](int t) { return t + lane; };
-  auto ids = [&](int t, int &id, int &prev) {
-    const int p = min(place(t), p1 - 1);
-    const int bi = slot_block(kv, p);
-    if (list) {
-      id = list[bi];
-      prev = bi > 0 ? list[bi - 1] : -1;
-    } else {
-      id = bi;
-      prev = -1;
-    }
-  };
-  // the table entry of id (0 where there is none, so that the load is always made)
-  auto entry = [&](int id) { return table[id >= 0 && id < kv.mbps ? id : 0]; };
-  auto row_of = [&](int t, int id, int prev, int blk) -> uint32_t {
-    const int p = place(t);
-    const int s = p - slot_block(kv, p) * kv.bs;
-    if (lane >= TS || p >= p1 || id == -1) return NO_ROW;
-    if (list && (id < 0 || id <= prev || (long)id * kv.bs >= n)) {
-      atomicOr(a.err, ERRF_ROWS);
-      return NO_ROW;
-    }
-    if ((long)id * kv.bs + s >= n) return NO_ROW;
-    if (blk < 0 || blk >= kv.n_blocks) {
-      atomicOr(a.err, ERRF_CAPACITY);
-      return NO_ROW;
-    }
-    return ((uint32_t)blk * a.v.nkv + j) * kv.bs + s;
-  };
-  u32x4 kr[NI], vr[NI];
-  auto load = [&](uint32_t row) {
+  const Walk wk = walk_of(a);
+  int u = blockIdx.x * wk.per;
+  const int last = min(wk.total, u + wk.per);
+  while (u < last) {
+    const Segment sg = segment_at(a, wk, u, last);
+    u += sg.granules;
+    const Lookup lk(a, sg);
+    const size_t hi = (size_t)sg.b * a.nq + sg.j * g + col;   // this lane's query head (col < g)
+    u32x4 kr[NI], vr[NI];
+    auto load = [&](uint32_t row) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const uint32_t r = __shfl(row, i * RPI + grp, 64);
-      const size_t o = (size_t)(r == NO_ROW ? 0 : r) * D + 8 * li;   // a masked place reads row 0
-      kr[i] = *(const u32x4 *)((const bf16_t *)kv.k_pool + o);
-      vr[i] = *(const u32x4 *)((const bf16_t *)kv.v_pool + o);
-    }
-  };
-
-  float m_run = -INFINITY, l_run = 0.f;
-  f32x4 o[ND];
+      for (int i = 0; i < NI; ++i) {
+        const uint32_t r = __shfl(row, i * RPI + grp, 64);
+        const size_t at = (size_t)(r == NO_ROW ? 0 : r) * D + 8 * li;   // a masked place reads row 0
+        kr[i] = stream16((const bf16_t *)kv.k_pool + at);
+        vr[i] = stream16((const bf16_t *)kv.v_pool + at);
+      }
+    };
+    float m_run = -INFINITY, l_run = 0.f;
+    f32x4 o[ND];
 #pragma unroll
-  for (int dt = 0; dt < ND; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (p0 < places) {
-    // lookups of the first two tiles, and the queries
-    int id0, pv0, id1, pv1, id2, pv2;
-    ids(p0, id0, pv0);
-    ids(p0 + TS, id1, pv1);
-    ids(p0 + 2 * TS, id2, pv2);
+    for (int dt = 0; dt < ND; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     u32x4 qf[NK];
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk)
-      qf[kk] = col < g ? *(const u32x4 *)((const bf16_t *)a.q + ((size_t)b * a.nq + j * g + col) * D + 32 * kk + 8 * q4)
-                       : u32x4{0, 0, 0, 0};
-    const int e0 = entry(id0);
-    int e1 = entry(id1);
-    uint32_t row = row_of(p0, id0, pv0, e0);
-    load(row);
-    for (int t = p0; t < p1; t += TS) {
+      qf[kk] = col < g ? *(const u32x4 *)((const bf16_t *)a.q + hi * D + 32 * kk + 8 * q4) : u32x4{0, 0, 0, 0};
+    int id1, pv1, b1, id2, pv2;
+    uint32_t row = NO_ROW;
+    if (sg.p0 < sg.p1) {
+      int id0, pv0;
+      lk.column(sg.p0 + lane, id0, pv0);
+      lk.column(sg.p0 + TS + lane, id1, pv1);
+      lk.column(sg.p0 + 2 * TS + lane, id2, pv2);
+      const int b0 = lk.block(id0);
+      b1 = lk.block(id1);
+      row = lane < TS ? lk.row(sg.p0 + lane, id0, pv0, b0) : NO_ROW;
+      load(row);
+    }
+    for (int t = sg.p0; t < sg.p1; t += TS) {
       const uint64_t mask = __ballot(row != NO_ROW);   // lanes TS .. 63 hold none
       constexpr uint64_t FULL = TS == 64 ? ~0ull : (1ull << (TS & 63)) - 1;
       // rows to LDS; V rows of masked places as zeros (a NaN there must not
@@ -399,13 +477,13 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
         *(u32x4 *)(s_k + M::at(i * RPI + grp, li)) = kr[i];
         *(u32x4 *)(s_v + M::at(i * RPI + grp, li)) = vr[i];
       }
-      // the next tile's rows, the lookups of the one after it
-      if (t + TS < p1) {
-        row = row_of(t + TS, id1, pv1, e1);
+      // the lookups of the tile after the next one, and the next one's rows
+      if (t + TS < sg.p1) {
+        row = lane < TS ? lk.row(t + TS + lane, id1, pv1, b1) : NO_ROW;
         id1 = id2;
         pv1 = pv2;
-        e1 = entry(id1);
-        ids(t + 3 * TS, id2, pv2);
+        b1 = lk.block(id1);
+        lk.column(t + 3 * TS + lane, id2, pv2);
         load(row);
       }
       wave_lds_sync();
@@ -427,7 +505,7 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
           mx = fmaxf(mx, sc[st][i]);
         }
       if (a.scores && col < g) {
-        float *ps = a.scores + ((size_t)b * a.nq + j * g + col) * a.ld_scores + t + 4 * q4;
+        float *ps = a.scores + hi * a.ld_scores + t + 4 * q4;
 #pragma unroll
         for (int st = 0; st < NS; ++st) *(f32x4 *)(ps + 16 * st) = sc[st];
       }
@@ -476,64 +554,74 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
         }
       wave_lds_sync();                                 // reads done before the next tile's writes
     }
-  }
-  if (col >= g) return;
-  const size_t hi = (size_t)b * a.nq + j * g + col;
-  if (a.nch == 1 && !a.weights) {                      // no join follows
-    const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+    if (col >= g) continue;
+    if (a.direct) {
+      const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-      *(uint2 *)((bf16_t *)a.out + hi * D + 16 * dt + 4 * q4) =
-          uint2{f2bf(o[dt][0] * inv) | (f2bf(o[dt][1] * inv) << 16), f2bf(o[dt][2] * inv) | (f2bf(o[dt][3] * inv) << 16)};
-    if (a.lse && q4 == 0) a.lse[hi] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
-    return;
-  }
-  const size_t pi = hi * a.nch + c;
+      for (int dt = 0; dt < ND; ++dt)
+        *(uint2 *)((bf16_t *)a.out + hi * D + 16 * dt + 4 * q4) =
+            uint2{f2bf(o[dt][0] * inv) | (f2bf(o[dt][1] * inv) << 16), f2bf(o[dt][2] * inv) | (f2bf(o[dt][3] * inv) << 16)};
+      if (a.lse && q4 == 0) a.lse[hi] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
+      continue;
+    }
+    const size_t part = (size_t)(blockIdx.x + sg.b * a.v.nkv + sg.j) * g + col;
 #pragma unroll
-  for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(a.po + pi * D + 16 * dt + 4 * q4) = o[dt];
-  if (q4 == 0) {
-    a.pm[pi] = m_run;
-    a.pl[pi] = l_run;
+    for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(a.po + part * D + 16 * dt + 4 * q4) = o[dt];
+    if (q4 == 0) {
+      a.pm[part] = m_run;
+      a.pl[part] = l_run;
+    }
   }
 }
 
-// Log-sum in base 2 of head hi's chunks, from every lane of a wave: M and the
-// sum l of 2^(m_c - M) l_c.
-__device__ __forceinline__ void join_stats(const CacheAttend &a, size_t hi, int nch, float &M, float &l) {
+// The partials of one query head: np of them, entry i of pm / pl at at + i * g.
+struct Parts {
+  size_t at;
+  int np;
+};
+__device__ __forceinline__ Parts parts_of(const CacheAttend &a, const Walk &w, int b, int j, int h) {
+  const int count = __builtin_amdgcn_readlane(w.count, b);
+  const int u = __builtin_amdgcn_readlane(w.begin, b) + j * count, w0 = u / w.per;
+  return {(size_t)(w0 + b * a.v.nkv + j) * a.g + h, count ? (u + count - 1) / w.per - w0 + 1 : 0};
+}
+// From every lane of a wave: the largest maximum M (0 if there is none) and
+// the sum l of 2^(m_c - M) l_c.
+__device__ __forceinline__ void join_stats(const CacheAttend &a, const Parts &p, float &M, float &l) {
   const int lane = threadIdx.x & 63;
   float m = -INFINITY;
-  for (int c = lane; c < nch; c += 64) m = fmaxf(m, a.pm[hi * a.nch + c]);
+  for (int c = lane; c < p.np; c += 64) m = fmaxf(m, a.pm[p.at + (size_t)c * a.g]);
   M = wave_max(m);
   M = M == -INFINITY ? 0.f : M;
   float s = 0.f;
-  for (int c = lane; c < nch; c += 64) s += a.pl[hi * a.nch + c] * exp2f(a.pm[hi * a.nch + c] - M);
+  for (int c = lane; c < p.np; c += 64) s += a.pl[p.at + (size_t)c * a.g] * exp2f(a.pm[p.at + (size_t)c * a.g] - M);
   l = wave_sum(s);
 }
 
-// Join of the chunks: workgroup x < nq adds the outputs of query head x, every
-// chunk weighted by 2^(its maximum - the largest one), in an order that only
-// the sizes set.  The others (with slot weights) take JOIN_P places of one KV
+// Join: workgroup x < nq adds the partial outputs of query head x, each
+// weighted by 2^(its maximum - the largest one), in an order that only the
+// lengths set.  The others (with slot weights) take JOIN_P places of one KV
 // head each: the sum over its g heads of 2^(score - log-sum) is added to the
 // place's slot, which one thread owns.
 constexpr int JOIN_P = 1024;
 template <typename T>
 __global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
   const int b = blockIdx.y, tid = threadIdx.x, wave = wave_id(), d = a.d;
-  const int n = visible_slots(a.v, b, a.err);
-  const int places = a.blocks ? a.span : min(n, a.span);
-  const int nch = (places + a.chunk - 1) / a.chunk;
+  const Walk w = walk_of(a);                           // every wave for itself
   if ((int)blockIdx.x < a.nq) {
     const int h = blockIdx.x;
     const size_t hi = (size_t)b * a.nq + h;
+    const Parts p = parts_of(a, w, b, h / a.g, h % a.g);
     __shared__ float red[256 * 4];
     float M, l;
-    join_stats(a, hi, nch, M, l);                      // every wave for itself
-    // thread = (4 dims, chunk group)
+    join_stats(a, p, M, l);
+    // thread = (4 dims, group of partials)
     const int q = d / 4, G = 256 / q, x = tid % q, grp = tid / q;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int c = grp; c < nch; c += G)
-      o += *(const f32x4 *)(a.po + (hi * a.nch + c) * d + 4 * x) * exp2f(a.pm[hi * a.nch + c] - M);
+    for (int c = grp; c < p.np; c += G) {
+      const size_t i = p.at + (size_t)c * a.g;
+      o += *(const f32x4 *)(a.po + i * d + 4 * x) * exp2f(a.pm[i] - M);
+    }
     *(f32x4 *)(red + 4 * tid) = o;
     __syncthreads();
     if (grp == 0) {
@@ -544,18 +632,23 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
     if (tid == 0 && a.lse) a.lse[hi] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
     return;
   }
-  const int w = blockIdx.x - a.nq, j = w % a.v.nkv, g = a.g;
-  const int t0 = w / a.v.nkv * JOIN_P;
+  const int y = blockIdx.x - a.nq, j = y % a.v.nkv, g = a.g;
+  const int n = __builtin_amdgcn_readlane(w.n, b), places = places_of(a, n);
+  const int t0 = y / a.v.nkv * JOIN_P;
   if (t0 >= places) return;
   __shared__ float lse[CACHE_MAXG];
   for (int h = wave; h < g; h += 4) {
     float M, l;
-    join_stats(a, (size_t)b * a.nq + j * g + h, nch, M, l);
+    join_stats(a, parts_of(a, w, b, j, h), M, l);
     if ((tid & 63) == 0) lse[h] = l == 0.f ? INFINITY : M + log2f(l);   // nothing seen: every weight 0
   }
   __syncthreads();
-  for (int p = t0 + tid; p < min(places, t0 + JOIN_P); p += 256) {
-    const uint32_t row = place_row(a, b, j, n, p);
+  const Segment sg{b, j, n, 0, 0, min(places, t0 + JOIN_P)};
+  const Lookup lk(a, sg);
+  for (int p = t0 + tid; p < sg.p1; p += 256) {
+    int id, prev;
+    lk.column(p, id, prev);
+    const uint32_t row = lk.row(p, id, prev, lk.block(id));
     if (row == NO_ROW) continue;
     float s = 0.f;
     for (int h = 0; h < g; ++h) s += exp2f(a.scores[((size_t)b * a.nq + j * g + h) * a.ld_scores + p] - lse[h]);
@@ -563,26 +656,31 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
   }
 }
 
-static void join(bool bf16, const CacheAttend &a, hipStream_t s) {
-  const dim3 g(a.nq + (a.weights ? a.v.nkv * ((a.span + JOIN_P - 1) / JOIN_P) : 0), a.v.kv.n_seq);
-  if (bf16) hipLaunchKernelGGL(k_cache_join<bf16_t>, g, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(k_cache_join<float>, g, dim3(256), 0, s, a);
+template <int D>
+static void attend_f32(const CacheAttend &a, hipStream_t s) {
+  const dim3 g(a.waves), t(64);
+  if (a.g == 1) hipLaunchKernelGGL((k_cache_attend<D, 1>), g, t, 0, s, a);
+  else if (a.g == 2) hipLaunchKernelGGL((k_cache_attend<D, 2>), g, t, 0, s, a);
+  else if (a.g <= 4) hipLaunchKernelGGL((k_cache_attend<D, 4>), g, t, 0, s, a);
+  else if constexpr (D < 256) hipLaunchKernelGGL((k_cache_attend<D, 8>), g, t, 0, s, a);   // g * d <= 1024
 }
 void launch_cache_attend(bool bf16, const CacheAttend &a, hipStream_t s) {
-  const dim3 g(a.v.nkv, a.v.kv.n_seq, a.nch), t(64);
+  const dim3 g(a.waves), t(64);
   if (bf16) {
     if (a.d == 32) hipLaunchKernelGGL((k_cache_attend_mfma<32>), g, t, 0, s, a);
     else if (a.d == 64) hipLaunchKernelGGL((k_cache_attend_mfma<64>), g, t, 0, s, a);
     else if (a.d == 128) hipLaunchKernelGGL((k_cache_attend_mfma<128>), g, t, 0, s, a);
     else hipLaunchKernelGGL((k_cache_attend_mfma<256>), g, t, 0, s, a);
-    if (a.nch > 1 || a.weights) join(true, a, s);
-    return;
+  } else {
+    if (a.d == 32) attend_f32<32>(a, s);
+    else if (a.d == 64) attend_f32<64>(a, s);
+    else if (a.d == 128) attend_f32<128>(a, s);
+    else attend_f32<256>(a, s);
   }
-  if (a.d == 32) hipLaunchKernelGGL((k_cache_attend<32>), g, t, 0, s, a);
-  else if (a.d == 64) hipLaunchKernelGGL((k_cache_attend<64>), g, t, 0, s, a);
-  else if (a.d == 128) hipLaunchKernelGGL((k_cache_attend<128>), g, t, 0, s, a);
-  else hipLaunchKernelGGL((k_cache_attend<256>), g, t, 0, s, a);
-  join(false, a, s);
+  if (a.direct) return;
+  const dim3 gj(a.nq + (a.weights ? a.v.nkv * ((a.span + JOIN_P - 1) / JOIN_P) : 0), a.v.kv.n_seq);
+  if (bf16) hipLaunchKernelGGL(k_cache_join<bf16_t>, gj, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_cache_join<float>, gj, dim3(256), 0, s, a);
 }
 
 // ---------------------------------------------------------------- summaries

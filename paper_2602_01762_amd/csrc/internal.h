@@ -387,9 +387,9 @@ struct CacheAttend {
   const int32_t *blocks; int n_list;    // [B, nkv, n_list] or NULL
   int span;                             // places per sequence: max_len, or all of a list's first
                                         // mbps entries
-  int chunk, nch;                       // places per workgroup, workgroups per (sequence, KV head)
+  int waves, direct;                    // cache_plan
   float scale;                          // log2(e) / sqrt(d)
-  float *pm, *pl, *po;                  // partials [B, nq, nch] / [.., d]
+  float *pm, *pl, *po;                  // partials [waves + B * nkv][g] / [.., d]
   float *scores; int ld_scores;         // [B, nq, ld_scores] in base 2 (weights only)
   void *out; float *lse;                // [B, nq, d] / [B, nq] or NULL
   float *weights;                       // slot weights, or NULL

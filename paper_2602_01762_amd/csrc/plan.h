@@ -356,23 +356,22 @@ inline long attention_partial_rows(int rows_max, int grp, int grp2, int nkv, int
   return most;
 }
 
-// Attention over the long-context cache: places per workgroup (one wave) and
-// workgroups per (sequence, KV head), for `units` pairs of a sequence and a KV
-// head of up to `span` places.
-constexpr int CACHE_TILE = 64;          // a chunk is a multiple of this
-constexpr int CACHE_WAVES = 4096;       // waves aimed at: two rounds of 8 per CU
-constexpr int CACHE_MAX_CHUNK = 1024;   // bounds the tail of a ragged batch
+// Attention over the long-context cache, for `units` pairs of a sequence and
+// a KV head of up to `span` places: the waves that share the granules of
+// CACHE_GRAN places.
+constexpr int CACHE_GRAN = 64;      // whole tiles of every attention kernel
+constexpr int CACHE_WAVES = 2048;   // 8 waves on each of 256 CUs, the most that are resident: each
+                                    // pays its first lookups once.  32 sequences of 32768 slots:
+                                    // 670 us, with 4096 waves 691, with 8192 724
 struct CachePlan {
-  int chunk, nch;
+  int waves;
+  bool direct;                      // a granule holds a whole segment, so no join is needed
 };
-// row length of the scores kept for the slot weights: whole tiles
-inline int cache_score_row(int span) { return (span + CACHE_TILE - 1) / CACHE_TILE * CACHE_TILE; }
-inline CachePlan cache_plan(int units, int span) {
-  const long want = units >= CACHE_WAVES ? 1 : CACHE_WAVES / units;
-  long chunk = (span + want - 1) / want;
-  chunk = (chunk + CACHE_TILE - 1) / CACHE_TILE * CACHE_TILE;
-  if (chunk > CACHE_MAX_CHUNK) chunk = CACHE_MAX_CHUNK;
-  return {(int)chunk, (int)((span + chunk - 1) / chunk)};
+inline CachePlan cache_plan(int units, int span, bool weights) {
+  const long granules = (long)units * ((span + CACHE_GRAN - 1) / CACHE_GRAN);
+  return {(int)(granules < CACHE_WAVES ? granules : CACHE_WAVES), span <= CACHE_GRAN && !weights};
 }
+// row length of the scores kept for the slot weights: whole granules
+inline int cache_score_row(int span) { return (span + CACHE_GRAN - 1) / CACHE_GRAN * CACHE_GRAN; }
 
 }  // namespace prism

@@ -1505,11 +1505,11 @@ static size_t cache_scratch(const prism_ctx *c, int call, int B, int span) {
   if (call == PRISM_CACHE_SELECT)
     return (size_t)B * c->nkv * ((span + c->cfg.kv_block_size - 1) / c->cfg.kv_block_size) * 4;
   if (call == PRISM_CACHE_EVICT) return (size_t)B * c->nkv * span * 4;
-  const CachePlan p = cache_plan(B * c->nkv, span);
-  const size_t parts = (size_t)B * c->nq * p.nch;
+  const bool weights = call == PRISM_CACHE_ATTEND_WEIGHTS;
+  const CachePlan p = cache_plan(B * c->nkv, span, weights);
+  const size_t parts = (size_t)(p.waves + B * c->nkv) * (c->nq / c->nkv);
   size_t n = ((parts * 4 + pad) & ~pad) * 2 + ((parts * c->d * 4 + pad) & ~pad);
-  if (call == PRISM_CACHE_ATTEND_WEIGHTS)
-    n += (size_t)B * c->nq * cache_score_row(span) * 4;
+  if (weights) n += (size_t)B * c->nq * cache_score_row(span) * 4;
   return n;
 }
 static prism_status check_scratch(prism_ctx *c, const void *p, uint64_t bytes, size_t need) {
@@ -1591,7 +1591,7 @@ prism_status prism_cache_attend(prism_ctx *c, const prism_cache_attention *io, v
   const int span = io->d_blocks ? std::min(io->n_blocks, c->cfg.max_blocks_per_seq) * c->cfg.kv_block_size : len;
   CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes,
                       cache_scratch(c, io->d_weights ? PRISM_CACHE_ATTEND_WEIGHTS : PRISM_CACHE_ATTEND, B, span)));
-  const CachePlan p = cache_plan(B * c->nkv, span);
+  const CachePlan p = cache_plan(B * c->nkv, span, io->d_weights != nullptr);
   CacheAttend a{};
   a.v = cache_view(c, io->kv, io->n_new, len);
   a.nq = c->nq;
@@ -1601,10 +1601,10 @@ prism_status prism_cache_attend(prism_ctx *c, const prism_cache_attention *io, v
   a.blocks = io->d_blocks;
   a.n_list = io->n_blocks;
   a.span = span;
-  a.chunk = p.chunk;
-  a.nch = p.nch;
+  a.waves = p.waves;
+  a.direct = p.direct;
   a.scale = 1.4426950408889634f / sqrtf((float)c->d);
-  const size_t parts = (size_t)B * c->nq * p.nch;
+  const size_t parts = (size_t)(p.waves + B * c->nkv) * a.g;
   char *ws = (char *)io->d_scratch;
   carve(ws, (void **)&a.pm, parts * 4);
   carve(ws, (void **)&a.pl, parts * 4);

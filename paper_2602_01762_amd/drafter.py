@@ -53,6 +53,7 @@ class Drafter:
         self.cfg = cfg
         self.ctx = B.prism_create(cfg)
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._cache_setup()
 
     def close(self):
         if self.ctx:
@@ -244,10 +245,26 @@ class Drafter:
         return out
 
     # long-context draft cache ---------------------------------------------------
-    def _expect(self, t, name: str, shape, dtype, optional=False):
-        """A contiguous tensor of this shape and type on the context's device."""
-        if t is None and optional:
-            return
+    # These calls take a few microseconds on the GPU when they are small, so the
+    # path to them is kept short: the sizes that the checks compare with are
+    # read from the config once, and one struct per call is filled again and
+    # again (a context is used by one host thread at a time).
+    def _cache_setup(self):
+        c = self.cfg
+        self._dt = torch.bfloat16 if c.dtype == B.PRISM_BF16 else torch.float32
+        self._nq, self._nkv, self._d = c.n_q_heads, c.n_kv_heads, c.head_dim
+        self._bs, self._columns = c.kv_block_size, c.max_blocks_per_seq
+        self._qkv = (self._nq + 2 * self._nkv) * self._d
+        self._io = (B.prism_cache_rows(), B.prism_cache_attention(), B.prism_cache_selection(),
+                    B.prism_cache_eviction())
+        self._scratch_bytes = {}
+
+    def _expect(self, t, name: str, shape, dtype) -> int:
+        """Data pointer of a contiguous tensor of this shape and type on the
+        context's device."""
+        if (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape
+                and t.device == self.device and t.is_contiguous()):
+            return t.data_ptr()
         if not isinstance(t, torch.Tensor):
             raise TypeError("%s must be a tensor" % name)
         if t.dtype != dtype:
@@ -258,37 +275,33 @@ class Drafter:
             raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
         if not t.is_contiguous():
             raise ValueError("%s must be contiguous" % name)
-
-    def _pool(self, kv):
-        c = self.cfg
-        return int(kv.n_pool_blocks), c.n_kv_heads, c.kv_block_size
-
-    @property
-    def _dtype(self):
-        return torch.bfloat16 if self.cfg.dtype == B.PRISM_BF16 else torch.float32
+        return t.data_ptr()          # a subclass of Tensor
 
     def _scratch(self, call: int, batch: int, max_len: int):
-        n = B.prism_cache_scratch(self.ctx, call, batch, max_len)
-        return torch.empty(n, dtype=torch.uint8, device=self.device)
+        key = (call, batch, max_len)
+        n = self._scratch_bytes.get(key)
+        if n is None:
+            n = B.prism_cache_scratch(self.ctx, call, batch, max_len)
+            if len(self._scratch_bytes) >= 1024:      # callers that pass a new bound at every step
+                self._scratch_bytes.clear()
+            self._scratch_bytes[key] = n
+        return n, torch.empty(n, dtype=torch.uint8, device=self.device)
 
     def cache(self, lens, k_pool, v_pool, block_table) -> B.prism_batch:
         """The sequences of a cache call: lens [B] int32 slots held, pools
         [blocks, n_kv_heads, kv_block_size, head_dim], block_table
         [B, max_blocks_per_seq] int32.  Keeps the tensors alive."""
-        c = self.cfg
-        nb = int(lens.shape[0])
-        self._expect(lens, "lens", (nb,), torch.int32)
-        for name, t in (("k_pool", k_pool), ("v_pool", v_pool)):
-            self._expect(t, name, (k_pool.shape[0], c.n_kv_heads, c.kv_block_size, c.head_dim), self._dtype)
-        self._expect(block_table, "block_table", (nb, c.max_blocks_per_seq), torch.int32)
+        nb, n = int(lens.shape[0]), int(k_pool.shape[0])
+        pool = (n, self._nkv, self._bs, self._d)
         kv = B.prism_batch()
         kv.batch = nb
-        kv.d_ctx_lens = B.ptr(lens)
-        kv.d_k_pool = B.ptr(k_pool)
-        kv.d_v_pool = B.ptr(v_pool)
-        kv.d_block_table = B.ptr(block_table)
-        kv.n_pool_blocks = int(k_pool.shape[0])
+        kv.d_ctx_lens = self._expect(lens, "lens", (nb,), torch.int32)
+        kv.d_k_pool = self._expect(k_pool, "k_pool", pool, self._dt)
+        kv.d_v_pool = self._expect(v_pool, "v_pool", pool, self._dt)
+        kv.d_block_table = self._expect(block_table, "block_table", (nb, self._columns), torch.int32)
+        kv.n_pool_blocks = n
         kv.tensors = (lens, k_pool, v_pool, block_table)
+        kv.nb, kv.slots, kv.summary = nb, pool[:3], (n, self._nkv, 2, self._d)
         return kv
 
     def cache_append(self, kv, qkv, q_gain=None, k_gain=None, offsets=None, positions=None,
@@ -296,28 +309,25 @@ class Drafter:
         """Normalise, rotate and append rows: qkv [T, (n_q + 2 n_kv) * d] of
         the sequences in order (rows offsets[b] .. offsets[b+1] - 1; None: one
         row each) at positions[b] (None: lens[b]) and the slots behind each
-        context.  Returns the queries [T, n_q, d]."""
-        c, dt = self.cfg, self._dtype
-        T = int(qkv.shape[0])
-        self._expect(qkv, "qkv", (T, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim), dt)
-        for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
-            self._expect(t, name, (c.head_dim,), dt, optional=True)
-        self._expect(offsets, "offsets", (kv.batch + 1,), torch.int32, optional=True)
-        self._expect(positions, "positions", (kv.batch,), torch.int32, optional=True)
-        self._expect(weights, "weights", self._pool(kv), torch.float32, optional=True)
-        if out is None:
-            out = torch.empty((T, c.n_q_heads, c.head_dim), dtype=dt, device=self.device)
-        self._expect(out, "out", (T, c.n_q_heads, c.head_dim), dt)
-        io = B.prism_cache_rows()
-        io.kv = ctypes.pointer(kv)
+        context; weights (slot weights) are set to 0 there.  Returns the
+        queries [T, n_q, d]."""
+        dt, T = self._dt, qkv.shape[0]
+        io = self._io[0]
+        io.kv = ctypes.addressof(kv)
         io.rows = T
-        io.d_offsets = B.ptr(offsets)
-        io.d_positions = B.ptr(positions)
-        io.d_qkv = B.ptr(qkv)
-        io.d_q_gain = B.ptr(q_gain)
-        io.d_k_gain = B.ptr(k_gain)
-        io.d_q = B.ptr(out)
-        io.d_weights = B.ptr(weights)
+        io.d_qkv = self._expect(qkv, "qkv", (T, self._qkv), dt)
+        io.d_q_gain = None if q_gain is None else self._expect(q_gain, "q_gain", (self._d,), dt)
+        io.d_k_gain = None if k_gain is None else self._expect(k_gain, "k_gain", (self._d,), dt)
+        io.d_offsets = (None if offsets is None
+                        else self._expect(offsets, "offsets", (kv.nb + 1,), torch.int32))
+        io.d_positions = (None if positions is None
+                          else self._expect(positions, "positions", (kv.nb,), torch.int32))
+        io.d_weights = (None if weights is None
+                        else self._expect(weights, "weights", kv.slots, torch.float32))
+        shape = (T, self._nq, self._d)
+        if out is None:
+            out = torch.empty(shape, dtype=dt, device=self.device)
+        io.d_q = self._expect(out, "out", shape, dt)
         B.prism_cache_append(self.ctx, io)
         return out
 
@@ -326,50 +336,44 @@ class Drafter:
         """Attention of one query row per sequence, q [B, n_q, d], over its
         cache or over blocks [B, n_kv, n] of it; adds what every slot receives
         to weights.  Returns out [B, n_q, d] and, if asked for, lse [B, n_q]."""
-        c, dt, nb = self.cfg, self._dtype, int(kv.batch)
-        self._expect(q, "q", (nb, c.n_q_heads, c.head_dim), dt)
-        span = max_len
-        n_blocks = 0
-        if blocks is not None:
-            n_blocks = int(blocks.shape[-1])
-            self._expect(blocks, "blocks", (nb, c.n_kv_heads, n_blocks), torch.int32)
-            if n_blocks < 1:
-                raise ValueError("blocks has no entry")
-            span = min(n_blocks, c.max_blocks_per_seq) * c.kv_block_size
-        self._expect(weights, "weights", self._pool(kv), torch.float32, optional=True)
-        if out is None:
-            out = torch.empty((nb, c.n_q_heads, c.head_dim), dtype=dt, device=self.device)
-        self._expect(out, "out", (nb, c.n_q_heads, c.head_dim), dt)
-        res = {"out": out,
-               "lse": (torch.empty((nb, c.n_q_heads), dtype=torch.float32, device=self.device)
-                       if lse else None)}
-        call = B.PRISM_CACHE_ATTEND if weights is None else B.PRISM_CACHE_ATTEND_WEIGHTS
-        scratch = self._scratch(call, nb, span)
-        io = B.prism_cache_attention()
-        io.kv = ctypes.pointer(kv)
+        dt, nb = self._dt, kv.nb
+        shape = (nb, self._nq, self._d)
+        io = self._io[1]
+        io.kv = ctypes.addressof(kv)
         io.n_new = n_new
-        io.max_len = max_len
-        io.d_q = B.ptr(q)
-        io.d_blocks = B.ptr(blocks)
-        io.n_blocks = n_blocks
-        io.d_weights = B.ptr(weights)
-        io.d_out = B.ptr(out)
-        io.d_lse = B.ptr(res["lse"])
-        io.d_scratch = B.ptr(scratch)
-        io.scratch_bytes = scratch.numel()
+        io.max_len = span = max_len
+        io.d_q = self._expect(q, "q", shape, dt)
+        if blocks is None:
+            io.d_blocks = None
+        else:
+            io.n_blocks = n = int(blocks.shape[-1])
+            io.d_blocks = self._expect(blocks, "blocks", (nb, self._nkv, n), torch.int32)
+            if n < 1:
+                raise ValueError("blocks has no entry")
+            span = min(n, self._columns) * self._bs
+        call = B.PRISM_CACHE_ATTEND
+        io.d_weights = None
+        if weights is not None:
+            io.d_weights = self._expect(weights, "weights", kv.slots, torch.float32)
+            call = B.PRISM_CACHE_ATTEND_WEIGHTS
+        if out is None:
+            out = torch.empty(shape, dtype=dt, device=self.device)
+        io.d_out = self._expect(out, "out", shape, dt)
+        sums = torch.empty(shape[:2], dtype=torch.float32, device=self.device) if lse else None
+        io.d_lse = None if sums is None else sums.data_ptr()
+        io.scratch_bytes, scratch = self._scratch(call, nb, span)
+        io.d_scratch = scratch.data_ptr()
         B.prism_cache_attend(self.ctx, io)
-        return res
+        return {"out": out, "lse": sums}
 
     def summary_buffer(self, kv):
         """A summary pool [blocks, n_kv, 2, d] for cache_summarize."""
-        n, h, _ = self._pool(kv)
-        return torch.zeros((n, h, 2, self.cfg.head_dim), dtype=self._dtype, device=self.device)
+        return torch.zeros(kv.summary, dtype=self._dt, device=self.device)
 
     def cache_summarize(self, kv, summary, n_new: int = 0, span: int = 0):
         """Write the key minima and maxima of the blocks that hold the last
         span slots (0: of every block) into summary [blocks, n_kv, 2, d]."""
-        n, h, _ = self._pool(kv)
-        self._expect(summary, "summary", (n, h, 2, self.cfg.head_dim), self._dtype)
+        self._expect(summary, "summary", kv.summary, self._dt)
         B.prism_cache_summarize(self.ctx, kv, n_new, span, summary)
         return summary
 
@@ -377,26 +381,22 @@ class Drafter:
                      n_new: int = 0, max_len: int = 0, out=None):
         """The n_blocks blocks of largest score bound for each sequence and KV
         head, [B, n_kv, n_blocks] int32: increasing, then -1."""
-        c, nb = self.cfg, int(kv.batch)
-        n, h, _ = self._pool(kv)
-        self._expect(q, "q", (nb, c.n_q_heads, c.head_dim), self._dtype)
-        self._expect(summary, "summary", (n, h, 2, c.head_dim), self._dtype)
-        if out is None:
-            out = torch.empty((nb, h, max(n_blocks, 0)), dtype=torch.int32, device=self.device)
-        self._expect(out, "out", (nb, h, n_blocks), torch.int32)
-        scratch = self._scratch(B.PRISM_CACHE_SELECT, nb, max_len)
-        io = B.prism_cache_selection()
-        io.kv = ctypes.pointer(kv)
+        nb = kv.nb
+        io = self._io[2]
+        io.kv = ctypes.addressof(kv)
         io.n_new = n_new
         io.max_len = max_len
-        io.d_q = B.ptr(q)
-        io.d_summary = B.ptr(summary)
+        io.d_q = self._expect(q, "q", (nb, self._nq, self._d), self._dt)
+        io.d_summary = self._expect(summary, "summary", kv.summary, self._dt)
         io.n_blocks = n_blocks
         io.n_first = n_first
         io.n_last = n_last
-        io.d_blocks = B.ptr(out)
-        io.d_scratch = B.ptr(scratch)
-        io.scratch_bytes = scratch.numel()
+        shape = (nb, self._nkv, max(n_blocks, 0))
+        if out is None:
+            out = torch.empty(shape, dtype=torch.int32, device=self.device)
+        io.d_blocks = self._expect(out, "out", shape, torch.int32)
+        io.scratch_bytes, scratch = self._scratch(B.PRISM_CACHE_SELECT, nb, max_len)
+        io.d_scratch = scratch.data_ptr()
         B.prism_cache_select(self.ctx, io)
         return out
 
@@ -405,26 +405,23 @@ class Drafter:
         """Copy the n_keep slots of largest weight to the blocks of new_table
         [B, max_blocks_per_seq].  Returns kept [B, n_kv, n_keep] (old slots)
         and lens [B], the lengths of the new cache."""
-        c, nb = self.cfg, int(kv.batch)
-        self._expect(new_table, "new_table", (nb, c.max_blocks_per_seq), torch.int32)
-        self._expect(weights, "weights", self._pool(kv), torch.float32)
-        i32 = dict(dtype=torch.int32, device=self.device)
-        res = {"kept": torch.empty((nb, c.n_kv_heads, max(n_keep, 0)), **i32), "lens": torch.empty(nb, **i32)}
-        scratch = self._scratch(B.PRISM_CACHE_EVICT, nb, max_len)
-        io = B.prism_cache_eviction()
-        io.kv = ctypes.pointer(kv)
+        nb = kv.nb
+        io = self._io[3]
+        io.kv = ctypes.addressof(kv)
         io.max_len = max_len
-        io.d_new_table = B.ptr(new_table)
-        io.d_weights = B.ptr(weights)
+        io.d_new_table = self._expect(new_table, "new_table", (nb, self._columns), torch.int32)
+        io.d_weights = self._expect(weights, "weights", kv.slots, torch.float32)
         io.n_keep = n_keep
         io.n_first = n_first
         io.n_recent = n_recent
-        io.d_kept = B.ptr(res["kept"])
-        io.d_new_lens = B.ptr(res["lens"])
-        io.d_scratch = B.ptr(scratch)
-        io.scratch_bytes = scratch.numel()
+        kept = torch.empty((nb, self._nkv, max(n_keep, 0)), dtype=torch.int32, device=self.device)
+        lens = torch.empty(nb, dtype=torch.int32, device=self.device)
+        io.d_kept = kept.data_ptr()
+        io.d_new_lens = lens.data_ptr()
+        io.scratch_bytes, scratch = self._scratch(B.PRISM_CACHE_EVICT, nb, max_len)
+        io.d_scratch = scratch.data_ptr()
         B.prism_cache_evict(self.ctx, io)
-        return res
+        return {"kept": kept, "lens": lens}
 
     def device_status(self) -> int:
         return B.prism_device_status(self.ctx)

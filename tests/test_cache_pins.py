@@ -67,6 +67,7 @@ def _fake():
     dr.device = torch.device("cpu")
     dr.cfg = B.prism_config(n_q_heads=4, n_kv_heads=2, head_dim=32, kv_block_size=16,
                             max_blocks_per_seq=5, max_batch=3, dtype=B.PRISM_BF16)
+    dr._cache_setup()
     return dr
 
 
@@ -155,28 +156,67 @@ def test_null_context_is_refused():
     assert L.prism_cache_evict(None, None, None) == -1
 
 
-def test_attention_plan_covers_every_place(tmp_path):
-    """Chunks are multiples of the tile, cover the span and no more than it."""
+def test_attention_runs_cover_every_granule(tmp_path):
+    """The runs that a plan's waves take over random lengths: every granule of
+    every (sequence, KV head) once, each (wave, segment) its own partial below
+    waves + segments, and a segment's partials next to each other, where the
+    join looks for them."""
     src, exe = tmp_path / "plan.cc", tmp_path / "plan"
-    src.write_text("""
+    src.write_text(r"""
 #include <cstdio>
+#include <cstdlib>
+#include <vector>
 #include "plan.h"
 using namespace prism;
 int main() {
-  const int units[] = {1, 2, 7, 8, 32, 128, 255, 256, 1000, 4096, 4097, 64 * 64};
-  for (int u : units)
-    for (long span = 1; span <= (1 << 20); span = span < 300 ? span + 1 : span * 5 / 4 + 1) {
-      const CachePlan p = cache_plan(u, (int)span);
-      if (p.chunk < CACHE_TILE || p.chunk % CACHE_TILE || p.chunk > CACHE_MAX_CHUNK || p.nch < 1 ||
-          (long)p.nch * p.chunk < span || (long)(p.nch - 1) * p.chunk >= span) {
-        printf("%d %ld: %d x %d\\n", u, span, p.nch, p.chunk);
-        return 1;
+  srand(1);
+  for (int it = 0; it < 4000; ++it) {
+    const int B = 1 + rand() % 64, nkv = 1 + rand() % 8, top = 1 << (rand() % 18);
+    std::vector<int> len(B);
+    int span = 1;
+    for (int &n : len) { n = rand() % 3 ? rand() % (top + 1) : 0; span = n > span ? n : span; }
+    const bool weights = rand() % 2;
+    const CachePlan p = cache_plan(B * nkv, span, weights);
+    if (p.waves < 1 || p.waves > CACHE_WAVES) return 1;
+    if (p.direct && (span > CACHE_GRAN || weights)) return 2;
+    std::vector<long> begin(B), count(B);
+    long total = 0;
+    for (int b = 0; b < B; ++b) {
+      count[b] = p.direct ? 1 : (len[b] + CACHE_GRAN - 1) / CACHE_GRAN;
+      begin[b] = total;
+      total += count[b] * nkv;
+    }
+    long per = (total + p.waves - 1) / p.waves;
+    if (per < 1) per = 1;
+    std::vector<int> owner(p.waves + (long)B * nkv, -1), seen(total, 0);
+    for (long w = 0; w < p.waves; ++w) {
+      long u = w * per, last = u + per < total ? u + per : total;
+      while (u < last) {
+        int b = 0;
+        while (begin[b] + count[b] * nkv <= u) ++b;
+        const long j = (u - begin[b]) / count[b], first = u - begin[b] - j * count[b];
+        long m = count[b] - first;
+        if (m > last - u) m = last - u;
+        for (long i = 0; i < m; ++i) ++seen[u + i];
+        const long part = w + (long)b * nkv + j, g0 = begin[b] + j * count[b];
+        if (part >= (long)owner.size() || owner[part] != -1) return 3;
+        owner[part] = b * nkv + (int)j;
+        const long w0 = g0 / per, w1 = (g0 + count[b] - 1) / per;   // the join's range
+        if (w < w0 || w > w1) return 4;
+        u += m;
       }
     }
+    for (int s : seen) if (s != 1) return 5;
+    for (int b = 0; b < B; ++b)
+      for (int j = 0; j < nkv && count[b]; ++j) {
+        const long g0 = begin[b] + j * count[b];
+        for (long w = g0 / per; w <= (g0 + count[b] - 1) / per; ++w)
+          if (owner[w + (long)b * nkv + j] != b * nkv + j) return 6;
+      }
+  }
   return 0;
 }
 """)
-    subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "paper_2602_01762_amd", "csrc"), str(src),
+    subprocess.run(["g++", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2602_01762_amd", "csrc"), str(src),
                     "-o", str(exe)], check=True)
-    r = subprocess.run([str(exe)], capture_output=True, text=True)
-    assert r.returncode == 0, r.stdout
+    assert subprocess.run([str(exe)]).returncode == 0

@@ -756,7 +756,7 @@ def test_refusals():
         assert e.value.status == -1 and str(e.value), i
     io = B.prism_cache_attention()
     import ctypes
-    io.kv = ctypes.pointer(kv)
+    io.kv = ctypes.addressof(kv)
     out, scratch = torch.empty_like(q), torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
     io.d_q, io.d_out, io.d_scratch, io.scratch_bytes = B.ptr(q), B.ptr(out), B.ptr(scratch), 1 << 20
     for field, value in (("scratch_bytes", 16), ("d_scratch", 0), ("d_q", 0), ("d_q", B.ptr(q) + 2),
