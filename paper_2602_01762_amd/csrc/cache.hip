@@ -783,22 +783,53 @@ __global__ __launch_bounds__(256) void k_cache_score(CacheSelect a) {
   }
   if (held && li == 0) {
     const bool forced = bi < a.n_first || bi >= nblk - a.n_last;
-    a.keys[((size_t)b * a.v.nkv + j) * a.columns + bi] =
+    a.keys[((size_t)b * a.v.nkv + j) * a.ld_keys + bi] =
         row == NO_ROW ? 0u : forced ? KEY_FORCED : choice_key(best);
   }
 }
 
+// Inclusive sum over the lanes below, in a wave (DPP: within rows of 16
+// lanes, then the last lane of a row to the next row, then of the first half
+// to the second).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);    // row_shr:1
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);    // row_shr:2
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);    // row_shr:4
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);    // row_shr:8
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);   // row_bcast:31
+  return v;
+}
+// sum of v[0 .. w - 1] (LDS, at most 64 entries), w wave-uniform
+__device__ __forceinline__ uint32_t sum_before(const uint32_t *v, int entries, int w) {
+  const int lane = threadIdx.x & 63;
+  return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(lane < entries && lane < w ? v[lane] : 0u), 63);
+}
+
 // The n_take candidates of largest key of one (sequence, KV head), ties to
-// the lowest index, in index order, then -1.  Radix descent over digits of 11,
-// 11 and 10 bits with an LDS histogram finds the key of the last one taken;
-// each wave then owns a run of candidates, so a prefix over the waves gives
-// every taken one its place.
+// the lowest index, in index order, then -1.  A radix descent over digits of
+// 11, 11 and 10 bits with an LDS histogram finds the key of the last one taken,
+// and ends where a whole digit is taken; the candidates left after the first
+// digit are listed in LDS if at most CHOOSE_LIST are.  Each wave then owns a run
+// of candidates, so a prefix over the waves gives every taken one its place.
+// Candidates are padded with keys of 0 to groups of 256: behind all others,
+// and never reached, since fewer are taken than there are.
+//   LDS: the keys fit CHOOSE_LDS and are read once; else every pass streams
+// them (from the L2 after the first), and the first histogram of slots is the
+// sum of those that k_cache_keys left per CHOOSE_SEG of them.  WEIGHTS (with LDS):
+// the keys are made here from the slot weights.
+//   One workgroup's instructions bound it: 512 cycles per instruction of a
+// pass over 131072 keys.  8192 blocks 10 us (13 with a loop per digit over all
+// keys and sums over the waves in loops).
 constexpr int CHOOSE_T = 1024, CHOOSE_W = CHOOSE_T / 64;
+constexpr int CHOOSE_LIST = 8192;
+template <bool WEIGHTS, bool LDS>
 __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
   const int j = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
-  __shared__ uint32_t hist[2048];
+  extern __shared__ __attribute__((aligned(16))) uint32_t s_keys[];
+  __shared__ uint32_t hist[2][2048], list[CHOOSE_LIST];
   __shared__ uint32_t wsum[CHOOSE_W], wgt[CHOOSE_W], weq[CHOOSE_W];
-  __shared__ uint32_t s_digit, s_above;
+  __shared__ uint32_t s_digit, s_above, s_count, s_listed;
   const int n_vis = visible_slots(a.v, b, a.err);
   const int bs = a.per_block ? a.v.kv.bs : 1;
   const int n = (int)(((long)n_vis + bs - 1) / bs);
@@ -810,73 +841,245 @@ __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
     for (int i = tid; i < a.n_take; i += CHOOSE_T) out[i] = i < n ? i : -1;
     return;
   }
-  uint32_t prefix = 0, mask = 0, need = a.n_take;
-  const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
-  for (int p = 0; p < 3; ++p) {
-    for (int i = tid; i < 2048; i += CHOOSE_T) hist[i] = 0;
-    __syncthreads();
-    const uint32_t dm = (1u << bits[p]) - 1;
-    for (int i = tid; i < n; i += CHOOSE_T) {
-      const uint32_t k = keys[i];
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shifts[p]) & dm], 1u);
-    }
-    __syncthreads();
-    // thread t owns digits 2t, 2t + 1; counts of the digits above it
-    const uint32_t h0 = hist[2 * tid], h1 = hist[2 * tid + 1];
-    uint32_t suf = h0 + h1;                         // inclusive suffix sum over the wave
+  // a run of groups of 256 candidates per wave; lane l holds candidates
+  // 4 l .. 4 l + 3 of a group
+  const int groups = (n + 255) / 256, per = (groups + CHOOSE_W - 1) / CHOOSE_W;
+  const int g0 = wave * per, g1 = min(groups, g0 + per);
+  for (int i = tid; i < 4096; i += CHOOSE_T) (&hist[0][0])[i] = 0;
+  if (tid == 0) s_listed = 0;
+  if constexpr (LDS) {
+    constexpr int U = 4;                            // loads in flight per thread
+    for (int i0 = 0; i0 < 256 * groups; i0 += U * CHOOSE_T) {
+      uint32_t k[U];
+      if constexpr (WEIGHTS) {
+        uint32_t row[U];
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) {
-      const uint32_t v = __shfl_down(suf, x, 64);
-      if (lane + x < 64) suf += v;
+        for (int x = 0; x < U; ++x) {
+          const int i = i0 + x * CHOOSE_T + tid, bi = slot_block(a.v.kv, i);
+          row[x] = i < n ? pool_row(a.v, a.v.kv.block_table, b, j, bi, slot_in_block(a.v.kv, i, bi), a.err) : NO_ROW;
+        }
+        float w[U];
+#pragma unroll
+        for (int x = 0; x < U; ++x) w[x] = a.weights[row[x] == NO_ROW ? 0 : row[x]];
+#pragma unroll
+        for (int x = 0; x < U; ++x) {
+          const int i = i0 + x * CHOOSE_T + tid;
+          k[x] = row[x] == NO_ROW ? 0u : i < a.n_first || i >= n - a.n_last ? KEY_FORCED : choice_key(w[x]);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < U; ++x) {
+          const int i = i0 + x * CHOOSE_T + tid;
+          k[x] = i < n ? keys[i] : 0u;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < U; ++x) {
+        const int i = i0 + x * CHOOSE_T + tid;
+        if (i < 256 * groups) s_keys[i] = k[x];
+      }
     }
-    if (lane == 0) wsum[wave] = suf;
+  }
+  __syncthreads();
+  auto load4 = [&](int gr) -> u32x4 {
+    const int i = gr * 256 + 4 * lane;
+    if constexpr (LDS) {
+      return *(const u32x4 *)(s_keys + i);
+    } else {
+      if (gr * 256 + 256 <= n) return *(const u32x4 *)(keys + i);
+      u32x4 k;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = i + e < n ? keys[i + e] : 0u;
+      return k;
+    }
+  };
+  constexpr int UG = LDS ? 2 : 8;                   // groups in flight per wave
+  uint32_t prefix = 0, mask = 0, need = a.n_take;
+  bool listed = false;
+#pragma unroll 1
+  for (int p = 0; p < 3; ++p) {
+    const int shift = p == 0 ? 21 : p == 1 ? 10 : 0;
+    const uint32_t dm = p == 2 ? 1023u : 2047u;
+    uint32_t *hg = hist[p & 1];
+    // one key's digit; many lanes with one digit (equal keys: unweighted
+    // slots) would queue for its counter: one addition for all of them
+    auto add = [&](uint32_t k, bool in) {
+      const uint32_t dg = (k >> shift) & dm, d0 = __builtin_amdgcn_readfirstlane(dg);
+      const uint64_t same = __ballot(in && dg == d0);
+      if (__popcll(same) >= 16) {
+        if (lane == __builtin_ctzll(same)) atomicAdd(&hg[d0], (uint32_t)__popcll(same));
+        in &= dg != d0;
+      }
+      if (in) atomicAdd(&hg[dg], 1u);
+    };
+    if (listed) {
+      for (int i = tid; i < (int)s_listed; i += CHOOSE_T) add(list[i], (list[i] & mask) == prefix);
+    } else if (!LDS && p == 0 && a.hists) {                    // 2 digits per thread
+      const int segs = (n + CHOOSE_SEG - 1) / CHOOSE_SEG;
+      const uint32_t *h = a.hists + u * a.ld_hists + tid;
+      uint32_t lo = 0, hi = 0;
+#pragma unroll 8
+      for (int sgm = 0; sgm < segs; ++sgm) {
+        const uint32_t v = h[sgm * 1024];
+        lo += v & 0xffffu;
+        hi += v >> 16;
+      }
+      hg[2 * tid] = lo;
+      hg[2 * tid + 1] = hi;
+    } else {
+#pragma unroll 1
+      for (int gr = g0; gr < g1; gr += UG) {
+        u32x4 k[UG];
+#pragma unroll
+        for (int x = 0; x < UG; ++x) k[x] = load4(min(gr + x, g1 - 1));
+#pragma unroll
+        for (int x = 0; x < UG; ++x) {
+          if (gr + x >= g1) break;
+          bool in[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) in[e] = (k[x][e] & mask) == prefix;
+          if (!__ballot(in[0] | in[1] | in[2] | in[3])) continue;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) add(k[x][e], in[e]);
+        }
+      }
+    }
     __syncthreads();
-    uint32_t above = suf - h0 - h1;
-    for (int w = wave + 1; w < CHOOSE_W; ++w) above += wsum[w];
+    // thread t owns the digits 2047 - 2t and 2046 - 2t: a sum over the threads
+    // before it counts the digits above
+    const uint32_t h1 = hg[2047 - 2 * tid], h0 = hg[2046 - 2 * tid];
+    const uint32_t scan = wave_scan(h0 + h1);
+    if (lane == 63) wsum[wave] = scan;
+    if (p == 0) {                                   // (the third pass counts here again)
+      hg[2047 - 2 * tid] = 0;
+      hg[2046 - 2 * tid] = 0;
+    }
+    __syncthreads();
+    const uint32_t above = sum_before(wsum, CHOOSE_W, wave) + scan - h0 - h1;
     if (above < need && above + h1 >= need) {
-      s_digit = 2 * tid + 1;
+      s_digit = 2047 - 2 * tid;
       s_above = above;
+      s_count = h1;
     } else if (above + h1 < need && above + h1 + h0 >= need) {
-      s_digit = 2 * tid;
+      s_digit = 2046 - 2 * tid;
       s_above = above + h1;
+      s_count = h0;
     }
     __syncthreads();
-    prefix |= s_digit << shifts[p];
-    mask |= dm << shifts[p];
+    prefix |= s_digit << shift;
+    mask |= dm << shift;
     need -= s_above;
-    __syncthreads();
+    if (need == s_count) break;                     // the whole digit (uniform)
+    if (p == 0 && s_count <= CHOOSE_LIST) {         // (uniform) in any order: only counted
+      listed = true;
+#pragma unroll 1
+      for (int gr = g0; gr < g1; gr += UG) {
+        u32x4 k[UG];
+#pragma unroll
+        for (int x = 0; x < UG; ++x) k[x] = load4(min(gr + x, g1 - 1));
+#pragma unroll
+        for (int x = 0; x < UG; ++x) {
+          if (gr + x >= g1) break;
+          uint64_t m[4];
+          uint32_t all = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            m[e] = __ballot((k[x][e] & mask) == prefix);
+            all += __popcll(m[e]);
+          }
+          if (!all) continue;
+          uint32_t to = 0;
+          if (lane == 0) to = atomicAdd(&s_listed, all);
+          to = __builtin_amdgcn_readfirstlane(to);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((k[x][e] & mask) == prefix) list[to + __popcll(m[e] & ((1ull << lane) - 1))] = k[x][e];
+            to += __popcll(m[e]);
+          }
+        }
+      }
+      __syncthreads();
+    }
   }
-  // taken: key > prefix, and the first `need` of those equal to it
-  const int per = ((n + CHOOSE_T - 1) / CHOOSE_T) * 64;   // candidates of one wave
-  const int i0 = wave * per, i1 = min(n, i0 + per);
+  // taken: key & mask > prefix, and the first `need` of those equal to it
   uint32_t gt = 0, eq = 0;
-  for (int i = i0; i < i1; i += 64) {
-    const uint32_t k = i + lane < i1 ? keys[i + lane] : 0u;
-    gt += __popcll(__ballot(i + lane < i1 && k > prefix));
-    eq += __popcll(__ballot(i + lane < i1 && k == prefix));
+#pragma unroll 1
+  for (int gr = g0; gr < g1; gr += UG) {
+    u32x4 k[UG];
+#pragma unroll
+    for (int x = 0; x < UG; ++x) k[x] = load4(min(gr + x, g1 - 1));
+#pragma unroll
+    for (int x = 0; x < UG; ++x) {
+      if (gr + x >= g1) break;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        gt += (k[x][e] & mask) > prefix;
+        eq += (k[x][e] & mask) == prefix;
+      }
+    }
   }
-  if (lane == 0) {
+  gt = wave_scan(gt);
+  eq = wave_scan(eq);
+  if (lane == 63) {
     wgt[wave] = gt;
     weq[wave] = eq;
   }
   __syncthreads();
-  uint32_t eq0 = 0, at = 0;
-  for (int w = 0; w < wave; ++w) {
-    eq0 += weq[w];
-    at += wgt[w];
-  }
-  at += min(eq0, need);
+  uint32_t eq0 = sum_before(weq, CHOOSE_W, wave), to = sum_before(wgt, CHOOSE_W, wave) + min(eq0, need);
   const uint64_t below = (1ull << lane) - 1;
-  for (int i = i0; i < i1; i += 64) {
-    const bool in = i + lane < i1;
-    const uint32_t k = in ? keys[i + lane] : 0u;
-    const uint64_t me = __ballot(in && k == prefix);
-    const bool take = in && (k > prefix || (k == prefix && eq0 + __popcll(me & below) < need));
-    const uint64_t mt = __ballot(take);
-    if (take) out[at + __popcll(mt & below)] = i + lane;
-    at += __popcll(mt);
-    eq0 += __popcll(me);
+#pragma unroll 1
+  for (int gr = g0; gr < g1; gr += UG) {
+    u32x4 k[UG];
+#pragma unroll
+    for (int x = 0; x < UG; ++x) k[x] = load4(min(gr + x, g1 - 1)) & mask;
+#pragma unroll
+    for (int x = 0; x < UG; ++x) {
+      if (gr + x >= g1) break;
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any |= k[x][e] >= prefix;
+      if (!__ballot(any)) continue;
+      bool take[4], some_eq = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        take[e] = k[x][e] > prefix;
+        some_eq |= k[x][e] == prefix;
+      }
+      if (__ballot(some_eq)) {
+        uint32_t ahead = eq0;                       // equal ones before this lane's next candidate
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint64_t m = __ballot(k[x][e] == prefix);
+          ahead += __popcll(m & below);
+          eq0 += __popcll(m);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          take[e] |= k[x][e] == prefix && ahead < need;
+          ahead += k[x][e] == prefix;
+        }
+      }
+      uint32_t pos = to;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint64_t t = __ballot(take[e]);
+        pos += __popcll(t & below);
+        to += __popcll(t);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (take[e]) out[pos++] = gr * 256 + x * 256 + 4 * lane + e;
+    }
   }
+}
+// at most CHOOSE_LDS candidates have their keys in LDS (96 KB beside the 48
+// of histograms and list; a workgroup may take 160)
+static void choose(const CacheChoose &a, int most, hipStream_t s) {
+  const dim3 g(a.v.nkv, a.v.kv.n_seq), t(CHOOSE_T);
+  const size_t lds = (size_t)((most + 255) / 256) * 1024;
+  if (most > CHOOSE_LDS) hipLaunchKernelGGL((k_cache_choose<false, false>), g, t, 0, s, a);
+  else if (a.weights) hipLaunchKernelGGL((k_cache_choose<true, true>), g, t, lds, s, a);
+  else hipLaunchKernelGGL((k_cache_choose<false, true>), g, t, lds, s, a);
 }
 
 template <typename T>
@@ -891,21 +1094,40 @@ static void score_d(const CacheSelect &a, int d, hipStream_t s) {
 void launch_cache_select(bool bf16, const CacheSelect &a, int d, hipStream_t s) {
   if (bf16) score_d<bf16_t>(a, d, s);
   else score_d<float>(a, d, s);
-  CacheChoose c{a.v, a.keys, a.columns, 1, a.n_take, a.out, nullptr, a.err};
-  hipLaunchKernelGGL(k_cache_choose, dim3(a.v.nkv, a.v.kv.n_seq), dim3(CHOOSE_T), 0, s, c);
+  choose({a.v, a.keys, a.ld_keys, nullptr, 0, nullptr, 1, a.n_take, 0, 0, a.out, nullptr, a.err}, a.columns, s);
 }
 
 // ---------------------------------------------------------------- eviction
-// Order keys of the slots of one sequence and KV head.
+// Order keys of the slots of one sequence and KV head (those that do not fit
+// the choice's LDS), and the histogram of their first digits, two to a word.
 __global__ __launch_bounds__(256) void k_cache_keys(CacheEvict a) {
-  const int t = blockIdx.x * 256 + threadIdx.x, j = blockIdx.y, b = blockIdx.z;
+  constexpr int U = CHOOSE_SEG / 256;
+  const int t0 = blockIdx.x * CHOOSE_SEG, j = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  __shared__ uint32_t hist[1024];
   const int n = visible_slots(a.v, b, a.err);
-  if (t >= n) return;
-  const int bi = slot_block(a.v.kv, t);
-  const uint32_t row = pool_row(a.v, a.v.kv.block_table, b, j, bi, slot_in_block(a.v.kv, t, bi), a.err);
-  const bool forced = t < a.n_first || t >= n - a.n_recent;
-  a.keys[((size_t)b * a.v.nkv + j) * a.ld_keys + t] =
-      row == NO_ROW ? 0u : forced ? KEY_FORCED : choice_key(a.weights[row]);
+  if (t0 >= n) return;
+  for (int i = tid; i < 1024; i += 256) hist[i] = 0;
+  __syncthreads();
+  const size_t u = (size_t)b * a.v.nkv + j;
+  uint32_t row[U];
+#pragma unroll
+  for (int x = 0; x < U; ++x) {
+    const int t = t0 + x * 256 + tid, bi = slot_block(a.v.kv, t);
+    row[x] = t < n ? pool_row(a.v, a.v.kv.block_table, b, j, bi, slot_in_block(a.v.kv, t, bi), a.err) : NO_ROW;
+  }
+  float w[U];
+#pragma unroll
+  for (int x = 0; x < U; ++x) w[x] = a.weights[row[x] == NO_ROW ? 0 : row[x]];
+#pragma unroll
+  for (int x = 0; x < U; ++x) {
+    const int t = t0 + x * 256 + tid;
+    if (t >= n) break;
+    const uint32_t k = row[x] == NO_ROW ? 0u : t < a.n_first || t >= n - a.n_recent ? KEY_FORCED : choice_key(w[x]);
+    a.keys[u * a.ld_keys + t] = k;
+    atomicAdd(&hist[k >> 22], (k >> 21) & 1 ? 0x10000u : 1u);   // at most CHOOSE_SEG < 2^16 each
+  }
+  __syncthreads();
+  for (int i = tid; i < 1024; i += 256) a.hists[u * a.ld_hists + blockIdx.x * 1024 + i] = hist[i];
 }
 
 // Keys, values and weight of the kept slots to the new blocks: a lane group
@@ -948,9 +1170,11 @@ static void copy_d(const CacheEvict &a, int d, hipStream_t s) {
   else hipLaunchKernelGGL((k_cache_copy<T, 256>), g, dim3(256), 0, s, a);
 }
 void launch_cache_evict(bool bf16, const CacheEvict &a, int d, hipStream_t s) {
-  hipLaunchKernelGGL(k_cache_keys, dim3((a.v.max_len + 255) / 256, a.v.nkv, a.v.kv.n_seq), dim3(256), 0, s, a);
-  CacheChoose c{a.v, a.keys, a.ld_keys, 0, a.n_keep, a.kept, a.new_lens, a.err};
-  hipLaunchKernelGGL(k_cache_choose, dim3(a.v.nkv, a.v.kv.n_seq), dim3(CHOOSE_T), 0, s, c);
+  if (a.v.max_len > CHOOSE_LDS)
+    hipLaunchKernelGGL(k_cache_keys, dim3((a.v.max_len + CHOOSE_SEG - 1) / CHOOSE_SEG, a.v.nkv, a.v.kv.n_seq),
+                       dim3(256), 0, s, a);
+  choose({a.v, a.keys, a.ld_keys, a.hists, a.ld_hists, a.weights, 0, a.n_keep, a.n_first, a.n_recent, a.kept, a.new_lens, a.err},
+         a.v.max_len, s);
   if (bf16) copy_d<bf16_t>(a, d, s);
   else copy_d<float>(a, d, s);
 }

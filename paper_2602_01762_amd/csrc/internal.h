@@ -408,16 +408,18 @@ struct CacheSelect {
   int nq, g;
   const void *q, *summary;
   int n_take, n_first, n_last, columns; // columns: table columns of max_len slots
-  uint32_t *keys;                       // [B, nkv, columns]
+  uint32_t *keys; int ld_keys;          // [B, nkv, ld_keys]
   int32_t *out;                         // [B, nkv, n_take]
   uint32_t *err;
 };
 void launch_cache_select(bool bf16, const CacheSelect &a, int d, hipStream_t s);
 struct CacheChoose {
   CacheView v;
-  const uint32_t *keys; int ld_keys;    // [B, nkv, ld_keys]
+  const uint32_t *keys; int ld_keys;    // [B, nkv, ld_keys], ld_keys a multiple of 4
+  const uint32_t *hists; int ld_hists;  // first digits per CHOOSE_SEG keys, 1024 words each, or NULL
+  const float *weights;                 // slot weights to make the keys from, or NULL
   int per_block;                        // candidates are blocks (else slots)
-  int n_take;
+  int n_take, n_first, n_last;          // (n_first, n_last: with weights)
   int32_t *out, *lens;                  // [B, nkv, n_take]; [B] counts taken, or NULL
   uint32_t *err;
 };
@@ -425,8 +427,9 @@ struct CacheEvict {
   CacheView v;
   const int32_t *new_table;             // [B, mbps]
   float *weights;
-  int n_keep, n_first, n_recent, ld_keys;
-  uint32_t *keys;                       // [B, nkv, ld_keys]
+  int n_keep, n_first, n_recent;
+  uint32_t *keys; int ld_keys;          // [B, nkv, ld_keys]
+  uint32_t *hists; int ld_hists;        // [B, nkv, ld_hists] (more than CHOOSE_LDS candidates)
   int32_t *kept, *new_lens;             // [B, nkv, n_keep] / [B]
   uint32_t *err;
 };

@@ -374,4 +374,14 @@ inline CachePlan cache_plan(int units, int span, bool weights) {
 // row length of the scores kept for the slot weights: whole granules
 inline int cache_score_row(int span) { return (span + CACHE_GRAN - 1) / CACHE_GRAN * CACHE_GRAN; }
 
+// Choice of the best of many candidates by one workgroup: up to CHOOSE_LDS
+// have their keys in LDS; more go through scratch, in segments of CHOOSE_SEG
+// with a histogram of 1024 words each.
+constexpr int CHOOSE_LDS = 24576, CHOOSE_SEG = 4096;
+inline int choose_key_row(int most) { return (most + 3) / 4 * 4; }
+inline int choose_hist_row(int most) { return most > CHOOSE_LDS ? (most + CHOOSE_SEG - 1) / CHOOSE_SEG * 1024 : 0; }
+inline size_t choose_scratch(size_t units, int most) {
+  return units * ((size_t)choose_key_row(most) + choose_hist_row(most)) * 4;
+}
+
 }  // namespace prism

@@ -1503,8 +1503,8 @@ static prism_status check_len(prism_ctx *c, int32_t n_new, int32_t max_len, int 
 static size_t cache_scratch(const prism_ctx *c, int call, int B, int span) {
   const size_t pad = 255;
   if (call == PRISM_CACHE_SELECT)
-    return (size_t)B * c->nkv * ((span + c->cfg.kv_block_size - 1) / c->cfg.kv_block_size) * 4;
-  if (call == PRISM_CACHE_EVICT) return (size_t)B * c->nkv * span * 4;
+    return (size_t)B * c->nkv * choose_key_row((span + c->cfg.kv_block_size - 1) / c->cfg.kv_block_size) * 4;
+  if (call == PRISM_CACHE_EVICT) return choose_scratch((size_t)B * c->nkv, span);
   const bool weights = call == PRISM_CACHE_ATTEND_WEIGHTS;
   const CachePlan p = cache_plan(B * c->nkv, span, weights);
   const size_t parts = (size_t)(p.waves + B * c->nkv) * (c->nq / c->nkv);
@@ -1667,6 +1667,7 @@ prism_status prism_cache_select(prism_ctx *c, const prism_cache_selection *io, v
   a.n_last = io->n_last;
   a.columns = (len + c->cfg.kv_block_size - 1) / c->cfg.kv_block_size;
   a.keys = (uint32_t *)io->d_scratch;
+  a.ld_keys = choose_key_row(a.columns);
   a.out = io->d_blocks;
   a.err = c->err;
   launch_cache_select(c->bf16, a, c->d, (hipStream_t)stream);
@@ -1700,8 +1701,10 @@ prism_status prism_cache_evict(prism_ctx *c, const prism_cache_eviction *io, voi
   a.n_keep = io->n_keep;
   a.n_first = io->n_first;
   a.n_recent = io->n_recent;
-  a.ld_keys = len;
   a.keys = (uint32_t *)io->d_scratch;
+  a.ld_keys = choose_key_row(len);
+  a.hists = a.keys + (size_t)B * c->nkv * a.ld_keys;
+  a.ld_hists = choose_hist_row(len);
   a.kept = io->d_kept;
   a.new_lens = io->d_new_lens;
   a.err = c->err;

@@ -545,6 +545,15 @@ def test_evict(heads):
     c.close()
 
 
+def test_select_from_more_blocks_than_fit_on_chip():
+    c = Cache(2, 1, 32, "bf16", 1, [30000, 24577, 5], 30000)
+    q = c.normal((3, 2, 32))
+    s = c.dr.cache_summarize(c.kv(), c.dr.summary_buffer(c.kv()))
+    for n, first, last in ((100, 0, 0), (12000, 2, 5)):
+        check_select(c, q, s, c.dr.cache_select(c.kv(), q, s, n, first, last), n, first, last)
+    c.close()
+
+
 @pytest.mark.parametrize("bs", [1, 7, 64])
 def test_evict_block_sizes(bs):
     lens = [0, 1, 130, 301]
@@ -579,6 +588,17 @@ def test_evict_long_sequences():
     c = Cache(2, 1, 32, "bf16", 16, [40000, 33000, 1024], 2500, spare=3 * 700)
     for n in (1, 1025, 11000):
         check_evict(c, c.weights(0.3), n, min(4, n), n // 4 if n > 8 else 0)
+    c.close()
+
+
+@pytest.mark.parametrize("lens", [[40000, 25000, 24577], [24576, 20000, 9000]])
+def test_evict_many_equal_weights(lens):
+    """More slots with the weight of the cut than the choice lists."""
+    c = Cache(2, 2, 32, "bf16", 16, lens, 2500, spare=3 * 700)
+    for n, first, recent in ((11000, 4, 100), (3000, 0, 0)):
+        check_evict(c, c.weights(0.9), n, first, recent, max_len=max(lens))
+    w = c.weights(0.5)
+    check_evict(c, torch.where(w > 0, 1.0 + torch.floor(w), w), 9000, 1, 1, max_len=max(lens))
     c.close()
 
 
