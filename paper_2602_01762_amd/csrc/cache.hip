@@ -23,20 +23,37 @@ __device__ __forceinline__ int visible_slots(const CacheView &v, int b, uint32_t
   }
   return (int)n;
 }
-// Pool row of slot s of table column `bi` of sequence b, KV head j.
-__device__ __forceinline__ uint32_t pool_row(const CacheView &v, const int32_t *table, int b, int j,
-                                             int bi, int s, uint32_t *err) {
+// Pool block and KV head of table column bi of sequence b, as block * heads + j.
+__device__ __forceinline__ uint32_t pool_block(const CacheView &v, const int32_t *table, int b, int j, int bi,
+                                               uint32_t *err) {
   const int blk = bi < v.kv.mbps ? table[(size_t)b * v.kv.mbps + bi] : -1;
   if (blk < 0 || blk >= v.kv.n_blocks) {
     atomicOr(err, ERRF_CAPACITY);
     return NO_ROW;
   }
-  return ((uint32_t)blk * v.nkv + j) * v.kv.bs + s;
+  return (uint32_t)blk * v.nkv + j;
+}
+// Pool row of slot s of that block.
+__device__ __forceinline__ uint32_t pool_row(const CacheView &v, const int32_t *table, int b, int j,
+                                             int bi, int s, uint32_t *err) {
+  const uint32_t blk = pool_block(v, table, b, j, bi, err);
+  return blk == NO_ROW ? NO_ROW : blk * v.kv.bs + s;
 }
 
 // 16 bytes that the call reads once: a nontemporal load.  Read rates of a plain
 // streaming kernel over 4.3 GB: 6.3 TB/s, with nontemporal loads 7.1.
 __device__ __forceinline__ u32x4 stream16(const void *p) { return __builtin_nontemporal_load((const u32x4 *)p); }
+// N values of a row (N * sizeof(T) a multiple of 4)
+template <typename T, int N>
+__device__ __forceinline__ void store_n(T *p, const float *x) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) ((uint32_t *)p)[i / 2] = f2bf(x[i]) | (f2bf(x[i + 1]) << 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = x[i];
+  }
+}
 // 8 values of a row <-> fp32
 template <typename T>
 __device__ __forceinline__ void load8f(const T *p, float (&x)[8]) {
@@ -54,6 +71,20 @@ __device__ __forceinline__ void load8f(const T *p, float (&x)[8]) {
     for (int i = 0; i < 4; ++i) {
       x[i] = a[i];
       x[4 + i] = b[i];
+    }
+  }
+}
+// the same from the 16-byte pieces of 8 values
+template <typename T>
+__device__ __forceinline__ void unpack8(const u32x4 (&p)[sizeof(T) / 2], float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      x[2 * i] = __uint_as_float(p[0][i] << 16);
+      x[2 * i + 1] = __uint_as_float(p[0][i] & 0xffff0000u);
+    } else {
+      x[i] = __uint_as_float(p[0][i]);
+      x[4 + i] = __uint_as_float(p[sizeof(T) / 2 - 1][i]);
     }
   }
 }
@@ -684,57 +715,155 @@ void launch_cache_attend(bool bf16, const CacheAttend &a, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------- summaries
-// Channelwise minimum and maximum of the keys of one block and KV head: one
-// wave per (table column, KV head, sequence).  fminf and fmaxf pass over NaN.
+// Channelwise minimum and maximum of the keys of a.per consecutive table
+// columns of one sequence and KV head per wave, in steps of 4 rows per lane
+// group; two steps are in flight while one is compared.  fminf and fmaxf pass
+// over NaN.  The lane groups of a wave meet by swaps of half waves and of rows:
+// one exchange and one comparison reduce two channels, after which each half
+// keeps its own.
+__device__ __forceinline__ void swap32(float &x, float &y) {   // x: low halves of both, y: high halves
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+  x = __uint_as_float(r[0]);
+  y = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ void swap16(float &x, float &y) {   // the same of even and odd rows of 16 lanes
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+  x = __uint_as_float(r[0]);
+  y = __uint_as_float(r[1]);
+}
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_cache_summarize(CacheSummarize a) {
-  constexpr int LPR = D / 8, RPI = 64 / LPR;
-  const int lane = threadIdx.x & 63, j = blockIdx.y, b = blockIdx.z, bs = a.v.kv.bs;
+  constexpr int LPR = D / 8, RPI = 64 / LPR, NI = 4, P = sizeof(T) / 2;   // P: 16-byte pieces of 8 values
+  const int lane = threadIdx.x & 63, j = blockIdx.y * (blockDim.x >> 6) + wave_id(), b = blockIdx.z, bs = a.v.kv.bs;
   const int grp = lane / LPR, li = lane % LPR;
   const int n = visible_slots(a.v, b, a.err);
   const int nblk = (int)(((long)n + bs - 1) / bs);
   const int first = a.span > 0 && a.span < n ? (n - a.span) / bs : 0;
-  const int bi = first + blockIdx.x * 4 + wave_id();
-  if (bi >= nblk) return;
-  const uint32_t row = pool_row(a.v, a.v.kv.block_table, b, j, bi, 0, a.err);
-  if (row == NO_ROW) return;
-  const int held = min(bs, n - bi * bs);
-  float lo[8], hi[8];
+  const int c0 = first + blockIdx.x * a.per, c1 = min(nblk, c0 + a.per);
+  if (c0 >= c1 || j >= a.v.nkv) return;             // whole waves
+  // lane i < a.per: pool block and KV head of column c0 + i
+  const uint32_t blks = lane < c1 - c0 ? pool_block(a.v, a.v.kv.block_table, b, j, c0 + lane, a.err) : NO_ROW;
+  // step t of the wave: rows (t % spb) NI RPI .. of column c0 + t / spb (rows
+  // past the visible ones: the last of them again; past the last step: pool
+  // block 0).  The loads are made always, so that they can be counted.
+  const int spb = (bs + NI * RPI - 1) / (NI * RPI), steps = (c1 - c0) * spb;
+  int lt = 0, lc = c0, ls = 0;                      // the next step to load
+  auto load = [&](u32x4 (&k)[NI][P]) {
+    const bool in = lt < steps;
+    const uint32_t blk = in ? (uint32_t)__builtin_amdgcn_readlane((int)blks, lc - c0) : NO_ROW;
+    const uint32_t base = blk == NO_ROW ? 0u : blk;
+    const int top = in ? min(bs, n - lc * bs) - 1 : 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo[i] = INFINITY;
-    hi[i] = -INFINITY;
-  }
-  for (int s = grp; s < held; s += RPI) {
-    float k[8];
-    load8f<T>((const T *)a.v.kv.k_pool + (size_t)(row + s) * D + 8 * li, k);
+    for (int i = 0; i < NI; ++i) {
+      const int r = min(ls + i * RPI + grp, top);
+      const T *p = (const T *)a.v.kv.k_pool + ((size_t)base * bs + r) * D + 8 * li;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      lo[i] = fminf(lo[i], k[i]);
-      hi[i] = fmaxf(hi[i], k[i]);
+      for (int x = 0; x < P; ++x) k[i][x] = stream16((const u32x4 *)p + x);
     }
-  }
+    ++lt;
+    ls += NI * RPI;
+    const bool over = ls >= bs;
+    ls = over ? 0 : ls;
+    lc += over;
+  };
+  float v[16];                                      // minima and maxima of 8 channels
+  int c = c0, left = spb;                           // the step at hand: its column, steps left of it
+  auto compare = [&](const u32x4 (&k)[NI][P]) {
+    if (left == spb) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int x = LPR; x < 64; x *= 2) {
-      lo[i] = fminf(lo[i], __shfl_xor(lo[i], x, 64));
-      hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], x, 64));
+      for (int x = 0; x < 8; ++x) {
+        v[x] = INFINITY;
+        v[8 + x] = -INFINITY;
+      }
     }
-  if (grp == 0) {
-    T *o = (T *)a.summary + (size_t)(row / bs) * 2 * D + 8 * li;
-    store8f<T>(o, lo);
-    store8f<T>(o + D, hi);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      float y[8];
+      unpack8<T>(k[i], y);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        v[x] = fminf(v[x], y[x]);
+        v[8 + x] = fmaxf(v[8 + x], y[x]);
+      }
+    }
+  };
+  auto finish = [&]() {
+    if (--left || c >= c1) return;
+    left = spb;
+    const uint32_t blk = (uint32_t)__builtin_amdgcn_readlane((int)blks, c - c0);
+    ++c;
+    T *o = (T *)a.summary + (size_t)(blk == NO_ROW ? 0u : blk) * 2 * D;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      if constexpr (LPR <= 4) {
+        v[x] = fminf(v[x], dpp_f32<DPP_ROW_ROR4>(v[x]));
+        v[8 + x] = fmaxf(v[8 + x], dpp_f32<DPP_ROW_ROR4>(v[8 + x]));
+      }
+      if constexpr (LPR <= 8) {
+        v[x] = fminf(v[x], dpp_f32<DPP_ROW_ROR8>(v[x]));
+        v[8 + x] = fmaxf(v[8 + x], dpp_f32<DPP_ROW_ROR8>(v[8 + x]));
+      }
+    }
+    // halves: lanes below 32 keep channels 0 .. 3, the others 4 .. 7
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      swap32(v[x], v[4 + x]);
+      v[x] = fminf(v[x], v[4 + x]);
+      swap32(v[8 + x], v[12 + x]);
+      v[8 + x] = fmaxf(v[8 + x], v[12 + x]);
+    }
+    constexpr int W = LPR <= 16 ? 2 : 4;            // channels that a lane keeps
+    if constexpr (W == 2) {                         // rows: the first two of those four, or the others
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        swap16(v[x], v[2 + x]);
+        v[x] = fminf(v[x], v[2 + x]);
+        swap16(v[8 + x], v[10 + x]);
+        v[8 + x] = fmaxf(v[8 + x], v[10 + x]);
+      }
+    }
+    // into channel order, so that the stores fill their lines: lane l takes
+    // channels W l .. from the lane of column l / (8 / W) that keeps them
+    const int from = lane / (8 / W) % LPR + lane % (8 / W) * (64 / (8 / W));
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+      v[x] = __shfl(v[x], from, 64);
+      v[8 + x] = __shfl(v[8 + x], from, 64);
+    }
+    if (blk != NO_ROW && lane < D / W) {
+      store_n<T, W>(o + W * lane, v);
+      store_n<T, W>(o + D + W * lane, v + 8);
+    }
+  };
+  u32x4 k0[NI][P], k1[NI][P];
+  // (the loads in this order on every path, so that a wait for one set leaves
+  // the other in flight)
+  load(k0);
+  __builtin_amdgcn_sched_barrier(0);
+  load(k1);
+  __builtin_amdgcn_sched_barrier(0);
+  for (int t = 0; t < steps; t += 2) {              // (an odd last step is followed by an idle one)
+    compare(k0);
+    load(k0);
+    __builtin_amdgcn_sched_barrier(0);
+    finish();
+    compare(k1);
+    load(k1);
+    __builtin_amdgcn_sched_barrier(0);
+    finish();
   }
 }
 
 template <typename T>
 static void summarize_d(const CacheSummarize &a, int d, hipStream_t s) {
-  const dim3 g((a.columns + 3) / 4, a.v.nkv, a.v.kv.n_seq);
-  if (d == 32) hipLaunchKernelGGL((k_cache_summarize<T, 32>), g, dim3(256), 0, s, a);
-  else if (d == 64) hipLaunchKernelGGL((k_cache_summarize<T, 64>), g, dim3(256), 0, s, a);
-  else if (d == 128) hipLaunchKernelGGL((k_cache_summarize<T, 128>), g, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_cache_summarize<T, 256>), g, dim3(256), 0, s, a);
+  // the waves of a workgroup take different heads of the same columns, whose
+  // rows lie next to each other in the pool
+  const int nw = min(4, a.v.nkv);
+  const dim3 g((a.columns + a.per - 1) / a.per, (a.v.nkv + nw - 1) / nw, a.v.kv.n_seq), t(64 * nw);
+  if (d == 32) hipLaunchKernelGGL((k_cache_summarize<T, 32>), g, t, 0, s, a);
+  else if (d == 64) hipLaunchKernelGGL((k_cache_summarize<T, 64>), g, t, 0, s, a);
+  else if (d == 128) hipLaunchKernelGGL((k_cache_summarize<T, 128>), g, t, 0, s, a);
+  else hipLaunchKernelGGL((k_cache_summarize<T, 256>), g, t, 0, s, a);
 }
 void launch_cache_summarize(bool bf16, const CacheSummarize &a, int d, hipStream_t s) {
   if (bf16) summarize_d<bf16_t>(a, d, s);
@@ -752,40 +881,117 @@ __device__ __forceinline__ uint32_t choice_key(float v) { return (uint32_t)(cand
 // block's keys; the block's score is the largest of them.  Products of stored
 // values are exact in fp64 and their sum is as good as exact, so the order of
 // the blocks does not depend on the order of the sum.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void k_cache_score(CacheSelect a) {
-  constexpr int LPR = D / 8, RPI = 64 / LPR;
-  const int lane = threadIdx.x & 63, j = blockIdx.y, b = blockIdx.z, bs = a.v.kv.bs, g = a.g;
+//   A lane group of d / 8 lanes per block; a wave takes a.per blocks, with the
+// queries in registers (G of them: the heads of a KV head, rounded up to a
+// power of two; the missing ones repeat the last) and four steps of summaries
+// in flight.  The sums of the G heads meet pairwise, so that each exchange
+// halves what is left to add.
+// v of the lane whose index differs in bit 2^X (X < 4: DPP within 16 lanes,
+// where the mirrors pair lanes of equal sums; else permlane swaps)
+template <int X>
+__device__ __forceinline__ double xor_f64(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  uint32_t l = (uint32_t)u, h = (uint32_t)(u >> 32);
+  if constexpr (X == 0) { l = dpp_u32<DPP_QUAD_XOR1>(l); h = dpp_u32<DPP_QUAD_XOR1>(h); }
+  else if constexpr (X == 1) { l = dpp_u32<DPP_QUAD_XOR2>(l); h = dpp_u32<DPP_QUAD_XOR2>(h); }
+  else if constexpr (X == 2) {                      // lane ^ 4: the half-row mirror (^ 7), then ^ 3
+    l = dpp_u32<0x1B>(dpp_u32<DPP_HALF_MIRROR>(l)); h = dpp_u32<0x1B>(dpp_u32<DPP_HALF_MIRROR>(h));
+  } else if constexpr (X == 3) { l = dpp_u32<DPP_ROW_ROR8>(l); h = dpp_u32<DPP_ROW_ROR8>(h); }
+  else { l = __float_as_uint(xor16_f(__uint_as_float(l))); h = __float_as_uint(xor16_f(__uint_as_float(h))); }
+  return __builtin_bit_cast(double, ((uint64_t)h << 32) | l);
+}
+template <int X>
+__device__ __forceinline__ float xor_f32(float v) {
+  if constexpr (X == 0) return dpp_f32<DPP_QUAD_XOR1>(v);
+  else if constexpr (X == 1) return dpp_f32<DPP_QUAD_XOR2>(v);
+  else return dpp_f32<0x1B>(dpp_f32<DPP_HALF_MIRROR>(v));
+}
+// Sums of s[0 .. N - 1] over the lane groups of 2^(SH - X) lanes; lane l ends
+// with the sum of entry bits of l (the first exchanges halve N, the others add).
+template <int N, int X, int SH>
+__device__ __forceinline__ double group_sums(double (&s)[N]) {
+  if constexpr (X == SH) {
+    return s[0];
+  } else if constexpr (N > 1) {
+    const bool odd = (threadIdx.x >> X) & 1;
+    double t[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const double keep = odd ? s[N / 2 + i] : s[i], give = odd ? s[i] : s[N / 2 + i];
+      t[i] = keep + xor_f64<X>(give);
+    }
+    return group_sums<N / 2, X + 1, SH>(t);
+  } else {
+    s[0] += xor_f64<X>(s[0]);
+    return group_sums<N, X + 1, SH>(s);
+  }
+}
+__device__ __forceinline__ float nan_max(float a, float b) { return a != a ? a : b != b ? b : fmaxf(a, b); }
+
+template <typename T, int D, int G>
+__global__ __launch_bounds__(256, G > 4 ? 2 : 3) void k_cache_score(CacheSelect a) {
+  constexpr int LPR = D / 8, RPI = 64 / LPR, P = sizeof(T) / 2, DEPTH = 4;
+  constexpr int SH = D == 32 ? 2 : D == 64 ? 3 : D == 128 ? 4 : 5;   // log2 LPR
+  // with fewer lanes than heads (d = 32, 8 heads) two rounds of 4
+  constexpr int N = G > LPR ? LPR : G;
+  const int lane = threadIdx.x & 63, j = blockIdx.y, b = blockIdx.z, bs = a.v.kv.bs;
   const int grp = lane / LPR, li = lane % LPR;
   const int n = visible_slots(a.v, b, a.err);
   const int nblk = (int)(((long)n + bs - 1) / bs);
-  const int bi = (blockIdx.x * 4 + wave_id()) * RPI + grp;
-  if (bi - grp >= nblk) return;                     // whole waves
-  const bool held = bi < nblk;
-  const uint32_t row = held ? pool_row(a.v, a.v.kv.block_table, b, j, bi, 0, a.err) : NO_ROW;
-  float lo[8] = {}, hi[8] = {};
-  if (row != NO_ROW) {
-    const T *p = (const T *)a.summary + (size_t)(row / bs) * 2 * D + 8 * li;
-    load8f<T>(p, lo);
-    load8f<T>(p + D, hi);
-  }
-  float best = -INFINITY;
-  for (int h = 0; h < g; ++h) {
-    float q[8];
-    load8f<T>((const T *)a.q + ((size_t)b * a.nq + j * g + h) * D + 8 * li, q);
-    double s = 0.0;
+  const int c0 = (blockIdx.x * 4 + wave_id()) * a.per, c1 = min(nblk, c0 + a.per);
+  if (c0 >= c1) return;                             // whole waves
+  // lane i < a.per: pool block and KV head of column c0 + i
+  const uint32_t blks = lane < c1 - c0 ? pool_block(a.v, a.v.kv.block_table, b, j, c0 + lane, a.err) : NO_ROW;
+  u32x4 mn[DEPTH][P], mx[DEPTH][P];
+  auto load = [&](int x, int c) {
+    const uint32_t blk = (uint32_t)__shfl((int)blks, min(c + grp - c0, 63), 64);
+    const T *p = (const T *)a.summary + (size_t)(blk == NO_ROW ? 0 : blk) * 2 * D + 8 * li;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += (double)q[i] * (double)(q[i] >= 0.f ? hi[i] : lo[i]);
+    for (int y = 0; y < P; ++y) {
+      mn[x][y] = stream16((const u32x4 *)p + y);
+      mx[x][y] = stream16((const u32x4 *)(p + D) + y);
+    }
+  };
 #pragma unroll
-    for (int x = 1; x < LPR; x *= 2) s += __shfl_xor(s, x, 64);
-    const float f = (float)s;
-    best = f > best || f != f ? f : best;           // NaN stays
+  for (int x = 0; x < DEPTH; ++x) load(x, c0 + x * RPI);
+  double q[G][8];
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+    float x[8];
+    load8f<T>((const T *)a.q + ((size_t)b * a.nq + j * a.g + min(h, a.g - 1)) * D + 8 * li, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[h][i] = (double)x[i];
   }
-  if (held && li == 0) {
-    const bool forced = bi < a.n_first || bi >= nblk - a.n_last;
-    a.keys[((size_t)b * a.v.nkv + j) * a.ld_keys + bi] =
-        row == NO_ROW ? 0u : forced ? KEY_FORCED : choice_key(best);
-  }
+  for (int cc = c0; cc < c1; cc += DEPTH * RPI)
+#pragma unroll
+    for (int x = 0; x < DEPTH; ++x) {
+      const int c = cc + x * RPI;
+      float lo[8], hi[8];                           // (of pool block 0 past the last column: not kept)
+      unpack8<T>(mn[x], lo);
+      unpack8<T>(mx[x], hi);
+      load(x, c + DEPTH * RPI);                     // always, so that the loads can be counted
+      float best = -INFINITY;
+#pragma unroll
+      for (int h0 = 0; h0 < G; h0 += N) {
+        double s[N];
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+          s[h] = 0.0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[h] += q[h0 + h][i] * (double)(q[h0 + h][i] >= 0.0 ? hi[i] : lo[i]);
+        }
+        best = nan_max(best, (float)group_sums<N, 0, SH>(s));
+      }
+      if constexpr (N > 1) best = nan_max(best, xor_f32<0>(best));
+      if constexpr (N > 2) best = nan_max(best, xor_f32<1>(best));
+      if constexpr (N > 4) best = nan_max(best, xor_f32<2>(best));
+      const int bi = c + grp;
+      const bool bad = (uint32_t)__shfl((int)blks, min(bi - c0, 63), 64) == NO_ROW;
+      if (bi < c1 && li == 0) {
+        const bool forced = bi < a.n_first || bi >= nblk - a.n_last;
+        a.keys[((size_t)b * a.v.nkv + j) * a.ld_keys + bi] = bad ? 0u : forced ? KEY_FORCED : choice_key(best);
+      }
+    }
 }
 
 // Inclusive sum over the lanes below, in a wave (DPP: within rows of 16
@@ -1082,14 +1288,20 @@ static void choose(const CacheChoose &a, int most, hipStream_t s) {
   else hipLaunchKernelGGL((k_cache_choose<false, true>), g, t, lds, s, a);
 }
 
+template <typename T, int D>
+static void score_g(const CacheSelect &a, hipStream_t s) {
+  const dim3 g((a.columns + 4 * a.per - 1) / (4 * a.per), a.v.nkv, a.v.kv.n_seq);
+  if (a.g == 1) hipLaunchKernelGGL((k_cache_score<T, D, 1>), g, dim3(256), 0, s, a);
+  else if (a.g == 2) hipLaunchKernelGGL((k_cache_score<T, D, 2>), g, dim3(256), 0, s, a);
+  else if (a.g <= 4) hipLaunchKernelGGL((k_cache_score<T, D, 4>), g, dim3(256), 0, s, a);
+  else if constexpr (D < 256) hipLaunchKernelGGL((k_cache_score<T, D, 8>), g, dim3(256), 0, s, a);   // g * d <= 1024
+}
 template <typename T>
 static void score_d(const CacheSelect &a, int d, hipStream_t s) {
-  const int rpi = 64 / (d / 8);
-  const dim3 g((a.columns + 4 * rpi - 1) / (4 * rpi), a.v.nkv, a.v.kv.n_seq);
-  if (d == 32) hipLaunchKernelGGL((k_cache_score<T, 32>), g, dim3(256), 0, s, a);
-  else if (d == 64) hipLaunchKernelGGL((k_cache_score<T, 64>), g, dim3(256), 0, s, a);
-  else if (d == 128) hipLaunchKernelGGL((k_cache_score<T, 128>), g, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_cache_score<T, 256>), g, dim3(256), 0, s, a);
+  if (d == 32) score_g<T, 32>(a, s);
+  else if (d == 64) score_g<T, 64>(a, s);
+  else if (d == 128) score_g<T, 128>(a, s);
+  else score_g<T, 256>(a, s);
 }
 void launch_cache_select(bool bf16, const CacheSelect &a, int d, hipStream_t s) {
   if (bf16) score_d<bf16_t>(a, d, s);
@@ -1149,8 +1361,8 @@ __global__ __launch_bounds__(256) void k_cache_copy(CacheEvict a) {
   u32x4 k[U], v[U];
 #pragma unroll
   for (int x = 0; x < U; ++x) {
-    k[x] = ((const u32x4 *)((const T *)a.v.kv.k_pool + so))[x];
-    v[x] = ((const u32x4 *)((const T *)a.v.kv.v_pool + so))[x];
+    k[x] = stream16((const u32x4 *)((const T *)a.v.kv.k_pool + so) + x);
+    v[x] = stream16((const u32x4 *)((const T *)a.v.kv.v_pool + so) + x);
   }
 #pragma unroll
   for (int x = 0; x < U; ++x) {

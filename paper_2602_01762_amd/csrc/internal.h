@@ -399,6 +399,7 @@ void launch_cache_attend(bool bf16, const CacheAttend &a, hipStream_t s);
 struct CacheSummarize {
   CacheView v;
   int span, columns;                    // last slots covered (0: all), table columns they may touch
+  int per;                              // columns per wave, 1..64
   void *summary;                        // [n_blocks, nkv, 2, d]
   uint32_t *err;
 };
@@ -408,6 +409,7 @@ struct CacheSelect {
   int nq, g;
   const void *q, *summary;
   int n_take, n_first, n_last, columns; // columns: table columns of max_len slots
+  int per;                              // columns per wave, 1..64
   uint32_t *keys; int ld_keys;          // [B, nkv, ld_keys]
   int32_t *out;                         // [B, nkv, n_take]
   uint32_t *err;

@@ -374,6 +374,18 @@ inline CachePlan cache_plan(int units, int span, bool weights) {
 // row length of the scores kept for the slot weights: whole granules
 inline int cache_score_row(int span) { return (span + CACHE_GRAN - 1) / CACHE_GRAN * CACHE_GRAN; }
 
+// Table columns per wave of the passes over the blocks of a cache (summaries,
+// scores), for units * columns of them at most: about CACHE_BLOCK_WAVES waves,
+// a multiple of `step` columns (those of one load), at most `top` <= 64 (one
+// lane looks up each).
+constexpr int CACHE_BLOCK_WAVES = 4096;
+constexpr int CACHE_SUM_COLUMNS = 8;   // summaries
+inline int cache_columns_per_wave(long units, int columns, int step, int top) {
+  const long steps = (units * columns + (long)CACHE_BLOCK_WAVES * step - 1) / ((long)CACHE_BLOCK_WAVES * step);
+  const long most = top / step;
+  return (int)(steps < 1 ? 1 : steps > most ? most : steps) * step;
+}
+
 // Choice of the best of many candidates by one workgroup: up to CHOOSE_LDS
 // have their keys in LDS; more go through scratch, in segments of CHOOSE_SEG
 // with a histogram of 1024 words each.
