@@ -1006,6 +1006,15 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
   v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);   // row_bcast:31
   return v;
 }
+// the smallest of the wave, in every lane
+__device__ __forceinline__ uint32_t wave_least(uint32_t v) {
+  v = min(v, dpp_u32<DPP_QUAD_XOR1>(v));
+  v = min(v, dpp_u32<DPP_QUAD_XOR2>(v));
+  v = min(v, dpp_u32<DPP_HALF_MIRROR>(v));
+  v = min(v, dpp_u32<DPP_ROW_MIRROR>(v));
+  const uint32_t a = min((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 16));
+  return min(a, min((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48)));
+}
 // sum of v[0 .. w - 1] (LDS, at most 64 entries), w wave-uniform
 __device__ __forceinline__ uint32_t sum_before(const uint32_t *v, int entries, int w) {
   const int lane = threadIdx.x & 63;
@@ -1014,13 +1023,15 @@ __device__ __forceinline__ uint32_t sum_before(const uint32_t *v, int entries, i
 
 // The n_take candidates of largest key of one (sequence, KV head), ties to
 // the lowest index, in index order, then -1.  A radix descent over digits of
-// 11, 11 and 10 bits with an LDS histogram finds the key of the last one taken,
-// and ends where a whole digit is taken; the candidates left after the first
-// digit are listed in LDS if at most CHOOSE_LIST are.  Each wave then owns a run
+// 11 bits with an LDS histogram finds the key of the last one taken, and ends
+// where a whole digit is taken; the candidates left after the first digit are
+// listed in LDS if at most CHOOSE_LIST are.  Each wave then owns a run
 // of candidates, so a prefix over the waves gives every taken one its place.
 // Candidates are padded with keys of 0 to groups of 256: behind all others,
 // and never reached, since fewer are taken than there are.
-//   LDS: the keys fit CHOOSE_LDS and are read once; else every pass streams
+//   LDS: the keys fit CHOOSE_LDS and are read once, and the digits start at the
+// highest bit in which they differ (scores share their exponents, and lanes
+// that add to one counter queue); else every pass streams
 // them (from the L2 after the first), and the first histogram of slots is the
 // sum of those that k_cache_keys left per CHOOSE_SEG of them.  WEIGHTS (with LDS):
 // the keys are made here from the slot weights.
@@ -1034,7 +1045,7 @@ __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
   const int j = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
   extern __shared__ __attribute__((aligned(16))) uint32_t s_keys[];
   __shared__ uint32_t hist[2][2048], list[CHOOSE_LIST];
-  __shared__ uint32_t wsum[CHOOSE_W], wgt[CHOOSE_W], weq[CHOOSE_W];
+  __shared__ uint32_t wsum[CHOOSE_W], wgt[CHOOSE_W], weq[CHOOSE_W], wmin[CHOOSE_W], wmax[CHOOSE_W];
   __shared__ uint32_t s_digit, s_above, s_count, s_listed;
   const int n_vis = visible_slots(a.v, b, a.err);
   const int bs = a.per_block ? a.v.kv.bs : 1;
@@ -1053,7 +1064,12 @@ __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
   const int g0 = wave * per, g1 = min(groups, g0 + per);
   for (int i = tid; i < 4096; i += CHOOSE_T) (&hist[0][0])[i] = 0;
   if (tid == 0) s_listed = 0;
+  // a key counts as its distance from `base`, in digits from bit top_shift + 10
+  // down; forced ones, the largest of all, in the first digit's last counter
+  uint32_t base = 0;
+  int top_shift = 21;
   if constexpr (LDS) {
+    uint32_t least = KEY_FORCED, most = 0;
     constexpr int U = 4;                            // loads in flight per thread
     for (int i0 = 0; i0 < 256 * groups; i0 += U * CHOOSE_T) {
       uint32_t k[U];
@@ -1083,14 +1099,31 @@ __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
       for (int x = 0; x < U; ++x) {
         const int i = i0 + x * CHOOSE_T + tid;
         if (i < 256 * groups) s_keys[i] = k[x];
+        least = i < n ? min(least, k[x]) : least;
+        most = i < n && k[x] != KEY_FORCED ? max(most, k[x]) : most;
       }
     }
+    least = wave_least(least);
+    most = ~wave_least(~most);
+    if (lane == 0) {
+      wmin[wave] = least;
+      wmax[wave] = most;
+    }
+    __syncthreads();
+    base = wave_least(lane < CHOOSE_W ? wmin[lane] : KEY_FORCED);
+    most = ~wave_least(lane < CHOOSE_W ? ~wmax[lane] : KEY_FORCED);
+    // the largest distance that is not forced fits below the last counter
+    top_shift = most > base ? max(0, 22 - __clz((int)(most - base))) : 0;
+    if (top_shift && ((most - base) >> (top_shift - 1)) < 2047u) --top_shift;
   }
   __syncthreads();
   auto load4 = [&](int gr) -> u32x4 {
     const int i = gr * 256 + 4 * lane;
     if constexpr (LDS) {
-      return *(const u32x4 *)(s_keys + i);
+      u32x4 k = *(const u32x4 *)(s_keys + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = max(k[e], base) - base;   // (padding is below the base)
+      return k;
     } else {
       if (gr * 256 + 256 <= n) return *(const u32x4 *)(keys + i);
       u32x4 k;
@@ -1104,13 +1137,15 @@ __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
   bool listed = false;
 #pragma unroll 1
   for (int p = 0; p < 3; ++p) {
-    const int shift = p == 0 ? 21 : p == 1 ? 10 : 0;
-    const uint32_t dm = p == 2 ? 1023u : 2047u;
+    const int shift = max(0, top_shift - 11 * p);
+    // digits of 11 bits, the last one of what is left
+    const uint32_t dm = p == 0 || top_shift - 11 * p >= 0 ? 2047u : (1u << (top_shift - 11 * p + 11)) - 1;
     uint32_t *hg = hist[p & 1];
     // one key's digit; many lanes with one digit (equal keys: unweighted
     // slots) would queue for its counter: one addition for all of them
     auto add = [&](uint32_t k, bool in) {
-      const uint32_t dg = (k >> shift) & dm, d0 = __builtin_amdgcn_readfirstlane(dg);
+      const uint32_t dg = p == 0 ? min(k >> shift, 2047u) : (k >> shift) & dm;
+      const uint32_t d0 = __builtin_amdgcn_readfirstlane(dg);
       const uint64_t same = __ballot(in && dg == d0);
       if (__popcll(same) >= 16) {
         if (lane == __builtin_ctzll(same)) atomicAdd(&hg[d0], (uint32_t)__popcll(same));
@@ -1173,9 +1208,9 @@ __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
     }
     __syncthreads();
     prefix |= s_digit << shift;
-    mask |= dm << shift;
+    mask = ~0u << shift;
     need -= s_above;
-    if (need == s_count) break;                     // the whole digit (uniform)
+    if (need == s_count || shift == 0) break;       // the whole digit, or no digit left (uniform)
     if (p == 0 && s_count <= CHOOSE_LIST) {         // (uniform) in any order: only counted
       listed = true;
 #pragma unroll 1
