@@ -239,6 +239,11 @@ __device__ __forceinline__ Walk walk_of(const CacheAttend &a) {
   w.per = max(1, (w.total + a.waves - 1) / a.waves);
   return w;
 }
+// Where the score of place p and head h of a KV head is kept: 16 places of all
+// its heads together, so that a wave's scores are one run of memory.
+__device__ __forceinline__ size_t score_at(const CacheAttend &a, int b, int j, int h, int p) {
+  return ((((size_t)b * a.v.nkv + j) * (a.ld_scores >> 4) + (p >> 4)) * a.g + h) * 16 + (p & 15);
+}
 // The part of a segment that a run starting at granule u (< w.total) and
 // ending at `last` begins with.
 struct Segment {
@@ -366,7 +371,7 @@ __global__ __launch_bounds__(64, G > 4 ? 1 : 2) void k_cache_attend(CacheAttend 
             for (int x = 0; x < 8; ++x) s[i] += q[h][x] * kc[i][x];
             s[i] = group_sum(s[i], SH) * a.scale;
             if (!((mask >> (i * RPI + grp)) & 1)) s[i] = -INFINITY;
-            if (a.scores && li == 0) a.scores[(h0 + h) * a.ld_scores + t + i * RPI + grp] = s[i];
+            if (a.scores && li == 0) a.scores[score_at(a, sg.b, sg.j, h, t + i * RPI + grp)] = s[i];
             mx = fmaxf(mx, s[i]);
           }
           const float mn = fmaxf(m[h], mx);
@@ -446,13 +451,21 @@ struct MfmaTile {
   __device__ static int at(int s, int c) { return (s * LPR + (c ^ swz(s))) * 16; }
 };
 
-template <int D>
+//   Scores that are kept (KEEP, for the slot weights) gather in 4 KB of LDS
+// and are stored a buffer at a time, ahead of the next loads.  Stores count
+// with the loads and retire in order with them, so each one delays the wait
+// for a tile's rows: 16 sequences of up to 16384 slots took 109 us with a store
+// per tile, 93 without any, 105 so.
+template <int D, bool KEEP>
 __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
   using M = MfmaTile<D>;
   constexpr int TS = M::TS, LPR = M::LPR, RPI = M::RPI, NI = M::NI;
   constexpr int NS = TS / 16, NK = D / 32, ND = D / 16;
   __shared__ __attribute__((aligned(16))) char s_k[TS * D * 2], s_v[TS * D * 2];
+  constexpr int KEPT = 1024;                                // scores in LDS
+  __shared__ __attribute__((aligned(16))) float s_s[KEEP ? KEPT : 4];
   const int lane = threadIdx.x, g = a.g;
+  const int most = KEPT / (g * TS) * TS;                    // places whose scores fit (g <= 8: at least one tile)
   const int col = lane & 15, q4 = lane >> 4, grp = lane / LPR, li = lane % LPR;
   const KvArgs &kv = a.v.kv;
   const Walk wk = walk_of(a);
@@ -483,6 +496,14 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
       qf[kk] = col < g ? *(const u32x4 *)((const bf16_t *)a.q + hi * D + 32 * kk + 8 * q4) : u32x4{0, 0, 0, 0};
     int id1, pv1, b1, id2, pv2;
     uint32_t row = NO_ROW;
+    int kept = sg.p0;                                       // first place whose scores are in LDS
+    auto store_scores = [&](int to) {                       // places kept .. to - 1
+      wave_lds_sync();
+      float *ps = a.scores + score_at(a, sg.b, sg.j, 0, kept);
+      for (int i = 4 * lane; i < (to - kept) * g; i += 256) *(f32x4 *)(ps + i) = *(const f32x4 *)(s_s + i);
+      wave_lds_sync();
+      kept = to;
+    };
     if (sg.p0 < sg.p1) {
       int id0, pv0;
       lk.column(sg.p0 + lane, id0, pv0);
@@ -508,6 +529,8 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
         *(u32x4 *)(s_k + M::at(i * RPI + grp, li)) = kr[i];
         *(u32x4 *)(s_v + M::at(i * RPI + grp, li)) = vr[i];
       }
+      if constexpr (KEEP)
+        if (t - kept == most) store_scores(t);
       // the lookups of the tile after the next one, and the next one's rows
       if (t + TS < sg.p1) {
         row = lane < TS ? lk.row(t + TS + lane, id1, pv1, b1) : NO_ROW;
@@ -535,10 +558,11 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
           sc[st][i] = ((mask >> (16 * st + 4 * q4 + i)) & 1) ? sc[st][i] * a.scale : -INFINITY;
           mx = fmaxf(mx, sc[st][i]);
         }
-      if (a.scores && col < g) {
-        float *ps = a.scores + hi * a.ld_scores + t + 4 * q4;
+      if constexpr (KEEP) {
+        if (col < g) {
 #pragma unroll
-        for (int st = 0; st < NS; ++st) *(f32x4 *)(ps + 16 * st) = sc[st];
+          for (int st = 0; st < NS; ++st) *(f32x4 *)(s_s + (t - kept + 16 * st) * g + 16 * col + 4 * q4) = sc[st];
+        }
       }
       mx = fmaxf(mx, xor16_f(mx));
       mx = fmaxf(mx, xor32_f(mx));
@@ -585,6 +609,8 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
         }
       wave_lds_sync();                                 // reads done before the next tile's writes
     }
+    if constexpr (KEEP)
+      if (sg.p0 < sg.p1) store_scores(sg.p0 + (sg.p1 - sg.p0 + TS - 1) / TS * TS);
     if (col >= g) continue;
     if (a.direct) {
       const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
@@ -628,63 +654,123 @@ __device__ __forceinline__ void join_stats(const CacheAttend &a, const Parts &p,
   l = wave_sum(s);
 }
 
-// Join: workgroup x < nq adds the partial outputs of query head x, each
-// weighted by 2^(its maximum - the largest one), in an order that only the
-// lengths set.  The others (with slot weights) take JOIN_P places of one KV
-// head each: the sum over its g heads of 2^(score - log-sum) is added to the
-// place's slot, which one thread owns.
+// Join: T threads per query head add its partial outputs, each weighted by
+// 2^(its maximum - the largest one), in an order that only the lengths set:
+// a wave where a head has few partials, so that no barrier is needed, a
+// workgroup where it has many.  The first loads go out before the statistics
+// are known.  Workgroups past the heads (with slot weights) take JOIN_P places
+// of one KV head each: the sum over its g heads of 2^(score - log-sum) is
+// added to the place's slot, which one thread owns.
 constexpr int JOIN_P = 1024;
-template <typename T>
+template <typename T, int D, int TH>
 __global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
-  const int b = blockIdx.y, tid = threadIdx.x, wave = wave_id(), d = a.d;
+  constexpr int Q = D / 4, G = TH / Q, PRE = 4;         // lanes per partial, groups of partials, early loads
+  const int b = blockIdx.y, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
+  const int heads = (a.nq + 256 / TH - 1) / (256 / TH);   // workgroups that join
   const Walk w = walk_of(a);                           // every wave for itself
-  if ((int)blockIdx.x < a.nq) {
-    const int h = blockIdx.x;
+  if ((int)blockIdx.x < heads) {
+    const int h = blockIdx.x * (256 / TH) + tid / TH, t = tid % TH;
+    if (TH == 64 && h >= a.nq) return;                 // whole waves
     const size_t hi = (size_t)b * a.nq + h;
-    const Parts p = parts_of(a, w, b, h / a.g, h % a.g);
-    __shared__ float red[256 * 4];
+    const int hw = __builtin_amdgcn_readfirstlane(h);
+    const Parts p = parts_of(a, w, b, hw / a.g, hw % a.g);
+    const int x = t % Q, grp = t / Q;
+    f32x4 pre[PRE];
+#pragma unroll
+    for (int i = 0; i < PRE; ++i) {
+      const int c = grp + i * G;
+      pre[i] = c < p.np ? *(const f32x4 *)(a.po + (p.at + (size_t)c * a.g) * D + 4 * x) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    float pm[PRE];
+#pragma unroll
+    for (int i = 0; i < PRE; ++i) {
+      const int c = grp + i * G;
+      pm[i] = c < p.np ? a.pm[p.at + (size_t)c * a.g] : -INFINITY;
+    }
     float M, l;
     join_stats(a, p, M, l);
-    // thread = (4 dims, group of partials)
-    const int q = d / 4, G = 256 / q, x = tid % q, grp = tid / q;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int c = grp; c < p.np; c += G) {
-      const size_t i = p.at + (size_t)c * a.g;
-      o += *(const f32x4 *)(a.po + i * d + 4 * x) * exp2f(a.pm[i] - M);
-    }
-    *(f32x4 *)(red + 4 * tid) = o;
-    __syncthreads();
-    if (grp == 0) {
-      for (int y = 1; y < G; ++y) o += *(const f32x4 *)(red + 4 * (y * q + x));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) Ty<T>::st((T *)a.out, hi * d + 4 * x + i, l == 0.f ? 0.f : o[i] / l);
+    for (int i = 0; i < PRE; ++i) o += pre[i] * exp2f(pm[i] - M);
+#pragma unroll 4
+    for (int c = grp + PRE * G; c < p.np; c += G) {
+      const size_t i = p.at + (size_t)c * a.g;
+      o += *(const f32x4 *)(a.po + i * D + 4 * x) * exp2f(a.pm[i] - M);
     }
-    if (tid == 0 && a.lse) a.lse[hi] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
+    if constexpr (TH == 64) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = stride_sum(o[i], Q);
+    } else {
+      __shared__ float red[TH * 4];
+      *(f32x4 *)(red + 4 * t) = o;
+      __syncthreads();
+      if (grp == 0)
+        for (int y = 1; y < G; ++y) o += *(const f32x4 *)(red + 4 * (y * Q + x));
+    }
+    if (grp == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = l == 0.f ? 0.f : o[i] / l;
+      T *out = (T *)a.out + hi * D + 4 * x;
+      if constexpr (sizeof(T) == 2) *(uint2 *)out = uint2{f2bf(o[0]) | (f2bf(o[1]) << 16), f2bf(o[2]) | (f2bf(o[3]) << 16)};
+      else *(f32x4 *)out = o;
+    }
+    if (t == 0 && a.lse) a.lse[hi] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
     return;
   }
-  const int y = blockIdx.x - a.nq, j = y % a.v.nkv, g = a.g;
+  constexpr int U = JOIN_P / 256;
+  const int y = blockIdx.x - heads, j = y % a.v.nkv, g = a.g;
   const int n = __builtin_amdgcn_readlane(w.n, b), places = places_of(a, n);
   const int t0 = y / a.v.nkv * JOIN_P;
   if (t0 >= places) return;
+  const Segment sg{b, j, n, 0, 0, places};
+  const Lookup lk(a, sg);
+  int id[U], prev[U], blk[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) lk.column(t0 + i * 256 + tid, id[i], prev[i]);
+#pragma unroll
+  for (int i = 0; i < U; ++i) blk[i] = lk.block(id[i]);
   __shared__ float lse[CACHE_MAXG];
   for (int h = wave; h < g; h += 4) {
     float M, l;
     join_stats(a, parts_of(a, w, b, j, h), M, l);
-    if ((tid & 63) == 0) lse[h] = l == 0.f ? INFINITY : M + log2f(l);   // nothing seen: every weight 0
+    if (lane == 0) lse[h] = l == 0.f ? INFINITY : M + log2f(l);   // nothing seen: every weight 0
+  }
+  uint32_t row[U];
+  float old[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    row[i] = lk.row(t0 + i * 256 + tid, id[i], prev[i], blk[i]);
+    old[i] = a.weights[row[i] == NO_ROW ? 0 : row[i]];
   }
   __syncthreads();
-  const Segment sg{b, j, n, 0, 0, min(places, t0 + JOIN_P)};
-  const Lookup lk(a, sg);
-  for (int p = t0 + tid; p < sg.p1; p += 256) {
-    int id, prev;
-    lk.column(p, id, prev);
-    const uint32_t row = lk.row(p, id, prev, lk.block(id));
-    if (row == NO_ROW) continue;
-    float s = 0.f;
-    for (int h = 0; h < g; ++h) s += exp2f(a.scores[((size_t)b * a.nq + j * g + h) * a.ld_scores + p] - lse[h]);
-    a.weights[row] += s;
+  float sum[U] = {};
+  for (int h = 0; h < g; ++h) {
+    const float *sc = a.scores + score_at(a, b, j, h, t0 + tid);
+    float s[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) s[i] = t0 + i * 256 + tid < places ? sc[i * 256 * g] : 0.f;
+#pragma unroll
+    for (int i = 0; i < U; ++i) sum[i] += exp2f(s[i] - lse[h]);
   }
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+    if (row[i] != NO_ROW) a.weights[row[i]] = old[i] + sum[i];
+}
+template <typename T, int D>
+static void join_d(const CacheAttend &a, hipStream_t s) {
+  // partials of a head on average: a wave adds 64 / (D / 4) at a time
+  const bool few = a.waves / (a.v.nkv * a.v.kv.n_seq) <= 16;
+  const int per = few ? 4 : 1;
+  const dim3 g((a.nq + per - 1) / per + (a.weights ? a.v.nkv * ((a.span + JOIN_P - 1) / JOIN_P) : 0), a.v.kv.n_seq);
+  if (few) hipLaunchKernelGGL((k_cache_join<T, D, 64>), g, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_cache_join<T, D, 256>), g, dim3(256), 0, s, a);
+}
+template <typename T>
+static void join(const CacheAttend &a, hipStream_t s) {
+  if (a.d == 32) join_d<T, 32>(a, s);
+  else if (a.d == 64) join_d<T, 64>(a, s);
+  else if (a.d == 128) join_d<T, 128>(a, s);
+  else join_d<T, 256>(a, s);
 }
 
 template <int D>
@@ -695,13 +781,18 @@ static void attend_f32(const CacheAttend &a, hipStream_t s) {
   else if (a.g <= 4) hipLaunchKernelGGL((k_cache_attend<D, 4>), g, t, 0, s, a);
   else if constexpr (D < 256) hipLaunchKernelGGL((k_cache_attend<D, 8>), g, t, 0, s, a);   // g * d <= 1024
 }
-void launch_cache_attend(bool bf16, const CacheAttend &a, hipStream_t s) {
+template <int D>
+static void attend_bf16(const CacheAttend &a, hipStream_t s) {
   const dim3 g(a.waves), t(64);
+  if (a.weights) hipLaunchKernelGGL((k_cache_attend_mfma<D, true>), g, t, 0, s, a);
+  else hipLaunchKernelGGL((k_cache_attend_mfma<D, false>), g, t, 0, s, a);
+}
+void launch_cache_attend(bool bf16, const CacheAttend &a, hipStream_t s) {
   if (bf16) {
-    if (a.d == 32) hipLaunchKernelGGL((k_cache_attend_mfma<32>), g, t, 0, s, a);
-    else if (a.d == 64) hipLaunchKernelGGL((k_cache_attend_mfma<64>), g, t, 0, s, a);
-    else if (a.d == 128) hipLaunchKernelGGL((k_cache_attend_mfma<128>), g, t, 0, s, a);
-    else hipLaunchKernelGGL((k_cache_attend_mfma<256>), g, t, 0, s, a);
+    if (a.d == 32) attend_bf16<32>(a, s);
+    else if (a.d == 64) attend_bf16<64>(a, s);
+    else if (a.d == 128) attend_bf16<128>(a, s);
+    else attend_bf16<256>(a, s);
   } else {
     if (a.d == 32) attend_f32<32>(a, s);
     else if (a.d == 64) attend_f32<64>(a, s);
@@ -709,9 +800,8 @@ void launch_cache_attend(bool bf16, const CacheAttend &a, hipStream_t s) {
     else attend_f32<256>(a, s);
   }
   if (a.direct) return;
-  const dim3 gj(a.nq + (a.weights ? a.v.nkv * ((a.span + JOIN_P - 1) / JOIN_P) : 0), a.v.kv.n_seq);
-  if (bf16) hipLaunchKernelGGL(k_cache_join<bf16_t>, gj, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(k_cache_join<float>, gj, dim3(256), 0, s, a);
+  if (bf16) join<bf16_t>(a, s);
+  else join<float>(a, s);
 }
 
 // ---------------------------------------------------------------- summaries

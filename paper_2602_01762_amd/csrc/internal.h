@@ -390,7 +390,7 @@ struct CacheAttend {
   int waves, direct;                    // cache_plan
   float scale;                          // log2(e) / sqrt(d)
   float *pm, *pl, *po;                  // partials [waves + B * nkv][g] / [.., d]
-  float *scores; int ld_scores;         // [B, nq, ld_scores] in base 2 (weights only)
+  float *scores; int ld_scores;         // [B, nkv, ld_scores / 16, g, 16] in base 2 (weights only)
   void *out; float *lse;                // [B, nq, d] / [B, nq] or NULL
   float *weights;                       // slot weights, or NULL
   uint32_t *err;

@@ -259,6 +259,9 @@ class Drafter:
                     B.prism_cache_eviction())
         self._scratch_bytes = {}
 
+    def _stream(self) -> int:
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
+
     def _expect(self, t, name: str, shape, dtype) -> int:
         """Data pointer of a contiguous tensor of this shape and type on the
         context's device."""
@@ -277,7 +280,7 @@ class Drafter:
             raise ValueError("%s must be contiguous" % name)
         return t.data_ptr()          # a subclass of Tensor
 
-    def _scratch(self, call: int, batch: int, max_len: int):
+    def _scratch(self, call: int, batch: int, max_len: int, like):
         key = (call, batch, max_len)
         n = self._scratch_bytes.get(key)
         if n is None:
@@ -285,7 +288,7 @@ class Drafter:
             if len(self._scratch_bytes) >= 1024:      # callers that pass a new bound at every step
                 self._scratch_bytes.clear()
             self._scratch_bytes[key] = n
-        return n, torch.empty(n, dtype=torch.uint8, device=self.device)
+        return n, like.new_empty(-(-n // like.element_size()))
 
     def cache(self, lens, k_pool, v_pool, block_table) -> B.prism_batch:
         """The sequences of a cache call: lens [B] int32 slots held, pools
@@ -326,9 +329,11 @@ class Drafter:
                         else self._expect(weights, "weights", kv.slots, torch.float32))
         shape = (T, self._nq, self._d)
         if out is None:
-            out = torch.empty(shape, dtype=dt, device=self.device)
-        io.d_q = self._expect(out, "out", shape, dt)
-        B.prism_cache_append(self.ctx, io)
+            out = qkv.new_empty(shape)
+            io.d_q = out.data_ptr()
+        else:
+            io.d_q = self._expect(out, "out", shape, dt)
+        B.prism_cache_append(self.ctx, io, self._stream())
         return out
 
     def cache_attend(self, kv, q, n_new: int = 0, max_len: int = 0, blocks=None, weights=None,
@@ -357,13 +362,15 @@ class Drafter:
             io.d_weights = self._expect(weights, "weights", kv.slots, torch.float32)
             call = B.PRISM_CACHE_ATTEND_WEIGHTS
         if out is None:
-            out = torch.empty(shape, dtype=dt, device=self.device)
-        io.d_out = self._expect(out, "out", shape, dt)
+            out = q.new_empty(shape)
+            io.d_out = out.data_ptr()
+        else:
+            io.d_out = self._expect(out, "out", shape, dt)
         sums = torch.empty(shape[:2], dtype=torch.float32, device=self.device) if lse else None
         io.d_lse = None if sums is None else sums.data_ptr()
-        io.scratch_bytes, scratch = self._scratch(call, nb, span)
+        io.scratch_bytes, scratch = self._scratch(call, nb, span, q)
         io.d_scratch = scratch.data_ptr()
-        B.prism_cache_attend(self.ctx, io)
+        B.prism_cache_attend(self.ctx, io, self._stream())
         return {"out": out, "lse": sums}
 
     def summary_buffer(self, kv):
@@ -374,7 +381,7 @@ class Drafter:
         """Write the key minima and maxima of the blocks that hold the last
         span slots (0: of every block) into summary [blocks, n_kv, 2, d]."""
         self._expect(summary, "summary", kv.summary, self._dt)
-        B.prism_cache_summarize(self.ctx, kv, n_new, span, summary)
+        B.prism_cache_summarize(self.ctx, kv, n_new, span, summary, self._stream())
         return summary
 
     def cache_select(self, kv, q, summary, n_blocks: int, n_first: int = 0, n_last: int = 0,
@@ -394,10 +401,12 @@ class Drafter:
         shape = (nb, self._nkv, max(n_blocks, 0))
         if out is None:
             out = torch.empty(shape, dtype=torch.int32, device=self.device)
-        io.d_blocks = self._expect(out, "out", shape, torch.int32)
-        io.scratch_bytes, scratch = self._scratch(B.PRISM_CACHE_SELECT, nb, max_len)
+            io.d_blocks = out.data_ptr()
+        else:
+            io.d_blocks = self._expect(out, "out", shape, torch.int32)
+        io.scratch_bytes, scratch = self._scratch(B.PRISM_CACHE_SELECT, nb, max_len, q)
         io.d_scratch = scratch.data_ptr()
-        B.prism_cache_select(self.ctx, io)
+        B.prism_cache_select(self.ctx, io, self._stream())
         return out
 
     def cache_evict(self, kv, new_table, weights, n_keep: int, n_first: int = 0, n_recent: int = 0,
@@ -414,13 +423,13 @@ class Drafter:
         io.n_keep = n_keep
         io.n_first = n_first
         io.n_recent = n_recent
-        kept = torch.empty((nb, self._nkv, max(n_keep, 0)), dtype=torch.int32, device=self.device)
-        lens = torch.empty(nb, dtype=torch.int32, device=self.device)
+        kept = new_table.new_empty((nb, self._nkv, max(n_keep, 0)))
+        lens = new_table.new_empty(nb)
         io.d_kept = kept.data_ptr()
         io.d_new_lens = lens.data_ptr()
-        io.scratch_bytes, scratch = self._scratch(B.PRISM_CACHE_EVICT, nb, max_len)
+        io.scratch_bytes, scratch = self._scratch(B.PRISM_CACHE_EVICT, nb, max_len, weights)
         io.d_scratch = scratch.data_ptr()
-        B.prism_cache_evict(self.ctx, io)
+        B.prism_cache_evict(self.ctx, io, self._stream())
         return {"kept": kept, "lens": lens}
 
     def device_status(self) -> int:
