@@ -258,8 +258,8 @@ __device__ __forceinline__ Segment segment_at(const CacheAttend &a, const Walk &
   s.j = at / count;
   const int first = at - s.j * count;
   s.granules = min(last - u, count - first);
-  s.p0 = first * CACHE_GRAN;
-  s.p1 = min(places_of(a, s.n), (first + s.granules) * CACHE_GRAN);
+  s.p0 = first * CACHE_GRAN;                   // (0 in a direct call, whose one granule is the segment)
+  s.p1 = a.direct ? places_of(a, s.n) : min(places_of(a, s.n), (first + s.granules) * CACHE_GRAN);
   return s;
 }
 
@@ -1122,21 +1122,59 @@ __device__ __forceinline__ uint32_t sum_before(const uint32_t *v, int entries, i
 //   LDS: the keys fit CHOOSE_LDS and are read once, and the digits start at the
 // highest bit in which they differ (scores share their exponents, and lanes
 // that add to one counter queue); else every pass streams
-// them (from the L2 after the first), and the first histogram of slots is the
-// sum of those that k_cache_keys left per CHOOSE_SEG of them.  WEIGHTS (with LDS):
-// the keys are made here from the slot weights.
+// them (from the L2 after the first).  WEIGHTS (with LDS): the keys are made
+// here from the slot weights.
 //   One workgroup's instructions bound it: 512 cycles per instruction of a
 // pass over 131072 keys.  8192 blocks 10 us (13 with a loop per digit over all
 // keys and sums over the waves in loops).
 constexpr int CHOOSE_T = 1024, CHOOSE_W = CHOOSE_T / 64;
 constexpr int CHOOSE_LIST = 8192;
+// One key's digit counted.  Many lanes with one digit (equal keys: unweighted
+// slots) would queue for its counter: one addition for all of them.
+__device__ __forceinline__ void count_digit(uint32_t *hg, uint32_t dg, bool in) {
+  const uint32_t d0 = __builtin_amdgcn_readfirstlane(dg);
+  const uint64_t same = __ballot(in && dg == d0);
+  if (__popcll(same) >= 16) {
+    if ((int)(threadIdx.x & 63) == __builtin_ctzll(same)) atomicAdd(&hg[d0], (uint32_t)__popcll(same));
+    in &= dg != d0;
+  }
+  if (in) atomicAdd(&hg[dg], 1u);
+}
+// Of 2048 counters (complete: behind a barrier), the digit in which the
+// need-th largest lies, the number above it and its own count.  Whole workgroup
+// of CHOOSE_T threads; `clear` zeroes the counters.
+struct Digit {
+  uint32_t digit, above, count;
+};
+struct DigitWs {
+  uint32_t wsum[CHOOSE_W];
+  Digit d;
+};
+__device__ __forceinline__ Digit digit_of(uint32_t *hg, uint32_t need, bool clear, DigitWs &ws) {
+  const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
+  // thread t owns the digits 2047 - 2t and 2046 - 2t: a sum over the threads
+  // before it counts the digits above
+  const uint32_t h1 = hg[2047 - 2 * tid], h0 = hg[2046 - 2 * tid];
+  const uint32_t scan = wave_scan(h0 + h1);
+  if (lane == 63) ws.wsum[wave] = scan;
+  if (clear) {
+    hg[2047 - 2 * tid] = 0;
+    hg[2046 - 2 * tid] = 0;
+  }
+  __syncthreads();
+  const uint32_t above = sum_before(ws.wsum, CHOOSE_W, wave) + scan - h0 - h1;
+  if (above < need && above + h1 >= need) ws.d = {2047u - 2 * tid, above, h1};
+  else if (above + h1 < need && above + h1 + h0 >= need) ws.d = {2046u - 2 * tid, above + h1, h0};
+  __syncthreads();
+  return ws.d;
+}
 template <bool WEIGHTS, bool LDS>
 __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
   const int j = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
   extern __shared__ __attribute__((aligned(16))) uint32_t s_keys[];
   __shared__ uint32_t hist[2][2048], list[CHOOSE_LIST];
-  __shared__ uint32_t wsum[CHOOSE_W], wgt[CHOOSE_W], weq[CHOOSE_W], wmin[CHOOSE_W], wmax[CHOOSE_W];
-  __shared__ uint32_t s_digit, s_above, s_count, s_listed;
+  __shared__ uint32_t wgt[CHOOSE_W], weq[CHOOSE_W], wmin[CHOOSE_W], wmax[CHOOSE_W], s_listed;
+  __shared__ DigitWs dws;
   const int n_vis = visible_slots(a.v, b, a.err);
   const int bs = a.per_block ? a.v.kv.bs : 1;
   const int n = (int)(((long)n_vis + bs - 1) / bs);
@@ -1231,32 +1269,11 @@ __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
     // digits of 11 bits, the last one of what is left
     const uint32_t dm = p == 0 || top_shift - 11 * p >= 0 ? 2047u : (1u << (top_shift - 11 * p + 11)) - 1;
     uint32_t *hg = hist[p & 1];
-    // one key's digit; many lanes with one digit (equal keys: unweighted
-    // slots) would queue for its counter: one addition for all of them
     auto add = [&](uint32_t k, bool in) {
-      const uint32_t dg = p == 0 ? min(k >> shift, 2047u) : (k >> shift) & dm;
-      const uint32_t d0 = __builtin_amdgcn_readfirstlane(dg);
-      const uint64_t same = __ballot(in && dg == d0);
-      if (__popcll(same) >= 16) {
-        if (lane == __builtin_ctzll(same)) atomicAdd(&hg[d0], (uint32_t)__popcll(same));
-        in &= dg != d0;
-      }
-      if (in) atomicAdd(&hg[dg], 1u);
+      count_digit(hg, p == 0 ? min(k >> shift, 2047u) : (k >> shift) & dm, in);
     };
     if (listed) {
       for (int i = tid; i < (int)s_listed; i += CHOOSE_T) add(list[i], (list[i] & mask) == prefix);
-    } else if (!LDS && p == 0 && a.hists) {                    // 2 digits per thread
-      const int segs = (n + CHOOSE_SEG - 1) / CHOOSE_SEG;
-      const uint32_t *h = a.hists + u * a.ld_hists + tid;
-      uint32_t lo = 0, hi = 0;
-#pragma unroll 8
-      for (int sgm = 0; sgm < segs; ++sgm) {
-        const uint32_t v = h[sgm * 1024];
-        lo += v & 0xffffu;
-        hi += v >> 16;
-      }
-      hg[2 * tid] = lo;
-      hg[2 * tid + 1] = hi;
     } else {
 #pragma unroll 1
       for (int gr = g0; gr < g1; gr += UG) {
@@ -1276,32 +1293,12 @@ __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
       }
     }
     __syncthreads();
-    // thread t owns the digits 2047 - 2t and 2046 - 2t: a sum over the threads
-    // before it counts the digits above
-    const uint32_t h1 = hg[2047 - 2 * tid], h0 = hg[2046 - 2 * tid];
-    const uint32_t scan = wave_scan(h0 + h1);
-    if (lane == 63) wsum[wave] = scan;
-    if (p == 0) {                                   // (the third pass counts here again)
-      hg[2047 - 2 * tid] = 0;
-      hg[2046 - 2 * tid] = 0;
-    }
-    __syncthreads();
-    const uint32_t above = sum_before(wsum, CHOOSE_W, wave) + scan - h0 - h1;
-    if (above < need && above + h1 >= need) {
-      s_digit = 2047 - 2 * tid;
-      s_above = above;
-      s_count = h1;
-    } else if (above + h1 < need && above + h1 + h0 >= need) {
-      s_digit = 2046 - 2 * tid;
-      s_above = above + h1;
-      s_count = h0;
-    }
-    __syncthreads();
-    prefix |= s_digit << shift;
+    const Digit dg = digit_of(hg, need, p == 0, dws);   // (the third pass counts here again)
+    prefix |= dg.digit << shift;
     mask = ~0u << shift;
-    need -= s_above;
-    if (need == s_count || shift == 0) break;       // the whole digit, or no digit left (uniform)
-    if (p == 0 && s_count <= CHOOSE_LIST) {         // (uniform) in any order: only counted
+    need -= dg.above;
+    if (need == dg.count || shift == 0) break;      // the whole digit, or no digit left (uniform)
+    if (p == 0 && dg.count <= CHOOSE_LIST) {        // (uniform) in any order: only counted
       listed = true;
 #pragma unroll 1
       for (int gr = g0; gr < g1; gr += UG) {
@@ -1405,7 +1402,246 @@ __global__ __launch_bounds__(CHOOSE_T) void k_cache_choose(CacheChoose a) {
 }
 // at most CHOOSE_LDS candidates have their keys in LDS (96 KB beside the 48
 // of histograms and list; a workgroup may take 160)
+
+// The same choice for more slots than fit one CU's LDS, spread over the chip in
+// segments of CHOOSE_SEG keys: k_cache_keys makes the keys and the segments'
+// histograms of the first digit; a workgroup per segment (k_cache_collect)
+// finds the digit of the cut from all of them, counts its keys above and lists
+// those in it; one workgroup per (sequence, KV head) (k_cache_cut) descends
+// through the listed keys, or through all where they are too many, and leaves
+// the cut and each segment's place in the output; a workgroup per segment
+// (k_cache_emit) writes its indices there.  16384 of 131000 slots of 8 heads:
+// 27 us, by one workgroup per head 53.
+//   cut of unit u (words): prefix, mask, need, -, then per segment the number
+// taken before it and the number equal to the prefix before it, then per
+// segment its keys above the first digit's cut and in it.
+constexpr int CUT_SEG = 4;
+__device__ __forceinline__ int wide_count(const CacheChoose &a, int b) { return visible_slots(a.v, b, a.err); }
+// the segments' histograms summed into hg
+__device__ __forceinline__ void sum_hists(const CacheChoose &a, size_t u, int segs, uint32_t *hg) {
+  const uint32_t *h = a.hists + u * a.ld_hists + threadIdx.x;
+  uint32_t lo = 0, hi = 0;
+#pragma unroll 8
+  for (int x = 0; x < segs; ++x) {
+    const uint32_t v = h[x * 1024];
+    lo += v & 0xffffu;
+    hi += v >> 16;
+  }
+  hg[2 * threadIdx.x] = lo;
+  hg[2 * threadIdx.x + 1] = hi;
+  __syncthreads();
+}
+// 4 keys of this thread in a segment (0 past the end: behind all, never taken)
+__device__ __forceinline__ u32x4 seg_keys(const uint32_t *keys, int i, int n) {
+  if (i + 4 <= n) return *(const u32x4 *)(keys + i);
+  u32x4 k;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) k[e] = i + e < n ? keys[i + e] : 0u;
+  return k;
+}
+__global__ __launch_bounds__(CHOOSE_T) void k_cache_collect(CacheChoose a) {
+  static_assert(CHOOSE_SEG == 4 * CHOOSE_T, "4 keys per thread");
+  const int sg = blockIdx.x, j = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
+  __shared__ uint32_t hg[2048], wgt[CHOOSE_W], weq[CHOOSE_W];
+  __shared__ DigitWs dws;
+  const int n = wide_count(a, b);
+  if (n <= a.n_take || sg * CHOOSE_SEG >= n) return;
+  const size_t u = (size_t)b * a.v.nkv + j;
+  const int segs = (n + CHOOSE_SEG - 1) / CHOOSE_SEG;
+  const u32x4 k = seg_keys(a.keys + u * a.ld_keys, sg * CHOOSE_SEG + 4 * tid, n);
+  sum_hists(a, u, segs, hg);
+  const uint32_t d = digit_of(hg, a.n_take, false, dws).digit;
+  uint32_t gt = 0, eq = 0;
+  uint64_t m[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool in = sg * CHOOSE_SEG + 4 * tid + e < n;
+    gt += __popcll(__ballot(in && (k[e] >> 21) > d));
+    m[e] = __ballot(in && (k[e] >> 21) == d);
+    eq += __popcll(m[e]);
+  }
+  if (lane == 0) {
+    wgt[wave] = gt;
+    weq[wave] = eq;
+  }
+  __syncthreads();
+  uint32_t to = sum_before(weq, CHOOSE_W, wave);
+  uint32_t *cand = a.cand + u * a.ld_cand + (size_t)sg * CHOOSE_SEG;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if ((m[e] >> lane) & 1) cand[to + __popcll(m[e] & ((1ull << lane) - 1))] = k[e];
+    to += __popcll(m[e]);
+  }
+  if (wave == 0) {
+    const uint32_t g = sum_before(wgt, CHOOSE_W, CHOOSE_W), q = sum_before(weq, CHOOSE_W, CHOOSE_W);
+    uint32_t *c = a.cut + u * a.ld_cut + CUT_SEG + 2 * ((size_t)a.ld_cand / CHOOSE_SEG + sg);
+    if (lane == 0) {
+      c[0] = g;
+      c[1] = q;
+    }
+  }
+}
+// exclusive sums over up to CHOOSE_MAX_SEGS entries (LDS), by one wave; the
+// total in v[n]
+__device__ __forceinline__ void scan_segs(uint32_t *v, int n) {
+  const int lane = threadIdx.x & 63;
+  uint32_t run = 0;
+  for (int i = 0; i < n; i += 64) {
+    const uint32_t x = i + lane < n ? v[i + lane] : 0u, t = wave_scan(x);
+    if (i + lane < n) v[i + lane] = run + t - x;
+    run += (uint32_t)__builtin_amdgcn_readlane((int)t, 63);
+  }
+  if (lane == 0) v[n] = run;
+}
+__global__ __launch_bounds__(CHOOSE_T) void k_cache_cut(CacheChoose a) {
+  const int j = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
+  __shared__ uint32_t hist[2][2048], list[CHOOSE_LIST];
+  __shared__ uint32_t s_gt[CHOOSE_MAX_SEGS + 1], s_eq[CHOOSE_MAX_SEGS + 1];
+  __shared__ DigitWs dws;
+  const int n = wide_count(a, b);
+  if (j == 0 && tid == 0) a.lens[b] = min(n, a.n_take);
+  if (n <= a.n_take) return;
+  const size_t u = (size_t)b * a.v.nkv + j;
+  const int segs = (n + CHOOSE_SEG - 1) / CHOOSE_SEG;
+  const uint32_t *keys = a.keys + u * a.ld_keys, *cand = a.cand + u * a.ld_cand;
+  uint32_t *cut = a.cut + u * a.ld_cut, *counts = cut + CUT_SEG + 2 * (a.ld_cand / CHOOSE_SEG);
+  for (int i = tid; i < segs; i += CHOOSE_T) s_eq[i] = counts[2 * i + 1];
+  hist[1][tid] = 0;
+  hist[1][tid + CHOOSE_T] = 0;
+  sum_hists(a, u, segs, hist[0]);
+  Digit dg = digit_of(hist[0], a.n_take, true, dws);
+  uint32_t prefix = dg.digit << 21, mask = ~0u << 21, need = a.n_take - dg.above;
+  const bool listed = dg.count <= CHOOSE_LIST;
+  if (wave == 0) scan_segs(s_eq, segs);                // places in the list
+  __syncthreads();
+  // f(key, segment) for every listed key, or every key; a wave per segment
+  auto each = [&](auto f) {
+    for (int sg = wave; sg < segs; sg += CHOOSE_W) {
+      if (listed) {
+        const int l0 = s_eq[sg], l1 = s_eq[sg + 1];
+        for (int i = l0; i < l1; i += 64) f(i + lane < l1 ? list[i + lane] : 0u, i + lane < l1, sg);
+      } else {
+        const int k1 = min(n, (sg + 1) * CHOOSE_SEG);
+#pragma unroll 4
+        for (int i = sg * CHOOSE_SEG; i < k1; i += 64) f(i + lane < k1 ? keys[i + lane] : 0u, i + lane < k1, sg);
+      }
+    }
+  };
+  if (need < dg.count) {
+    if (listed) {
+      for (int sg = wave; sg < segs; sg += CHOOSE_W) {
+        const int l0 = s_eq[sg], l1 = s_eq[sg + 1];
+        for (int i = lane; i < l1 - l0; i += 64) list[l0 + i] = cand[(size_t)sg * CHOOSE_SEG + i];
+      }
+      __syncthreads();
+    }
+#pragma unroll 1
+    for (int p = 1; p < 3; ++p) {
+      const int shift = p == 1 ? 10 : 0;
+      const uint32_t dm = p == 1 ? 2047u : 1023u;
+      uint32_t *hg = hist[p & 1];
+      each([&](uint32_t k, bool in, int) { count_digit(hg, (k >> shift) & dm, in && (k & mask) == prefix); });
+      __syncthreads();
+      dg = digit_of(hg, need, false, dws);
+      prefix |= dg.digit << shift;
+      mask = ~0u << shift;
+      need -= dg.above;
+      if (need == dg.count) break;
+    }
+  }
+  // per segment: its keys above the cut and equal to it
+  const bool refined = mask != ~0u << 21;
+  for (int sg = wave; sg < segs; sg += CHOOSE_W) {
+    uint32_t gt = counts[2 * sg], eq = counts[2 * sg + 1];
+    if (refined) {
+      // (of all keys, or of the listed ones beside those above the first digit)
+      gt = listed ? gt : 0u;
+      eq = 0;
+      const int l0 = listed ? (int)s_eq[sg] : sg * CHOOSE_SEG;
+      const int l1 = listed ? (int)s_eq[sg + 1] : min(n, (sg + 1) * CHOOSE_SEG);
+      for (int i = l0; i < l1; i += 64) {
+        const uint32_t k = i + lane < l1 ? (listed ? list[i + lane] : keys[i + lane]) & mask : 0u;
+        gt += __popcll(__ballot(i + lane < l1 && k > prefix));
+        eq += __popcll(__ballot(i + lane < l1 && k == prefix));
+      }
+    }
+    if (lane == 0) {
+      s_gt[sg] = gt;
+      hist[0][sg] = eq;                                // (s_eq is still read)
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < segs; i += CHOOSE_T) s_eq[i] = hist[0][i];
+  __syncthreads();
+  if (wave == 0) scan_segs(s_gt, segs);
+  if (wave == 1) scan_segs(s_eq, segs);
+  __syncthreads();
+  for (int i = tid; i < segs; i += CHOOSE_T) {
+    cut[CUT_SEG + 2 * i] = s_gt[i] + min(s_eq[i], need);
+    cut[CUT_SEG + 2 * i + 1] = s_eq[i];
+  }
+  if (tid == 0) {
+    cut[0] = prefix;
+    cut[1] = mask;
+    cut[2] = need;
+  }
+}
+__global__ __launch_bounds__(CHOOSE_T) void k_cache_emit(CacheChoose a) {
+  const int sg = blockIdx.x, j = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
+  __shared__ uint32_t wgt[CHOOSE_W], weq[CHOOSE_W];
+  const int n = wide_count(a, b);
+  const size_t u = (size_t)b * a.v.nkv + j;
+  int32_t *out = a.out + u * a.n_take;
+  if (n <= a.n_take) {                                 // all of them, in the segments there are
+    for (int i = sg * CHOOSE_T + tid; i < a.n_take; i += (int)gridDim.x * CHOOSE_T) out[i] = i < n ? i : -1;
+    return;
+  }
+  if (sg * CHOOSE_SEG >= n) return;
+  const int i0 = sg * CHOOSE_SEG + 4 * tid;
+  const uint32_t *cut = a.cut + u * a.ld_cut;
+  const uint32_t prefix = cut[0], mask = cut[1], need = cut[2];
+  const u32x4 k = seg_keys(a.keys + u * a.ld_keys, i0, n) & mask;
+  uint32_t gt = 0, eq = 0;
+  uint64_t mg[4], me[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    mg[e] = __ballot(i0 + e < n && k[e] > prefix);
+    me[e] = __ballot(i0 + e < n && k[e] == prefix);
+    gt += __popcll(mg[e]);
+    eq += __popcll(me[e]);
+  }
+  if (lane == 0) {
+    wgt[wave] = gt;
+    weq[wave] = eq;
+  }
+  __syncthreads();
+  const uint32_t seg_eq = cut[CUT_SEG + 2 * sg + 1];
+  const uint32_t eq0 = seg_eq + sum_before(weq, CHOOSE_W, wave);   // equal ones before this wave
+  const uint64_t below = (1ull << lane) - 1;
+  // the place of this wave's first taken one, of this lane's
+  uint32_t to = cut[CUT_SEG + 2 * sg] + sum_before(wgt, CHOOSE_W, wave) + min(eq0, need) - min(seg_eq, need);
+  uint32_t ahead = eq0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    to += __popcll(mg[e] & below);
+    ahead += __popcll(me[e] & below);
+  }
+  to += min(ahead, need) - min(eq0, need);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool is_eq = (me[e] >> lane) & 1;
+    if (((mg[e] >> lane) & 1) || (is_eq && ahead < need)) out[to++] = i0 + e;
+    ahead += is_eq;
+  }
+}
 static void choose(const CacheChoose &a, int most, hipStream_t s) {
+  if (most > CHOOSE_LDS && a.hists) {
+    const dim3 gs((most + CHOOSE_SEG - 1) / CHOOSE_SEG, a.v.nkv, a.v.kv.n_seq);
+    hipLaunchKernelGGL(k_cache_collect, gs, dim3(CHOOSE_T), 0, s, a);
+    hipLaunchKernelGGL(k_cache_cut, dim3(a.v.nkv, a.v.kv.n_seq), dim3(CHOOSE_T), 0, s, a);
+    hipLaunchKernelGGL(k_cache_emit, gs, dim3(CHOOSE_T), 0, s, a);
+    return;
+  }
   const dim3 g(a.v.nkv, a.v.kv.n_seq), t(CHOOSE_T);
   const size_t lds = (size_t)((most + 255) / 256) * 1024;
   if (most > CHOOSE_LDS) hipLaunchKernelGGL((k_cache_choose<false, false>), g, t, 0, s, a);
@@ -1431,25 +1667,25 @@ static void score_d(const CacheSelect &a, int d, hipStream_t s) {
 void launch_cache_select(bool bf16, const CacheSelect &a, int d, hipStream_t s) {
   if (bf16) score_d<bf16_t>(a, d, s);
   else score_d<float>(a, d, s);
-  choose({a.v, a.keys, a.ld_keys, nullptr, 0, nullptr, 1, a.n_take, 0, 0, a.out, nullptr, a.err}, a.columns, s);
+  choose({a.v, a.keys, a.ld_keys, nullptr, 0, nullptr, 0, nullptr, 0, nullptr, 1, a.n_take, 0, 0, a.out, nullptr, a.err}, a.columns, s);
 }
 
 // ---------------------------------------------------------------- eviction
 // Order keys of the slots of one sequence and KV head (those that do not fit
 // the choice's LDS), and the histogram of their first digits, two to a word.
-__global__ __launch_bounds__(256) void k_cache_keys(CacheEvict a) {
-  constexpr int U = CHOOSE_SEG / 256;
+__global__ __launch_bounds__(CHOOSE_T) void k_cache_keys(CacheEvict a) {
+  constexpr int U = CHOOSE_SEG / CHOOSE_T;
   const int t0 = blockIdx.x * CHOOSE_SEG, j = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-  __shared__ uint32_t hist[1024];
+  __shared__ uint32_t hist[CHOOSE_T];
   const int n = visible_slots(a.v, b, a.err);
   if (t0 >= n) return;
-  for (int i = tid; i < 1024; i += 256) hist[i] = 0;
+  hist[tid] = 0;
   __syncthreads();
   const size_t u = (size_t)b * a.v.nkv + j;
   uint32_t row[U];
 #pragma unroll
   for (int x = 0; x < U; ++x) {
-    const int t = t0 + x * 256 + tid, bi = slot_block(a.v.kv, t);
+    const int t = t0 + x * CHOOSE_T + tid, bi = slot_block(a.v.kv, t);
     row[x] = t < n ? pool_row(a.v, a.v.kv.block_table, b, j, bi, slot_in_block(a.v.kv, t, bi), a.err) : NO_ROW;
   }
   float w[U];
@@ -1457,14 +1693,14 @@ __global__ __launch_bounds__(256) void k_cache_keys(CacheEvict a) {
   for (int x = 0; x < U; ++x) w[x] = a.weights[row[x] == NO_ROW ? 0 : row[x]];
 #pragma unroll
   for (int x = 0; x < U; ++x) {
-    const int t = t0 + x * 256 + tid;
+    const int t = t0 + x * CHOOSE_T + tid;
     if (t >= n) break;
     const uint32_t k = row[x] == NO_ROW ? 0u : t < a.n_first || t >= n - a.n_recent ? KEY_FORCED : choice_key(w[x]);
     a.keys[u * a.ld_keys + t] = k;
     atomicAdd(&hist[k >> 22], (k >> 21) & 1 ? 0x10000u : 1u);   // at most CHOOSE_SEG < 2^16 each
   }
   __syncthreads();
-  for (int i = tid; i < 1024; i += 256) a.hists[u * a.ld_hists + blockIdx.x * 1024 + i] = hist[i];
+  a.hists[u * a.ld_hists + blockIdx.x * 1024 + tid] = hist[tid];
 }
 
 // Keys, values and weight of the kept slots to the new blocks: a lane group
@@ -1509,8 +1745,9 @@ static void copy_d(const CacheEvict &a, int d, hipStream_t s) {
 void launch_cache_evict(bool bf16, const CacheEvict &a, int d, hipStream_t s) {
   if (a.v.max_len > CHOOSE_LDS)
     hipLaunchKernelGGL(k_cache_keys, dim3((a.v.max_len + CHOOSE_SEG - 1) / CHOOSE_SEG, a.v.nkv, a.v.kv.n_seq),
-                       dim3(256), 0, s, a);
-  choose({a.v, a.keys, a.ld_keys, a.hists, a.ld_hists, a.weights, 0, a.n_keep, a.n_first, a.n_recent, a.kept, a.new_lens, a.err},
+                       dim3(CHOOSE_T), 0, s, a);
+  choose({a.v, a.keys, a.ld_keys, a.hists, a.ld_hists, a.cand, a.ld_cand, a.cut, a.ld_cut, a.weights, 0, a.n_keep,
+          a.n_first, a.n_recent, a.kept, a.new_lens, a.err},
          a.v.max_len, s);
   if (bf16) copy_d<bf16_t>(a, d, s);
   else copy_d<float>(a, d, s);

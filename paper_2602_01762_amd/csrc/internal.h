@@ -419,6 +419,8 @@ struct CacheChoose {
   CacheView v;
   const uint32_t *keys; int ld_keys;    // [B, nkv, ld_keys], ld_keys a multiple of 4
   const uint32_t *hists; int ld_hists;  // first digits per CHOOSE_SEG keys, 1024 words each, or NULL
+  uint32_t *cand; int ld_cand;          // (with hists) listed keys, CHOOSE_SEG per segment
+  uint32_t *cut; int ld_cut;            // (with hists)
   const float *weights;                 // slot weights to make the keys from, or NULL
   int per_block;                        // candidates are blocks (else slots)
   int n_take, n_first, n_last;          // (n_first, n_last: with weights)
@@ -431,7 +433,11 @@ struct CacheEvict {
   float *weights;
   int n_keep, n_first, n_recent;
   uint32_t *keys; int ld_keys;          // [B, nkv, ld_keys]
-  uint32_t *hists; int ld_hists;        // [B, nkv, ld_hists] (more than CHOOSE_LDS candidates)
+  // more than CHOOSE_LDS candidates: per (sequence, KV head) the segments'
+  // histograms, listed keys and cuts
+  uint32_t *hists; int ld_hists;
+  uint32_t *cand; int ld_cand;
+  uint32_t *cut; int ld_cut;
   int32_t *kept, *new_lens;             // [B, nkv, n_keep] / [B]
   uint32_t *err;
 };

@@ -363,13 +363,17 @@ constexpr int CACHE_GRAN = 64;      // whole tiles of every attention kernel
 constexpr int CACHE_WAVES = 2048;   // 8 waves on each of 256 CUs, the most that are resident: each
                                     // pays its first lookups once.  32 sequences of 32768 slots:
                                     // 670 us, with 4096 waves 691, with 8192 724
+// A direct call gives each segment to one wave, which needs no join, up to
+// CACHE_DIRECT places.
+constexpr int CACHE_DIRECT = 128;
 struct CachePlan {
   int waves;
-  bool direct;                      // a granule holds a whole segment, so no join is needed
+  bool direct;
 };
 inline CachePlan cache_plan(int units, int span, bool weights) {
+  if (span <= CACHE_DIRECT && !weights) return {units, true};
   const long granules = (long)units * ((span + CACHE_GRAN - 1) / CACHE_GRAN);
-  return {(int)(granules < CACHE_WAVES ? granules : CACHE_WAVES), span <= CACHE_GRAN && !weights};
+  return {(int)(granules < CACHE_WAVES ? granules : CACHE_WAVES), false};
 }
 // row length of the scores kept for the slot weights: whole granules
 inline int cache_score_row(int span) { return (span + CACHE_GRAN - 1) / CACHE_GRAN * CACHE_GRAN; }
@@ -386,14 +390,19 @@ inline int cache_columns_per_wave(long units, int columns, int step, int top) {
   return (int)(steps < 1 ? 1 : steps > most ? most : steps) * step;
 }
 
-// Choice of the best of many candidates by one workgroup: up to CHOOSE_LDS
-// have their keys in LDS; more go through scratch, in segments of CHOOSE_SEG
-// with a histogram of 1024 words each.
+// Choice of the best of many candidates: up to CHOOSE_LDS have their keys in one
+// workgroup's LDS; more slots go through scratch, in segments of CHOOSE_SEG keys
+// with a histogram of 1024 words, a list of the keys at the cut and four words
+// of counts each.
 constexpr int CHOOSE_LDS = 24576, CHOOSE_SEG = 4096;
+constexpr int CHOOSE_MAX_SEGS = ATT_MAX_CHUNKS * ATT_STEP * ATT_MAX_SUB / CHOOSE_SEG;   // of a context's capacity
 inline int choose_key_row(int most) { return (most + 3) / 4 * 4; }
-inline int choose_hist_row(int most) { return most > CHOOSE_LDS ? (most + CHOOSE_SEG - 1) / CHOOSE_SEG * 1024 : 0; }
+inline int choose_segs(int most) { return most > CHOOSE_LDS ? (most + CHOOSE_SEG - 1) / CHOOSE_SEG : 0; }
+inline int choose_hist_row(int most) { return choose_segs(most) * 1024; }
+inline int choose_list_row(int most) { return choose_segs(most) * CHOOSE_SEG; }
+inline int choose_cut_row(int most) { return choose_segs(most) ? 4 + 4 * choose_segs(most) : 0; }
 inline size_t choose_scratch(size_t units, int most) {
-  return units * ((size_t)choose_key_row(most) + choose_hist_row(most)) * 4;
+  return units * ((size_t)choose_key_row(most) + choose_hist_row(most) + choose_list_row(most) + choose_cut_row(most)) * 4;
 }
 
 }  // namespace prism

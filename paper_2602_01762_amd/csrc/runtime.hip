@@ -1694,6 +1694,8 @@ prism_status prism_cache_evict(prism_ctx *c, const prism_cache_eviction *io, voi
   if (io->n_first < 0 || io->n_recent < 0 || (long)io->n_first + io->n_recent > io->n_keep)
     return fail(c, PRISM_ERR_INVALID_ARG, "n_first %d and n_recent %d of n_keep %d", io->n_first, io->n_recent,
                 io->n_keep);
+  if (len > CHOOSE_MAX_SEGS * CHOOSE_SEG)
+    return fail(c, PRISM_ERR_SHAPE, "max_len %d exceeds the choice's %d slots", len, CHOOSE_MAX_SEGS * CHOOSE_SEG);
   const int B = io->kv->batch;
   CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, cache_scratch(c, PRISM_CACHE_EVICT, B, len)));
   CacheEvict a{};
@@ -1707,6 +1709,10 @@ prism_status prism_cache_evict(prism_ctx *c, const prism_cache_eviction *io, voi
   a.ld_keys = choose_key_row(len);
   a.hists = a.keys + (size_t)B * c->nkv * a.ld_keys;
   a.ld_hists = choose_hist_row(len);
+  a.cand = a.hists + (size_t)B * c->nkv * a.ld_hists;
+  a.ld_cand = choose_list_row(len);
+  a.cut = a.cand + (size_t)B * c->nkv * a.ld_cand;
+  a.ld_cut = choose_cut_row(len);
   a.kept = io->d_kept;
   a.new_lens = io->d_new_lens;
   a.err = c->err;

@@ -177,8 +177,8 @@ int main() {
     for (int &n : len) { n = rand() % 3 ? rand() % (top + 1) : 0; span = n > span ? n : span; }
     const bool weights = rand() % 2;
     const CachePlan p = cache_plan(B * nkv, span, weights);
-    if (p.waves < 1 || p.waves > CACHE_WAVES) return 1;
-    if (p.direct && (span > CACHE_GRAN || weights)) return 2;
+    if (p.waves < 1 || p.waves > (p.direct ? B * nkv : CACHE_WAVES)) return 1;
+    if (p.direct && (span > CACHE_DIRECT || weights)) return 2;
     std::vector<long> begin(B), count(B);
     long total = 0;
     for (int b = 0; b < B; ++b) {
