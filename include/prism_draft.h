@@ -414,9 +414,9 @@ prism_status prism_verify_tree(prism_ctx *ctx, int32_t batch, int32_t n_nodes,
  *     negative length taken as 0; both raise PRISM_ERR_CAPACITY in
  *     prism_device_status.
  *   - d_scratch: device memory of the caller's, at least prism_cache_scratch()
- *     bytes, 16-byte aligned, written and read by the one call only (calls on
- *     several streams, and captured graphs that may overlap, each need their
- *     own).
+ *     bytes (0: it may be NULL), 16-byte aligned, written and read by the one
+ *     call only (calls on several streams, and captured graphs that may
+ *     overlap, each need their own).
  *   - A block or slot that the block table or the pool does not hold is
  *     skipped and raises PRISM_ERR_CAPACITY.
  *   - n_pool_blocks * n_kv_heads * kv_block_size < 2^32 - 1. */
@@ -512,8 +512,9 @@ prism_status prism_cache_scratch(prism_ctx *ctx, int32_t call, int32_t batch, in
  * normalised, x / sqrt(mean(x^2) + rms_eps) * gain (where its gain is given),
  * and rotated, (x_i, x_{i + d/2}) by the angle p * rope_theta^(-2i/d), in one
  * pass; one rounding to the context dtype at the end.  Keys and values go to
- * the cache, queries to d_q.  A malformed d_offsets raises
- * PRISM_ERR_INVALID_ARG in prism_device_status and appends nothing. */
+ * the cache, queries to d_q.  A block that receives rows belongs to one
+ * sequence of the call.  A malformed d_offsets raises PRISM_ERR_INVALID_ARG in
+ * prism_device_status and appends nothing. */
 prism_status prism_cache_append(prism_ctx *ctx, const prism_cache_rows *io, void *stream);
 
 /* out = softmax(q K^T / sqrt(d)) V over the visible slots of each sequence
@@ -521,8 +522,8 @@ prism_status prism_cache_append(prism_ctx *ctx, const prism_cache_rows *io, void
  * the cache's length and joined.  A sequence that sees nothing, or whose every
  * score is -inf, gives zeros and a log-sum of -inf.  With d_weights no block
  * may belong to two sequences of the call.  An entry of d_blocks that is out
- * of range or not increasing is skipped and raises PRISM_ERR_INVALID_ARG in
- * prism_device_status. */
+ * of range, or not larger than the entry before it, is skipped and raises
+ * PRISM_ERR_INVALID_ARG in prism_device_status. */
 prism_status prism_cache_attend(prism_ctx *ctx, const prism_cache_attention *io, void *stream);
 
 /* Summaries of cache blocks: d_summary[block, head, 0 / 1, :] = the minimum /

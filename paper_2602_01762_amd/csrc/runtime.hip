@@ -1507,12 +1507,14 @@ static size_t cache_scratch(const prism_ctx *c, int call, int B, int span) {
   if (call == PRISM_CACHE_EVICT) return choose_scratch((size_t)B * c->nkv, span);
   const bool weights = call == PRISM_CACHE_ATTEND_WEIGHTS;
   const CachePlan p = cache_plan(B * c->nkv, span, weights);
+  if (p.direct) return 0;
   const size_t parts = (size_t)(p.waves + B * c->nkv) * (c->nq / c->nkv);
   size_t n = ((parts * 4 + pad) & ~pad) * 2 + ((parts * c->d * 4 + pad) & ~pad);
   if (weights) n += (size_t)B * c->nq * cache_score_row(span) * 4;
   return n;
 }
 static prism_status check_scratch(prism_ctx *c, const void *p, uint64_t bytes, size_t need) {
+  if (!need) return PRISM_OK;
   if (!p || ((uintptr_t)p & 15)) return fail(c, PRISM_ERR_INVALID_ARG, "d_scratch is NULL or not 16-byte aligned");
   if (bytes < need)
     return fail(c, PRISM_ERR_INVALID_ARG, "scratch of %llu bytes, %zu needed", (unsigned long long)bytes, need);

@@ -288,7 +288,7 @@ class Drafter:
             if len(self._scratch_bytes) >= 1024:      # callers that pass a new bound at every step
                 self._scratch_bytes.clear()
             self._scratch_bytes[key] = n
-        return n, like.new_empty(-(-n // like.element_size()))
+        return n, like.new_empty(-(-n // like.element_size())) if n else None
 
     def cache(self, lens, k_pool, v_pool, block_table) -> B.prism_batch:
         """The sequences of a cache call: lens [B] int32 slots held, pools
@@ -369,7 +369,7 @@ class Drafter:
         sums = torch.empty(shape[:2], dtype=torch.float32, device=self.device) if lse else None
         io.d_lse = None if sums is None else sums.data_ptr()
         io.scratch_bytes, scratch = self._scratch(call, nb, span, q)
-        io.d_scratch = scratch.data_ptr()
+        io.d_scratch = None if scratch is None else scratch.data_ptr()
         B.prism_cache_attend(self.ctx, io, self._stream())
         return {"out": out, "lse": sums}
 

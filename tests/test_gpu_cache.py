@@ -309,6 +309,21 @@ def test_attend_long_sequences(heads):
     c.close()
 
 
+@pytest.mark.parametrize("top", [1, 64, 65, 128, 129, 192])
+@pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (8, 8, 128, "bf16"), (4, 1, 256, "bf16"), (7, 1, 32, "bf16"),
+                                   (8, 1, 128, "f32"), (3, 3, 64, "f32")])
+def test_attend_short_sequences(heads, top):
+    """Around the bound up to which a segment is one wave's."""
+    lens = [0, 1, top // 2, top, max(1, top - 1)]
+    c = Cache(*heads, 16, lens, 13)
+    q = c.normal((c.B, c.nq, c.d), 2.0)
+    check_attend(c, q, c.dr.cache_attend(c.kv(), q, max_len=top, lse=True))
+    w = c.weights()
+    w0 = w.clone()
+    check_attend(c, q, c.dr.cache_attend(c.kv(), q, max_len=top, weights=w, lse=True), w=w, w0=w0)
+    c.close()
+
+
 def test_attend_sixty_four_sequences():
     lens = [(b * 131) % 700 for b in range(64)]
     c = Cache(8, 2, 64, "bf16", 16, lens, 44)
@@ -779,6 +794,8 @@ def test_refusals():
     io.kv = ctypes.addressof(kv)
     out, scratch = torch.empty_like(q), torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
     io.d_q, io.d_out, io.d_scratch, io.scratch_bytes = B.ptr(q), B.ptr(out), B.ptr(scratch), 1 << 20
+    io.max_len = 0
+    io.d_weights = B.ptr(w)                                                    # a call that needs scratch
     for field, value in (("scratch_bytes", 16), ("d_scratch", 0), ("d_q", 0), ("d_q", B.ptr(q) + 2),
                          ("d_out", B.ptr(out) + 8), ("kv", None)):
         keep = getattr(io, field)
@@ -791,6 +808,11 @@ def test_refusals():
         B.prism_cache_scratch(c.dr.ctx, 4, 1, 0)
     with pytest.raises(PrismError):
         B.prism_cache_scratch(c.dr.ctx, 0, 3, 0)
+    more = c.dr.cache(torch.zeros(3, dtype=torch.int32, device=DEV), c.k, c.v,
+                      torch.zeros((3, 4), dtype=torch.int32, device=DEV))
+    with pytest.raises(PrismError) as e:                                       # 3 sequences, max_batch 2
+        c.dr.cache_summarize(more, s)
+    assert e.value.status == -1
     big = c.dr.cache(c.lens, c.k, c.v, c.table)
     big.n_pool_blocks = 1 << 27                                                # 2^32 rows
     with pytest.raises(PrismError) as e:
