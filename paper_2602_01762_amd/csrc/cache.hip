@@ -106,7 +106,7 @@ __device__ __forceinline__ void store8f(T *p, const float (&x)[8]) {
 // their rotation partners d/2 + 8i ...  The angles of a row are the same for
 // all its heads: d / 2 threads of the workgroup compute them once.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_cache_append(CacheAppend a) {
+__global__ __launch_bounds__(512) void k_cache_append(CacheAppend a) {
   constexpr int LPH = D / 16, HPW = 64 / LPH;      // lanes per head, heads per wave
   const int r = blockIdx.x, tid = threadIdx.x, wave = wave_id(), lane = tid & 63;
   __shared__ float cs[D / 2], sn[D / 2];
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheAppend a) {
 template <typename T>
 static void append_d(const CacheAppend &a, int d, hipStream_t s) {
   const int hpw = 64 / (d / 16), nh = a.nq + 2 * a.v.nkv;
-  const int nw = min(4, (nh + hpw - 1) / hpw);
+  const int nw = min(8, (nh + hpw - 1) / hpw);
   const dim3 g(a.rows, (nh + nw * hpw - 1) / (nw * hpw)), t(64 * nw);
   if (d == 32) hipLaunchKernelGGL((k_cache_append<T, 32>), g, t, 0, s, a);
   else if (d == 64) hipLaunchKernelGGL((k_cache_append<T, 64>), g, t, 0, s, a);
@@ -1024,12 +1024,12 @@ __global__ __launch_bounds__(256, G > 4 ? 2 : 3) void k_cache_score(CacheSelect 
   constexpr int SH = D == 32 ? 2 : D == 64 ? 3 : D == 128 ? 4 : 5;   // log2 LPR
   // with fewer lanes than heads (d = 32, 8 heads) two rounds of 4
   constexpr int N = G > LPR ? LPR : G;
-  const int lane = threadIdx.x & 63, j = blockIdx.y, b = blockIdx.z, bs = a.v.kv.bs;
+  const int lane = threadIdx.x & 63, j = blockIdx.y * (blockDim.x >> 6) + wave_id(), b = blockIdx.z, bs = a.v.kv.bs;
   const int grp = lane / LPR, li = lane % LPR;
   const int n = visible_slots(a.v, b, a.err);
   const int nblk = (int)(((long)n + bs - 1) / bs);
-  const int c0 = (blockIdx.x * 4 + wave_id()) * a.per, c1 = min(nblk, c0 + a.per);
-  if (c0 >= c1) return;                             // whole waves
+  const int c0 = blockIdx.x * a.per, c1 = min(nblk, c0 + a.per);
+  if (c0 >= c1 || j >= a.v.nkv) return;             // whole waves
   // lane i < a.per: pool block and KV head of column c0 + i
   const uint32_t blks = lane < c1 - c0 ? pool_block(a.v, a.v.kv.block_table, b, j, c0 + lane, a.err) : NO_ROW;
   u32x4 mn[DEPTH][P], mx[DEPTH][P];
@@ -1651,11 +1651,14 @@ static void choose(const CacheChoose &a, int most, hipStream_t s) {
 
 template <typename T, int D>
 static void score_g(const CacheSelect &a, hipStream_t s) {
-  const dim3 g((a.columns + 4 * a.per - 1) / (4 * a.per), a.v.nkv, a.v.kv.n_seq);
-  if (a.g == 1) hipLaunchKernelGGL((k_cache_score<T, D, 1>), g, dim3(256), 0, s, a);
-  else if (a.g == 2) hipLaunchKernelGGL((k_cache_score<T, D, 2>), g, dim3(256), 0, s, a);
-  else if (a.g <= 4) hipLaunchKernelGGL((k_cache_score<T, D, 4>), g, dim3(256), 0, s, a);
-  else if constexpr (D < 256) hipLaunchKernelGGL((k_cache_score<T, D, 8>), g, dim3(256), 0, s, a);   // g * d <= 1024
+  // the waves of a workgroup take different heads of the same blocks, whose
+  // summaries lie next to each other
+  const int nw = min(4, a.v.nkv);
+  const dim3 g((a.columns + a.per - 1) / a.per, (a.v.nkv + nw - 1) / nw, a.v.kv.n_seq), t(64 * nw);
+  if (a.g == 1) hipLaunchKernelGGL((k_cache_score<T, D, 1>), g, t, 0, s, a);
+  else if (a.g == 2) hipLaunchKernelGGL((k_cache_score<T, D, 2>), g, t, 0, s, a);
+  else if (a.g <= 4) hipLaunchKernelGGL((k_cache_score<T, D, 4>), g, t, 0, s, a);
+  else if constexpr (D < 256) hipLaunchKernelGGL((k_cache_score<T, D, 8>), g, t, 0, s, a);   // g * d <= 1024
 }
 template <typename T>
 static void score_d(const CacheSelect &a, int d, hipStream_t s) {
