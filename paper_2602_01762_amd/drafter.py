@@ -94,7 +94,7 @@ class Drafter:
         b.d_v_pool = B.ptr(inp.v_pool)
         b.d_block_table = B.ptr(inp.block_table)
         b.n_pool_blocks = int(inp.k_pool.shape[0])
-        return b
+        return self._sizes(b)
 
     # calls --------------------------------------------------------------------
     def chain_buffers(self, nb: int, K: int, logits=False, hidden=False):
@@ -304,7 +304,13 @@ class Drafter:
         kv.d_block_table = self._expect(block_table, "block_table", (nb, self._columns), torch.int32)
         kv.n_pool_blocks = n
         kv.tensors = (lens, k_pool, v_pool, block_table)
-        kv.nb, kv.slots, kv.summary = nb, pool[:3], (n, self._nkv, 2, self._d)
+        return self._sizes(kv)
+
+    def _sizes(self, kv):
+        """What the cache calls compare a batch's tensors with (the batches of
+        drafting calls, batch(), can be passed to them too)."""
+        n = kv.n_pool_blocks
+        kv.nb, kv.slots, kv.summary = kv.batch, (n, self._nkv, self._bs), (n, self._nkv, 2, self._d)
         return kv
 
     def cache_append(self, kv, qkv, q_gain=None, k_gain=None, offsets=None, positions=None,

@@ -699,6 +699,71 @@ def test_drafting_goes_on_over_an_evicted_cache():
     dr.close()
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (8, 1, 128, "f32")])
+def test_a_batch_without_any_slot(heads):
+    c = Cache(*heads, 16, [0, 0, 0], 4, spare=6)
+    q, w = c.normal((3, c.nq, c.d)), c.weights()
+    kv, w0, k0 = c.kv(), w.clone(), c.k.clone()
+    s = torch.full((c.k.shape[0], c.nkv, 2, c.d), 3.0, dtype=c.dt, device=DEV)
+    c.dr.cache_summarize(kv, s)
+    c.dr.cache_summarize(kv, s, span=5)
+    assert float((s - 3).abs().max()) == 0.0
+    blocks = c.dr.cache_select(kv, q, s, 2, 1, 1)
+    assert (blocks == -1).all()
+    for kw in (dict(), dict(weights=w), dict(blocks=blocks), dict(blocks=blocks, weights=w), dict(max_len=1)):
+        r = c.dr.cache_attend(kv, q, lse=True, out=torch.full_like(q, 5.0), **kw)
+        assert float(r["out"].float().abs().max()) == 0.0 and torch.isneginf(r["lse"]).all()
+    new = torch.full((3, 4), -1, dtype=torch.int32, device=DEV)
+    new[:, :2] = torch.tensor(c.free[:6].reshape(3, 2), device=DEV)
+    r = c.dr.cache_evict(kv, new, w, 20, 1, 2)
+    assert r["lens"].tolist() == [0, 0, 0] and (r["kept"] == -1).all()
+    assert torch.equal(w, w0) and torch.equal(c.k.view(torch.uint8), k0.view(torch.uint8))
+    c.close()
+
+
+def test_blocks_that_the_pool_does_not_hold():
+    """Summaries and scores skip them and flag; every other block is right."""
+    c = Cache(8, 2, 64, "bf16", 16, [160, 160], 10)
+    q = c.normal((2, 8, 64))
+    good = c.dr.cache_summarize(c.kv(), c.dr.summary_buffer(c.kv()))
+    keep = c.table.clone()
+    for bad in (-1, c.k.shape[0], 2 ** 31 - 1):
+        c.table.copy_(keep)
+        c.table[0, 4] = bad
+        s = torch.zeros_like(good)
+        c.dr.cache_summarize(c.kv(), s)
+        assert c.dr.device_status() == -7
+        want = good.clone()
+        want[int(keep[0, 4])] = 0
+        assert torch.equal(s.view(torch.int16), want.view(torch.int16))
+        blocks = c.dr.cache_select(c.kv(), q, good, 9)
+        assert c.dr.device_status() == -7
+        assert blocks[0].tolist() == [[0, 1, 2, 3, 5, 6, 7, 8, 9]] * 2       # ranks last
+    c.table.copy_(keep)
+    c.lens[0] = 400                                          # past the capacity
+    for call in (lambda: c.dr.cache_summarize(c.kv(), s), lambda: c.dr.cache_select(c.kv(), q, good, 3),
+                 lambda: c.dr.cache_select(c.kv(), q, good, 3, max_len=160)):
+        call()
+        assert c.dr.device_status() == -7
+    c.close()
+
+
+def test_a_drafting_batch_serves_the_cache_calls():
+    from paper_2602_01762_amd import Drafter
+    from synth import SMALL_BF16_CHAIN, make_inputs
+    cfg = SMALL_BF16_CHAIN.with_(batch=2, ctx_range=(20, 33), n_steps=2)
+    inp = make_inputs(cfg, DEV)
+    dr = Drafter(cfg)
+    q = torch.randn((2, cfg.n_q_heads, cfg.head_dim), device=DEV).to(torch.bfloat16)
+    w = torch.zeros(inp.k_pool.shape[:3], device=DEV)
+    a = dr.cache_attend(dr.batch(inp), q, weights=w)["out"]
+    b = dr.cache_attend(dr.cache(inp.ctx_lens, inp.k_pool, inp.v_pool, inp.block_table), q)["out"]
+    assert float((a.float() - b.float()).abs().max()) <= 2.0 ** -7 * float(b.float().abs().max())
+    assert abs(float(w.sum()) - 2 * cfg.n_q_heads) < 1e-3
+    assert dr.device_status() == 0
+    dr.close()
+
+
 def test_calls_repeat_bit_for_bit_and_replay_in_a_graph():
     c = Cache(32, 8, 128, "bf16", 16, [1, 700, 333, 64], 48, spare=4 * 8)
     q = c.normal((4, 32, 128), 2.0)
