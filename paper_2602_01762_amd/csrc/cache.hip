@@ -323,15 +323,18 @@ __global__ __launch_bounds__(64, G > 4 ? 1 : 2) void k_cache_attend(CacheAttend 
       m[h] = -INFINITY;
       l[h] = 0.f;
     }
-    float k[NI][8], v[NI][8];
+    u32x4 k[NI][2], v[NI][2];
     uint32_t rows = NO_ROW;
     auto load = [&]() {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const uint32_t r = __shfl(rows, i * RPI + grp, 64);
         const size_t at = (size_t)(r == NO_ROW ? 0 : r) * D + 8 * li;   // a masked place reads row 0
-        load8f<float>((const float *)a.v.kv.k_pool + at, k[i]);
-        load8f<float>((const float *)a.v.kv.v_pool + at, v[i]);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          k[i][x] = stream16((const u32x4 *)((const float *)a.v.kv.k_pool + at) + x);
+          v[i][x] = stream16((const u32x4 *)((const float *)a.v.kv.v_pool + at) + x);
+        }
       }
     };
     int id1, pv1, b1;
@@ -348,12 +351,12 @@ __global__ __launch_bounds__(64, G > 4 ? 1 : 2) void k_cache_attend(CacheAttend 
       const uint64_t mask = __ballot(rows != NO_ROW);
       float kc[NI][8], vc[NI][8];
 #pragma unroll
-      for (int i = 0; i < NI; ++i)
+      for (int i = 0; i < NI; ++i) {
+        unpack8<float>(k[i], kc[i]);
+        unpack8<float>(v[i], vc[i]);
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          kc[i][x] = k[i][x];
-          vc[i][x] = ((mask >> (i * RPI + grp)) & 1) ? v[i][x] : 0.f;
-        }
+        for (int x = 0; x < 8; ++x) vc[i][x] = ((mask >> (i * RPI + grp)) & 1) ? vc[i][x] : 0.f;
+      }
       if (t + TS < sg.p1) {
         rows = lane < TS ? lk.row(t + TS + lane, id1, pv1, b1) : NO_ROW;
         lk.column(t + 2 * TS + lane, id1, pv1);
