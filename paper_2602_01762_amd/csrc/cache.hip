@@ -297,145 +297,23 @@ struct Lookup {
   }
 };
 
-// fp32 caches: tiles of 4 rows per lane group of d / 8 lanes; the group keeps
-// its own softmax state, and the groups of the wave are merged at the end of a
-// segment.  The next tile's rows are in flight while one is computed.
-// G: query heads per KV head, rounded up to a power of two.
-template <int D, int G>
-__global__ __launch_bounds__(64, G > 4 ? 1 : 2) void k_cache_attend(CacheAttend a) {
-  constexpr int LPR = D / 8, RPI = 64 / LPR, NI = 4, TS = NI * RPI;
-  constexpr int SH = D == 32 ? 2 : D == 64 ? 3 : D == 128 ? 4 : 5;   // log2 LPR
-  const int lane = threadIdx.x, grp = lane / LPR, li = lane % LPR, g = a.g;
-  const Walk wk = walk_of(a);
-  int u = blockIdx.x * wk.per;
-  const int last = min(wk.total, u + wk.per);
-  while (u < last) {
-    const Segment sg = segment_at(a, wk, u, last);
-    u += sg.granules;
-    const Lookup lk(a, sg);
-    const size_t h0 = (size_t)sg.b * a.nq + sg.j * g;
-    float q[G][8], o[G][8], m[G], l[G];
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-      if (h < g) load8f<float>((const float *)a.q + (h0 + h) * D + 8 * li, q[h]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[h][i] = 0.f;
-      m[h] = -INFINITY;
-      l[h] = 0.f;
-    }
-    u32x4 k[NI][2], v[NI][2];
-    uint32_t rows = NO_ROW;
-    auto load = [&]() {
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const uint32_t r = __shfl(rows, i * RPI + grp, 64);
-        const size_t at = (size_t)(r == NO_ROW ? 0 : r) * D + 8 * li;   // a masked place reads row 0
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          k[i][x] = stream16((const u32x4 *)((const float *)a.v.kv.k_pool + at) + x);
-          v[i][x] = stream16((const u32x4 *)((const float *)a.v.kv.v_pool + at) + x);
-        }
-      }
-    };
-    int id1, pv1, b1;
-    if (sg.p0 < sg.p1) {
-      int id0, pv0;
-      lk.column(sg.p0 + lane, id0, pv0);
-      lk.column(sg.p0 + TS + lane, id1, pv1);
-      const int b0 = lk.block(id0);
-      b1 = lk.block(id1);
-      rows = lane < TS ? lk.row(sg.p0 + lane, id0, pv0, b0) : NO_ROW;
-      load();
-    }
-    for (int t = sg.p0; t < sg.p1; t += TS) {
-      const uint64_t mask = __ballot(rows != NO_ROW);
-      float kc[NI][8], vc[NI][8];
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        unpack8<float>(k[i], kc[i]);
-        unpack8<float>(v[i], vc[i]);
-#pragma unroll
-        for (int x = 0; x < 8; ++x) vc[i][x] = ((mask >> (i * RPI + grp)) & 1) ? vc[i][x] : 0.f;
-      }
-      if (t + TS < sg.p1) {
-        rows = lane < TS ? lk.row(t + TS + lane, id1, pv1, b1) : NO_ROW;
-        lk.column(t + 2 * TS + lane, id1, pv1);
-        b1 = lk.block(id1);
-        load();
-      }
-#pragma unroll
-      for (int h = 0; h < G; ++h)
-        if (h < g) {
-          float s[NI], mx = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < NI; ++i) {
-            s[i] = 0.f;
-#pragma unroll
-            for (int x = 0; x < 8; ++x) s[i] += q[h][x] * kc[i][x];
-            s[i] = group_sum(s[i], SH) * a.scale;
-            if (!((mask >> (i * RPI + grp)) & 1)) s[i] = -INFINITY;
-            if (a.scores && li == 0) a.scores[score_at(a, sg.b, sg.j, h, t + i * RPI + grp)] = s[i];
-            mx = fmaxf(mx, s[i]);
-          }
-          const float mn = fmaxf(m[h], mx);
-          // nothing but -inf so far: subtract 0, so that every p is 0 (a NaN
-          // score still makes its p, and with it the sum, NaN)
-          const float ms = mn == -INFINITY ? 0.f : mn, al = exp2f(m[h] - ms);
-          m[h] = mn;
-          l[h] *= al;
-#pragma unroll
-          for (int x = 0; x < 8; ++x) o[h][x] *= al;
-#pragma unroll
-          for (int i = 0; i < NI; ++i) {
-            const float p = exp2f(s[i] - ms);
-            l[h] += p;
-#pragma unroll
-            for (int x = 0; x < 8; ++x) o[h][x] += p * vc[i][x];
-          }
-        }
-    }
-    const size_t part = (size_t)(blockIdx.x + sg.b * a.v.nkv + sg.j) * g;
-#pragma unroll
-    for (int h = 0; h < G; ++h)
-      if (h < g) {
-        float M = m[h];
-#pragma unroll
-        for (int x = LPR; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x, 64));
-        const float w = exp2f(m[h] - (M == -INFINITY ? 0.f : M));
-        const float ls = stride_sum(l[h] * w, LPR);
-#pragma unroll
-        for (int x = 0; x < 8; ++x) o[h][x] = stride_sum(o[h][x] * w, LPR);
-        if (a.direct) {
-#pragma unroll
-          for (int x = 0; x < 8; ++x) o[h][x] = ls == 0.f ? 0.f : o[h][x] / ls;
-          if (grp == 0) store8f<float>((float *)a.out + (h0 + h) * D + 8 * li, o[h]);
-          if (a.lse && lane == 0) a.lse[h0 + h] = ls == 0.f ? -INFINITY : (M + log2f(ls)) * LN2;
-        } else {
-          if (grp == 0) store8f<float>(a.po + (part + h) * D + 8 * li, o[h]);
-          if (lane == 0) {
-            a.pm[part + h] = M;
-            a.pl[part + h] = ls;
-          }
-        }
-      }
-  }
-}
-
-// The same on the matrix cores, for bf16 caches.  A wave takes tiles of TS
-// places.  K and V rows are loaded whole, D / 8 lanes per row, so that every
-// cache line is requested once, into registers, and pass through LDS into
-// operand order: the scores are MFMAs of 16 slots x 16 heads (K rows as A, the
-// queries as B), the outputs MFMAs of 16 dims x 16 heads (V transposed by the
-// LDS read as A, the probabilities, straight from the score layout, as B).
+// A wave takes tiles of TS places.  K and V rows are loaded whole, 16 bytes per
+// lane, so that every cache line is requested once, into registers, and pass
+// through LDS into operand order: the scores are MFMAs of 16 slots x 16 heads
+// (K rows as A, the queries as B), the outputs MFMAs of 16 dims x 16 heads (V
+// transposed by the LDS read as A, the probabilities, straight from the score
+// layout, as B).  fp32 caches use the fp32 MFMAs, which take the same 16-byte
+// pieces four values at a time (on the vector units 8 heads per KV head were
+// bound by arithmetic at 3.2 TB/s).
 // Each lane then holds one head's softmax state and output, so nothing is
 // exchanged but the maximum and the sum over the four lane rows.  The next
 // tile's rows are in flight while one is computed, and the block-table
 // entries of the one after it.
 //   In LDS the 16-byte pieces of row s are permuted by s, so that both the
-// A-operand reads (16 rows, one piece) and the transposing reads (4 rows, half
+// A-operand reads (16 rows, one piece) and the transposing reads (4 rows, the
 // pieces of 16 dims) spread over all banks.
-//   Probabilities are multiplied as a pair of bf16 (value and remainder,
-// 2^-16), so that the output keeps the accuracy of its own rounding.
+//   In bf16 caches probabilities are multiplied as a pair of bf16 (value and
+// remainder, 2^-16), so that the output keeps the accuracy of its own rounding.
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -443,12 +321,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-template <int D>
-struct MfmaTile {
-  static constexpr int TS = D >= 256 ? 16 : D >= 128 ? 32 : 64;   // places per tile
-  static constexpr int LPR = D / 8, RPI = 64 / LPR, NI = TS / RPI;
+template <typename T, int D>
+struct Tile {
+  static constexpr int LPR = D * (int)sizeof(T) / 16, RPI = 64 / LPR;   // lanes (pieces) per row, rows per load
+  static constexpr int TS = LPR >= 32 ? 16 : LPR >= 16 ? 32 : 64;       // places per tile
+  static constexpr int NI = TS / RPI;
   __device__ static int swz(int s) {
-    return D >= 128 ? s & 15 : D == 64 ? (s >> 1) & 7 : (s >> 2) & 3;
+    return LPR >= 16 ? s & 15 : LPR == 8 ? (s >> 1) & 7 : (s >> 2) & 3;
   }
   // byte of 16-byte piece c of row s
   __device__ static int at(int s, int c) { return (s * LPR + (c ^ swz(s))) * 16; }
@@ -459,12 +338,12 @@ struct MfmaTile {
 // with the loads and retire in order with them, so each one delays the wait
 // for a tile's rows: 16 sequences of up to 16384 slots took 109 us with a store
 // per tile, 93 without any, 105 so.
-template <int D, bool KEEP>
-__global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
-  using M = MfmaTile<D>;
-  constexpr int TS = M::TS, LPR = M::LPR, RPI = M::RPI, NI = M::NI;
-  constexpr int NS = TS / 16, NK = D / 32, ND = D / 16;
-  __shared__ __attribute__((aligned(16))) char s_k[TS * D * 2], s_v[TS * D * 2];
+template <typename T, int D, bool KEEP>
+__global__ __launch_bounds__(64, D * sizeof(T) > 512 ? 1 : 2) void k_cache_attend(CacheAttend a) {
+  using M = Tile<T, D>;
+  constexpr int TS = M::TS, LPR = M::LPR, RPI = M::RPI, NI = M::NI, E = 16 / sizeof(T);   // E: values of a piece
+  constexpr int NS = TS / 16, NK = LPR / 4, ND = D / 16;
+  __shared__ __attribute__((aligned(16))) char s_k[TS * LPR * 16], s_v[TS * LPR * 16];
   constexpr int KEPT = 1024;                                // scores in LDS
   __shared__ __attribute__((aligned(16))) float s_s[KEEP ? KEPT : 4];
   const int lane = threadIdx.x, g = a.g;
@@ -484,9 +363,9 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const uint32_t r = __shfl(row, i * RPI + grp, 64);
-        const size_t at = (size_t)(r == NO_ROW ? 0 : r) * D + 8 * li;   // a masked place reads row 0
-        kr[i] = stream16((const bf16_t *)kv.k_pool + at);
-        vr[i] = stream16((const bf16_t *)kv.v_pool + at);
+        const size_t at = (size_t)(r == NO_ROW ? 0 : r) * D + E * li;   // a masked place reads row 0
+        kr[i] = stream16((const T *)kv.k_pool + at);
+        vr[i] = stream16((const T *)kv.v_pool + at);
       }
     };
     float m_run = -INFINITY, l_run = 0.f;
@@ -496,7 +375,7 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
     u32x4 qf[NK];
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk)
-      qf[kk] = col < g ? *(const u32x4 *)((const bf16_t *)a.q + hi * D + 32 * kk + 8 * q4) : u32x4{0, 0, 0, 0};
+      qf[kk] = col < g ? *(const u32x4 *)((const T *)a.q + hi * D + (4 * kk + q4) * E) : u32x4{0, 0, 0, 0};
     int id1, pv1, b1, id2, pv2;
     uint32_t row = NO_ROW;
     int kept = sg.p0;                                       // first place whose scores are in LDS
@@ -551,7 +430,7 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
         sc[st] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk)
-          sc[st] = Ty<bf16_t>::mma(*(const u32x4 *)(s_k + M::at(16 * st + col, 4 * kk + q4)), qf[kk], sc[st]);
+          sc[st] = Ty<T>::mma(*(const u32x4 *)(s_k + M::at(16 * st + col, 4 * kk + q4)), qf[kk], sc[st]);
       }
       float mx = -INFINITY;
 #pragma unroll
@@ -590,26 +469,33 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) o[dt] *= al;
       }
-      s16x4 ph[NS], pl[NS];
-#pragma unroll
-      for (int st = 0; st < NS; ++st) {
-        const uint32_t h0 = pack_bf16(sc[st][0], sc[st][1]), h1 = pack_bf16(sc[st][2], sc[st][3]);
-        const uint32_t l0 = pack_bf16(sc[st][0] - __uint_as_float(h0 << 16), sc[st][1] - __uint_as_float(h0 & 0xffff0000u));
-        const uint32_t l1 = pack_bf16(sc[st][2] - __uint_as_float(h1 << 16), sc[st][3] - __uint_as_float(h1 & 0xffff0000u));
-        ph[st] = __builtin_bit_cast(s16x4, uint2{h0, h1});
-        pl[st] = __builtin_bit_cast(s16x4, uint2{l0, l1});
-      }
       // O[dim 16 dt + 4 q4 + i][head col]
 #pragma unroll
-      for (int st = 0; st < NS; ++st)
+      for (int st = 0; st < NS; ++st) {
+        if constexpr (sizeof(T) == 2) {
+          const uint32_t h0 = pack_bf16(sc[st][0], sc[st][1]), h1 = pack_bf16(sc[st][2], sc[st][3]);
+          const uint32_t l0 = pack_bf16(sc[st][0] - __uint_as_float(h0 << 16), sc[st][1] - __uint_as_float(h0 & 0xffff0000u));
+          const uint32_t l1 = pack_bf16(sc[st][2] - __uint_as_float(h1 << 16), sc[st][3] - __uint_as_float(h1 & 0xffff0000u));
+          const s16x4 ph = __builtin_bit_cast(s16x4, uint2{h0, h1}), pl = __builtin_bit_cast(s16x4, uint2{l0, l1});
+          const int row = 16 * st + 4 * q4 + (col >> 2);
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
-          const int r = 16 * st + 4 * q4 + (col >> 2);
-          const char *pv = s_v + M::at(r, 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
-          const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv);
-          o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, ph[st], o[dt], 0, 0, 0);
-          o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pl[st], o[dt], 0, 0, 0);
+          for (int dt = 0; dt < ND; ++dt) {
+            const char *pv = s_v + M::at(row, 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
+            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv);
+            o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, ph, o[dt], 0, 0, 0);
+            o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pl, o[dt], 0, 0, 0);
+          }
+        } else {
+          // step i: slot 4 q4 + i of each lane row
+#pragma unroll
+          for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const char *pv = s_v + M::at(16 * st + 4 * q4 + i, 4 * dt + (col >> 2)) + 4 * (col & 3);
+              o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(*(const float *)pv, sc[st][i], o[dt], 0, 0, 0);
+            }
         }
+      }
       wave_lds_sync();                                 // reads done before the next tile's writes
     }
     if constexpr (KEEP)
@@ -618,9 +504,10 @@ __global__ __launch_bounds__(64, 2) void k_cache_attend_mfma(CacheAttend a) {
     if (a.direct) {
       const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt)
-        *(uint2 *)((bf16_t *)a.out + hi * D + 16 * dt + 4 * q4) =
-            uint2{f2bf(o[dt][0] * inv) | (f2bf(o[dt][1] * inv) << 16), f2bf(o[dt][2] * inv) | (f2bf(o[dt][3] * inv) << 16)};
+      for (int dt = 0; dt < ND; ++dt) {
+        const float y[4] = {o[dt][0] * inv, o[dt][1] * inv, o[dt][2] * inv, o[dt][3] * inv};
+        store_n<T, 4>((T *)a.out + hi * D + 16 * dt + 4 * q4, y);
+      }
       if (a.lse && q4 == 0) a.lse[hi] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
       continue;
     }
@@ -713,9 +600,8 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
     if (grp == 0) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = l == 0.f ? 0.f : o[i] / l;
-      T *out = (T *)a.out + hi * D + 4 * x;
-      if constexpr (sizeof(T) == 2) *(uint2 *)out = uint2{f2bf(o[0]) | (f2bf(o[1]) << 16), f2bf(o[2]) | (f2bf(o[3]) << 16)};
-      else *(f32x4 *)out = o;
+      const float y[4] = {o[0], o[1], o[2], o[3]};
+      store_n<T, 4>((T *)a.out + hi * D + 4 * x, y);
     }
     if (t == 0 && a.lse) a.lse[hi] = l == 0.f ? -INFINITY : (M + log2f(l)) * LN2;
     return;
@@ -768,43 +654,23 @@ static void join_d(const CacheAttend &a, hipStream_t s) {
   if (few) hipLaunchKernelGGL((k_cache_join<T, D, 64>), g, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((k_cache_join<T, D, 256>), g, dim3(256), 0, s, a);
 }
+template <typename T, int D>
+static void attend_d(const CacheAttend &a, hipStream_t s) {
+  const dim3 g(a.waves), t(64);
+  if (a.weights) hipLaunchKernelGGL((k_cache_attend<T, D, true>), g, t, 0, s, a);
+  else hipLaunchKernelGGL((k_cache_attend<T, D, false>), g, t, 0, s, a);
+  if (!a.direct) join_d<T, D>(a, s);
+}
 template <typename T>
-static void join(const CacheAttend &a, hipStream_t s) {
-  if (a.d == 32) join_d<T, 32>(a, s);
-  else if (a.d == 64) join_d<T, 64>(a, s);
-  else if (a.d == 128) join_d<T, 128>(a, s);
-  else join_d<T, 256>(a, s);
-}
-
-template <int D>
-static void attend_f32(const CacheAttend &a, hipStream_t s) {
-  const dim3 g(a.waves), t(64);
-  if (a.g == 1) hipLaunchKernelGGL((k_cache_attend<D, 1>), g, t, 0, s, a);
-  else if (a.g == 2) hipLaunchKernelGGL((k_cache_attend<D, 2>), g, t, 0, s, a);
-  else if (a.g <= 4) hipLaunchKernelGGL((k_cache_attend<D, 4>), g, t, 0, s, a);
-  else if constexpr (D < 256) hipLaunchKernelGGL((k_cache_attend<D, 8>), g, t, 0, s, a);   // g * d <= 1024
-}
-template <int D>
-static void attend_bf16(const CacheAttend &a, hipStream_t s) {
-  const dim3 g(a.waves), t(64);
-  if (a.weights) hipLaunchKernelGGL((k_cache_attend_mfma<D, true>), g, t, 0, s, a);
-  else hipLaunchKernelGGL((k_cache_attend_mfma<D, false>), g, t, 0, s, a);
+static void attend_t(const CacheAttend &a, hipStream_t s) {
+  if (a.d == 32) attend_d<T, 32>(a, s);
+  else if (a.d == 64) attend_d<T, 64>(a, s);
+  else if (a.d == 128) attend_d<T, 128>(a, s);
+  else attend_d<T, 256>(a, s);
 }
 void launch_cache_attend(bool bf16, const CacheAttend &a, hipStream_t s) {
-  if (bf16) {
-    if (a.d == 32) attend_bf16<32>(a, s);
-    else if (a.d == 64) attend_bf16<64>(a, s);
-    else if (a.d == 128) attend_bf16<128>(a, s);
-    else attend_bf16<256>(a, s);
-  } else {
-    if (a.d == 32) attend_f32<32>(a, s);
-    else if (a.d == 64) attend_f32<64>(a, s);
-    else if (a.d == 128) attend_f32<128>(a, s);
-    else attend_f32<256>(a, s);
-  }
-  if (a.direct) return;
-  if (bf16) join<bf16_t>(a, s);
-  else join<float>(a, s);
+  if (bf16) attend_t<bf16_t>(a, s);
+  else attend_t<float>(a, s);
 }
 
 // ---------------------------------------------------------------- summaries
