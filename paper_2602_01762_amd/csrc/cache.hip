@@ -338,15 +338,18 @@ struct Tile {
 // with the loads and retire in order with them, so each one delays the wait
 // for a tile's rows: 16 sequences of up to 16384 slots took 109 us with a store
 // per tile, 93 without any, 105 so.
-template <typename T, int D, bool KEEP>
-__global__ __launch_bounds__(64, D * sizeof(T) > 512 ? 1 : 2) void k_cache_attend(CacheAttend a) {
+//   NW > 1 (direct calls): a workgroup per segment, whose waves take its tiles
+// in turn and meet in LDS.
+template <typename T, int D, bool KEEP, int NW>
+__global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_cache_attend(CacheAttend a) {
   using M = Tile<T, D>;
   constexpr int TS = M::TS, LPR = M::LPR, RPI = M::RPI, NI = M::NI, E = 16 / sizeof(T);   // E: values of a piece
   constexpr int NS = TS / 16, NK = LPR / 4, ND = D / 16;
-  __shared__ __attribute__((aligned(16))) char s_k[TS * LPR * 16], s_v[TS * LPR * 16];
+  __shared__ __attribute__((aligned(16))) char sh_k[NW][TS * LPR * 16], sh_v[NW][TS * LPR * 16];
   constexpr int KEPT = 1024;                                // scores in LDS
   __shared__ __attribute__((aligned(16))) float s_s[KEEP ? KEPT : 4];
-  const int lane = threadIdx.x, g = a.g;
+  const int wave = NW > 1 ? wave_id() : 0, lane = threadIdx.x & 63, g = a.g;
+  char *s_k = sh_k[wave], *s_v = sh_v[wave];
   const int most = KEPT / (g * TS) * TS;                    // places whose scores fit (g <= 8: at least one tile)
   const int col = lane & 15, q4 = lane >> 4, grp = lane / LPR, li = lane % LPR;
   const KvArgs &kv = a.v.kv;
@@ -386,17 +389,19 @@ __global__ __launch_bounds__(64, D * sizeof(T) > 512 ? 1 : 2) void k_cache_atten
       wave_lds_sync();
       kept = to;
     };
-    if (sg.p0 < sg.p1) {
+    constexpr int STEP = NW * TS;
+    const int t0 = sg.p0 + wave * TS;
+    if (t0 < sg.p1) {
       int id0, pv0;
-      lk.column(sg.p0 + lane, id0, pv0);
-      lk.column(sg.p0 + TS + lane, id1, pv1);
-      lk.column(sg.p0 + 2 * TS + lane, id2, pv2);
+      lk.column(t0 + lane, id0, pv0);
+      lk.column(t0 + STEP + lane, id1, pv1);
+      lk.column(t0 + 2 * STEP + lane, id2, pv2);
       const int b0 = lk.block(id0);
       b1 = lk.block(id1);
-      row = lane < TS ? lk.row(sg.p0 + lane, id0, pv0, b0) : NO_ROW;
+      row = lane < TS ? lk.row(t0 + lane, id0, pv0, b0) : NO_ROW;
       load(row);
     }
-    for (int t = sg.p0; t < sg.p1; t += TS) {
+    for (int t = t0; t < sg.p1; t += STEP) {
       const uint64_t mask = __ballot(row != NO_ROW);   // lanes TS .. 63 hold none
       constexpr uint64_t FULL = TS == 64 ? ~0ull : (1ull << (TS & 63)) - 1;
       // rows to LDS; V rows of masked places as zeros (a NaN there must not
@@ -414,12 +419,12 @@ __global__ __launch_bounds__(64, D * sizeof(T) > 512 ? 1 : 2) void k_cache_atten
       if constexpr (KEEP)
         if (t - kept == most) store_scores(t);
       // the lookups of the tile after the next one, and the next one's rows
-      if (t + TS < sg.p1) {
-        row = lane < TS ? lk.row(t + TS + lane, id1, pv1, b1) : NO_ROW;
+      if (t + STEP < sg.p1) {
+        row = lane < TS ? lk.row(t + STEP + lane, id1, pv1, b1) : NO_ROW;
         id1 = id2;
         pv1 = pv2;
         b1 = lk.block(id1);
-        lk.column(t + 3 * TS + lane, id2, pv2);
+        lk.column(t + 3 * STEP + lane, id2, pv2);
         load(row);
       }
       wave_lds_sync();
@@ -500,17 +505,38 @@ __global__ __launch_bounds__(64, D * sizeof(T) > 512 ? 1 : 2) void k_cache_atten
     }
     if constexpr (KEEP)
       if (sg.p0 < sg.p1) store_scores(sg.p0 + (sg.p1 - sg.p0 + TS - 1) / TS * TS);
-    if (col >= g) continue;
-    if (a.direct) {
-      const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+    if constexpr (NW > 1) {
+      __shared__ float s_m[NW][16], s_l[NW][16];
+      float *so = (float *)s_k;                        // this wave's outputs [g][D]: within its K tile
+      if (col < g) {
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) {
-        const float y[4] = {o[dt][0] * inv, o[dt][1] * inv, o[dt][2] * inv, o[dt][3] * inv};
-        store_n<T, 4>((T *)a.out + hi * D + 16 * dt + 4 * q4, y);
+        for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(so + col * D + 16 * dt + 4 * q4) = o[dt];
       }
-      if (a.lse && q4 == 0) a.lse[hi] = l_run == 0.f ? -INFINITY : (m_run + log2f(l_run)) * LN2;
-      continue;
+      if (q4 == 0) {
+        s_m[wave][col] = m_run;
+        s_l[wave][col] = l_run;
+      }
+      __syncthreads();
+      for (int e = threadIdx.x; e < g * D / 4; e += 64 * NW) {
+        const int h = e / (D / 4);
+        float M2 = -INFINITY, l = 0.f;
+        for (int w = 0; w < NW; ++w) M2 = fmaxf(M2, s_m[w][h]);
+        M2 = M2 == -INFINITY ? 0.f : M2;
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < NW; ++w) {
+          const float wt = __builtin_amdgcn_exp2f(s_m[w][h] - M2);
+          l += s_l[w][h] * wt;
+          y += *(const f32x4 *)((const float *)sh_k[w] + 4 * e) * wt;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+        store_n<T, 4>((T *)a.out + ((size_t)sg.b * a.nq + sg.j * g) * D + 4 * e, z);
+        if (a.lse && e % (D / 4) == 0)
+          a.lse[(size_t)sg.b * a.nq + sg.j * g + h] = l == 0.f ? -INFINITY : (M2 + log2f(l)) * LN2;
+      }
+      return;                                          // one segment per workgroup
     }
+    if (col >= g) continue;
     const size_t part = (size_t)(blockIdx.x + sg.b * a.v.nkv + sg.j) * g + col;
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(a.po + part * D + 16 * dt + 4 * q4) = o[dt];
@@ -656,10 +682,15 @@ static void join_d(const CacheAttend &a, hipStream_t s) {
 }
 template <typename T, int D>
 static void attend_d(const CacheAttend &a, hipStream_t s) {
-  const dim3 g(a.waves), t(64);
-  if (a.weights) hipLaunchKernelGGL((k_cache_attend<T, D, true>), g, t, 0, s, a);
-  else hipLaunchKernelGGL((k_cache_attend<T, D, false>), g, t, 0, s, a);
-  if (!a.direct) join_d<T, D>(a, s);
+  constexpr int NW = D * sizeof(T) > 512 ? 2 : 4;      // 64 KB of LDS
+  const dim3 g(a.waves);
+  if (a.direct) {
+    hipLaunchKernelGGL((k_cache_attend<T, D, false, NW>), g, dim3(64 * NW), 0, s, a);
+    return;
+  }
+  if (a.weights) hipLaunchKernelGGL((k_cache_attend<T, D, true, 1>), g, dim3(64), 0, s, a);
+  else hipLaunchKernelGGL((k_cache_attend<T, D, false, 1>), g, dim3(64), 0, s, a);
+  join_d<T, D>(a, s);
 }
 template <typename T>
 static void attend_t(const CacheAttend &a, hipStream_t s) {

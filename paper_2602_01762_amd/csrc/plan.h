@@ -363,9 +363,9 @@ constexpr int CACHE_GRAN = 64;      // whole tiles of every attention kernel
 constexpr int CACHE_WAVES = 2048;   // 8 waves on each of 256 CUs, the most that are resident: each
                                     // pays its first lookups once.  32 sequences of 32768 slots:
                                     // 670 us, with 4096 waves 691, with 8192 724
-// A direct call gives each segment to one wave, which needs no join, up to
+// A direct call gives each segment to one workgroup, which needs no join, up to
 // CACHE_DIRECT places.
-constexpr int CACHE_DIRECT = 128;
+constexpr int CACHE_DIRECT = 512;
 struct CachePlan {
   int waves;
   bool direct;
