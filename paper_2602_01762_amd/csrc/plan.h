@@ -363,15 +363,17 @@ constexpr int CACHE_GRAN = 64;      // whole tiles of every attention kernel
 constexpr int CACHE_WAVES = 2048;   // 8 waves on each of 256 CUs, the most that are resident: each
                                     // pays its first lookups once.  32 sequences of 32768 slots:
                                     // 670 us, with 4096 waves 691, with 8192 724
-// A direct call gives each segment to one workgroup, which needs no join, up to
-// CACHE_DIRECT places.
-constexpr int CACHE_DIRECT = 512;
+// A direct call gives each segment to one workgroup, which needs no join: up to
+// CACHE_DIRECT places (8 segments of 512: 10.4 us, joined 10.9; of 768: 14.0 and
+// 10.8), and up to CACHE_DIRECT_MANY where CACHE_DIRECT_UNITS segments fill the
+// chip (256 segments of 1024: 25.7 us, joined 29.7; of 1 .. 1024: 22.8 and 21.6).
+constexpr int CACHE_DIRECT = 512, CACHE_DIRECT_MANY = 1024, CACHE_DIRECT_UNITS = 256;
 struct CachePlan {
   int waves;
   bool direct;
 };
 inline CachePlan cache_plan(int units, int span, bool weights) {
-  if (span <= CACHE_DIRECT && !weights) return {units, true};
+  if (span <= (units >= CACHE_DIRECT_UNITS ? CACHE_DIRECT_MANY : CACHE_DIRECT) && !weights) return {units, true};
   const long granules = (long)units * ((span + CACHE_GRAN - 1) / CACHE_GRAN);
   return {(int)(granules < CACHE_WAVES ? granules : CACHE_WAVES), false};
 }

@@ -178,7 +178,7 @@ int main() {
     const bool weights = rand() % 2;
     const CachePlan p = cache_plan(B * nkv, span, weights);
     if (p.waves < 1 || p.waves > (p.direct ? B * nkv : CACHE_WAVES)) return 1;
-    if (p.direct && (span > CACHE_DIRECT || weights)) return 2;
+    if (p.direct && (span > (B * nkv >= CACHE_DIRECT_UNITS ? CACHE_DIRECT_MANY : CACHE_DIRECT) || weights)) return 2;
     std::vector<long> begin(B), count(B);
     long total = 0;
     for (int b = 0; b < B; ++b) {

@@ -309,13 +309,13 @@ def test_attend_long_sequences(heads):
     c.close()
 
 
-@pytest.mark.parametrize("top", [1, 64, 65, 128, 129, 192])
+@pytest.mark.parametrize("top", [1, 64, 65, 129, 511, 512, 513])
 @pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (8, 8, 128, "bf16"), (4, 1, 256, "bf16"), (7, 1, 32, "bf16"),
                                    (8, 1, 128, "f32"), (3, 3, 64, "f32")])
 def test_attend_short_sequences(heads, top):
-    """Around the bound up to which a segment is one wave's."""
+    """Around the bound up to which a segment is one workgroup's."""
     lens = [0, 1, top // 2, top, max(1, top - 1)]
-    c = Cache(*heads, 16, lens, 13)
+    c = Cache(*heads, 16, lens, 33)
     q = c.normal((c.B, c.nq, c.d), 2.0)
     check_attend(c, q, c.dr.cache_attend(c.kv(), q, max_len=top, lse=True))
     w = c.weights()
@@ -324,11 +324,15 @@ def test_attend_short_sequences(heads, top):
     c.close()
 
 
-def test_attend_sixty_four_sequences():
-    lens = [(b * 131) % 700 for b in range(64)]
-    c = Cache(8, 2, 64, "bf16", 16, lens, 44)
-    q = c.normal((64, 8, 64), 2.0)
-    check_attend(c, q, c.dr.cache_attend(c.kv(), q, max_len=700, lse=True))
+@pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (8, 4, 64, "bf16"), (5, 5, 128, "f32")])
+def test_attend_sixty_four_sequences(heads):
+    """Below and above the number of segments that fill the chip."""
+    lens = [(b * 131) % 1025 for b in range(64)]
+    lens[3] = 1024
+    c = Cache(*heads, 16, lens, 65)
+    q = c.normal((64, c.nq, c.d), 2.0)
+    check_attend(c, q, c.dr.cache_attend(c.kv(), q, max_len=1024, lse=True))
+    check_attend(c, q, c.dr.cache_attend(c.kv(), q, max_len=1025, lse=True))
     c.close()
 
 
