@@ -875,7 +875,10 @@ __device__ __forceinline__ uint32_t choice_key(float v) { return (uint32_t)(cand
 // queries in registers (G of them: the heads of a KV head, rounded up to a
 // power of two; the missing ones repeat the last) and four steps of summaries
 // in flight.  The sums of the G heads meet pairwise, so that each exchange
-// halves what is left to add.
+// halves what is left to add.  Bound by instructions, some 250 per step of 64 /
+// (d / 8) blocks: 147,000 blocks of 8 KV heads' 4 queries (75 MB of summaries)
+// take 20 us; with a key made and stored per step 24.
+
 // v of the lane whose index differs in bit 2^X (X < 4: DPP within 16 lanes,
 // where the mirrors pair lanes of equal sums; else permlane swaps)
 template <int X>
@@ -916,7 +919,12 @@ __device__ __forceinline__ double group_sums(double (&s)[N]) {
     return group_sums<N, X + 1, SH>(s);
   }
 }
-__device__ __forceinline__ float nan_max(float a, float b) { return a != a ? a : b != b ? b : fmaxf(a, b); }
+// the larger one, NaN if either is
+__device__ __forceinline__ float nan_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+// A bf16 value as a double has no low word.
+__device__ __forceinline__ uint32_t high_word(float x) {
+  return (uint32_t)(__builtin_bit_cast(uint64_t, (double)x) >> 32);
+}
 
 template <typename T, int D, int G>
 __global__ __launch_bounds__(256, G > 4 ? 2 : 3) void k_cache_score(CacheSelect a) {
@@ -930,6 +938,12 @@ __global__ __launch_bounds__(256, G > 4 ? 2 : 3) void k_cache_score(CacheSelect 
   const int nblk = (int)(((long)n + bs - 1) / bs);
   const int c0 = blockIdx.x * a.per, c1 = min(nblk, c0 + a.per);
   if (c0 >= c1 || j >= a.v.nkv) return;             // whole waves
+  u32x4 raw[G][P];
+#pragma unroll
+  for (int h = 0; h < G; ++h)
+#pragma unroll
+    for (int y = 0; y < P; ++y)
+      raw[h][y] = *((const u32x4 *)((const T *)a.q + ((size_t)b * a.nq + j * a.g + min(h, a.g - 1)) * D + 8 * li) + y);
   // lane i < a.per: pool block and KV head of column c0 + i
   const uint32_t blks = lane < c1 - c0 ? pool_block(a.v, a.v.kv.block_table, b, j, c0 + lane, a.err) : NO_ROW;
   u32x4 mn[DEPTH][P], mx[DEPTH][P];
@@ -942,24 +956,39 @@ __global__ __launch_bounds__(256, G > 4 ? 2 : 3) void k_cache_score(CacheSelect 
       mx[x][y] = stream16((const u32x4 *)(p + D) + y);
     }
   };
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int x = 0; x < DEPTH; ++x) load(x, c0 + x * RPI);
+  for (int x = 0; x < DEPTH; ++x) {                 // in this order: a wait for one leaves the others in flight
+    load(x, c0 + x * RPI);
+    __builtin_amdgcn_sched_barrier(0);
+  }
   double q[G][8];
 #pragma unroll
   for (int h = 0; h < G; ++h) {
     float x[8];
-    load8f<T>((const T *)a.q + ((size_t)b * a.nq + j * a.g + min(h, a.g - 1)) * D + 8 * li, x);
+    unpack8<T>(raw[h], x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[h][i] = (double)x[i];
   }
+  float mine = 0.f;                                 // score of column c0 + li * RPI + grp (a.per <= 64)
+  int step = 0;
   for (int cc = c0; cc < c1; cc += DEPTH * RPI)
 #pragma unroll
-    for (int x = 0; x < DEPTH; ++x) {
+    for (int x = 0; x < DEPTH; ++x, ++step) {
       const int c = cc + x * RPI;
       float lo[8], hi[8];                           // (of pool block 0 past the last column: not kept)
       unpack8<T>(mn[x], lo);
       unpack8<T>(mx[x], hi);
+      uint32_t lo_w[8], hi_w[8];                    // bf16: high words as doubles
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          lo_w[i] = high_word(lo[i]);
+          hi_w[i] = high_word(hi[i]);
+        }
+      }
       load(x, c + DEPTH * RPI);                     // always, so that the loads can be counted
+      __builtin_amdgcn_sched_barrier(0);
       float best = -INFINITY;
 #pragma unroll
       for (int h0 = 0; h0 < G; h0 += N) {
@@ -968,20 +997,29 @@ __global__ __launch_bounds__(256, G > 4 ? 2 : 3) void k_cache_score(CacheSelect 
         for (int h = 0; h < N; ++h) {
           s[h] = 0.0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s[h] += q[h0 + h][i] * (double)(q[h0 + h][i] >= 0.0 ? hi[i] : lo[i]);
+          for (int i = 0; i < 8; ++i) {
+            const double x = q[h0 + h][i];
+            double m;
+            if constexpr (sizeof(T) == 2)
+              m = __builtin_bit_cast(double, (uint64_t)(x >= 0.0 ? hi_w[i] : lo_w[i]) << 32);
+            else
+              m = (double)(x >= 0.0 ? hi[i] : lo[i]);
+            s[h] += x * m;
+          }
         }
         best = nan_max(best, (float)group_sums<N, 0, SH>(s));
       }
       if constexpr (N > 1) best = nan_max(best, xor_f32<0>(best));
       if constexpr (N > 2) best = nan_max(best, xor_f32<1>(best));
       if constexpr (N > 4) best = nan_max(best, xor_f32<2>(best));
-      const int bi = c + grp;
-      const bool bad = (uint32_t)__shfl((int)blks, min(bi - c0, 63), 64) == NO_ROW;
-      if (bi < c1 && li == 0) {
-        const bool forced = bi < a.n_first || bi >= nblk - a.n_last;
-        a.keys[((size_t)b * a.v.nkv + j) * a.ld_keys + bi] = bad ? 0u : forced ? KEY_FORCED : choice_key(best);
-      }
+      if (li == step) mine = best;
     }
+  const int bi = c0 + li * RPI + grp;
+  const bool bad = (uint32_t)__shfl((int)blks, bi - c0, 64) == NO_ROW;
+  if (bi < c1) {
+    const bool forced = bi < a.n_first || bi >= nblk - a.n_last;
+    a.keys[((size_t)b * a.v.nkv + j) * a.ld_keys + bi] = bad ? 0u : forced ? KEY_FORCED : choice_key(mine);
+  }
 }
 
 // Inclusive sum over the lanes below, in a wave (DPP: within rows of 16

@@ -381,13 +381,15 @@ inline CachePlan cache_plan(int units, int span, bool weights) {
 inline int cache_score_row(int span) { return (span + CACHE_GRAN - 1) / CACHE_GRAN * CACHE_GRAN; }
 
 // Table columns per wave of the passes over the blocks of a cache (summaries,
-// scores), for units * columns of them at most: about CACHE_BLOCK_WAVES waves,
-// a multiple of `step` columns (those of one load), at most `top` <= 64 (one
-// lane looks up each).
-constexpr int CACHE_BLOCK_WAVES = 4096;
-constexpr int CACHE_SUM_COLUMNS = 8;   // summaries
-inline int cache_columns_per_wave(long units, int columns, int step, int top) {
-  const long steps = (units * columns + (long)CACHE_BLOCK_WAVES * step - 1) / ((long)CACHE_BLOCK_WAVES * step);
+// scores), for units * columns of them at most: about `waves` waves, a multiple
+// of `step` columns (those of one load), at most `top` <= 64 (one lane looks up
+// each).  Scores take fewer waves, since each has queries to convert (131071
+// slots, 8 KV heads of 4 queries, the whole sparse step: 2048 waves 32.5 us,
+// 4096 34.1, 8192 40.2).
+constexpr int CACHE_SUM_WAVES = 4096, CACHE_SUM_COLUMNS = 8;
+constexpr int CACHE_SCORE_WAVES = 2048, CACHE_SCORE_COLUMNS = 64;
+inline int cache_columns_per_wave(long units, int columns, int step, int top, int waves) {
+  const long steps = (units * columns + (long)waves * step - 1) / ((long)waves * step);
   const long most = top / step;
   return (int)(steps < 1 ? 1 : steps > most ? most : steps) * step;
 }

@@ -1636,7 +1636,7 @@ prism_status prism_cache_summarize(prism_ctx *c, const prism_batch *kv, int32_t 
   const int bs = c->cfg.kv_block_size;
   a.columns = c->cfg.max_blocks_per_seq;
   if (span > 0) a.columns = (int)std::min((long)a.columns, ((long)span + bs - 1) / bs + 1);
-  a.per = cache_columns_per_wave((long)kv->batch * c->nkv, a.columns, 1, CACHE_SUM_COLUMNS);
+  a.per = cache_columns_per_wave((long)kv->batch * c->nkv, a.columns, 1, CACHE_SUM_COLUMNS, CACHE_SUM_WAVES);
   a.summary = d_summary;
   a.err = c->err;
   launch_cache_summarize(c->bf16, a, c->d, (hipStream_t)stream);
@@ -1669,7 +1669,8 @@ prism_status prism_cache_select(prism_ctx *c, const prism_cache_selection *io, v
   a.n_first = io->n_first;
   a.n_last = io->n_last;
   a.columns = (len + c->cfg.kv_block_size - 1) / c->cfg.kv_block_size;
-  a.per = cache_columns_per_wave((long)B * c->nkv, a.columns, 512 / c->d, 64);   // d / 8 lanes per block
+  // d / 8 lanes per block
+  a.per = cache_columns_per_wave((long)B * c->nkv, a.columns, 512 / c->d, CACHE_SCORE_COLUMNS, CACHE_SCORE_WAVES);
   a.keys = (uint32_t *)io->d_scratch;
   a.ld_keys = choose_key_row(a.columns);
   a.out = io->d_blocks;
