@@ -512,8 +512,8 @@ prism_status prism_cache_scratch(prism_ctx *ctx, int32_t call, int32_t batch, in
  * normalised, x / sqrt(mean(x^2) + rms_eps) * gain (where its gain is given),
  * and rotated, (x_i, x_{i + d/2}) by the angle p * rope_theta^(-2i/d), in one
  * pass; one rounding to the context dtype at the end.  Keys and values go to
- * the cache, queries to d_q.  A block that receives rows belongs to one
- * sequence of the call.  A malformed d_offsets raises PRISM_ERR_INVALID_ARG in
+ * the cache, queries to d_q.  A block that receives rows stands once in the
+ * block table (of all sequences).  A malformed d_offsets raises PRISM_ERR_INVALID_ARG in
  * prism_device_status and appends nothing. */
 prism_status prism_cache_append(prism_ctx *ctx, const prism_cache_rows *io, void *stream);
 
@@ -521,7 +521,8 @@ prism_status prism_cache_append(prism_ctx *ctx, const prism_cache_rows *io, void
  * (GQA: query head h reads KV head h / (n_q_heads / n_kv_heads)), split over
  * the cache's length and joined.  A sequence that sees nothing, or whose every
  * score is -inf, gives zeros and a log-sum of -inf.  With d_weights no block
- * may belong to two sequences of the call.  An entry of d_blocks that is out
+ * may stand twice in the visible columns of the block table, in one sequence or
+ * in two.  An entry of d_blocks that is out
  * of range, or not larger than the entry before it, is skipped and raises
  * PRISM_ERR_INVALID_ARG in prism_device_status. */
 prism_status prism_cache_attend(prism_ctx *ctx, const prism_cache_attention *io, void *stream);

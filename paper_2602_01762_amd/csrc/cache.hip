@@ -875,9 +875,8 @@ __device__ __forceinline__ uint32_t choice_key(float v) { return (uint32_t)(cand
 // queries in registers (G of them: the heads of a KV head, rounded up to a
 // power of two; the missing ones repeat the last) and four steps of summaries
 // in flight.  The sums of the G heads meet pairwise, so that each exchange
-// halves what is left to add.  Bound by instructions, some 250 per step of 64 /
-// (d / 8) blocks: 147,000 blocks of 8 KV heads' 4 queries (75 MB of summaries)
-// take 20 us; with a key made and stored per step 24.
+// halves what is left to add.  Bound by instructions, some 250 per step (d =
+// 128, 4 heads): 147,000 summaries (75 MB) of 16 sequences take 20 us.
 
 // v of the lane whose index differs in bit 2^X (X < 4: DPP within 16 lanes,
 // where the mirrors pair lanes of equal sums; else permlane swaps)
