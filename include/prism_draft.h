@@ -520,11 +520,12 @@ prism_status prism_cache_append(prism_ctx *ctx, const prism_cache_rows *io, void
 /* out = softmax(q K^T / sqrt(d)) V over the visible slots of each sequence
  * (GQA: query head h reads KV head h / (n_q_heads / n_kv_heads)), split over
  * the cache's length and joined.  A sequence that sees nothing, or whose every
- * score is -inf, gives zeros and a log-sum of -inf.  With d_weights no block
- * may stand twice in the visible columns of the block table, in one sequence or
- * in two.  An entry of d_blocks that is out
- * of range, or not larger than the entry before it, is skipped and raises
- * PRISM_ERR_INVALID_ARG in prism_device_status. */
+ * score is -inf, gives zeros and a log-sum of -inf.  An infinite value gives
+ * its channel that infinity (NaN where both signs meet; that or NaN where its
+ * probability is below 2^-126).  With d_weights no block may stand twice in
+ * the visible columns of the block table, in one sequence or in two.  An entry
+ * of d_blocks that is out of range, or not larger than the entry before it, is
+ * skipped and raises PRISM_ERR_INVALID_ARG in prism_device_status. */
 prism_status prism_cache_attend(prism_ctx *ctx, const prism_cache_attention *io, void *stream);
 
 /* Summaries of cache blocks: d_summary[block, head, 0 / 1, :] = the minimum /

@@ -312,13 +312,32 @@ struct Lookup {
 //   In LDS the 16-byte pieces of row s are permuted by s, so that both the
 // A-operand reads (16 rows, one piece) and the transposing reads (4 rows, the
 // pieces of 16 dims) spread over all banks.
-//   In bf16 caches probabilities are multiplied as a pair of bf16 (value and
-// remainder, 2^-16), so that the output keeps the accuracy of its own rounding.
+//   In bf16 caches a probability is multiplied as the sum of three bf16, which
+// hold its 24 bits exactly (split_bf16).
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+// The upper halves of two fp32: their bf16 values cut off.
+__device__ __forceinline__ uint32_t pack_upper(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+// Four probabilities as hi + mid + lo, each the next 8 bits of the value, cut
+// off: no part is negative, and a part is 0 only where p is (what would be 0 is
+// 2^-126, below every rounding of a sum), so that an infinite value times the
+// parts is that infinity and no NaN.
+__device__ __forceinline__ void split_bf16(const f32x4 &p, uint32_t (&hi)[2], uint32_t (&mid)[2], uint32_t (&lo)[2]) {
+  float m[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float least = fminf(p[i], 0x1p-126f);
+    const float r = p[i] - __uint_as_float(__float_as_uint(p[i]) & 0xffff0000u);
+    m[i] = fmaxf(r, least);
+    l[i] = fmaxf(r - __uint_as_float(__float_as_uint(m[i]) & 0xffff0000u), least);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    hi[i] = pack_upper(p[2 * i], p[2 * i + 1]);
+    mid[i] = pack_upper(m[2 * i], m[2 * i + 1]);
+    lo[i] = pack_upper(l[2 * i], l[2 * i + 1]);
+  }
 }
 
 template <typename T, int D>
@@ -475,20 +494,33 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_cache_
         for (int dt = 0; dt < ND; ++dt) o[dt] *= al;
       }
       // O[dim 16 dt + 4 q4 + i][head col]
+      constexpr int NP = sizeof(T) == 2 && NS > 1 ? 2 : 1;   // groups of 16 slots per bf16 MFMA (32 slots, or 16)
 #pragma unroll
-      for (int st = 0; st < NS; ++st) {
+      for (int st = 0; st < NS; st += NP) {
         if constexpr (sizeof(T) == 2) {
-          const uint32_t h0 = pack_bf16(sc[st][0], sc[st][1]), h1 = pack_bf16(sc[st][2], sc[st][3]);
-          const uint32_t l0 = pack_bf16(sc[st][0] - __uint_as_float(h0 << 16), sc[st][1] - __uint_as_float(h0 & 0xffff0000u));
-          const uint32_t l1 = pack_bf16(sc[st][2] - __uint_as_float(h1 << 16), sc[st][3] - __uint_as_float(h1 & 0xffff0000u));
-          const s16x4 ph = __builtin_bit_cast(s16x4, uint2{h0, h1}), pl = __builtin_bit_cast(s16x4, uint2{l0, l1});
-          const int row = 16 * st + 4 * q4 + (col >> 2);
+          uint32_t hi[NP][2], mid[NP][2], lo[NP][2];
+#pragma unroll
+          for (int x = 0; x < NP; ++x) split_bf16(sc[st + x], hi[x], mid[x], lo[x]);
 #pragma unroll
           for (int dt = 0; dt < ND; ++dt) {
-            const char *pv = s_v + M::at(row, 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
-            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv);
-            o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, ph, o[dt], 0, 0, 0);
-            o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pl, o[dt], 0, 0, 0);
+            uint2 v[NP];
+#pragma unroll
+            for (int x = 0; x < NP; ++x) {
+              const char *pv = s_v + M::at(16 * (st + x) + 4 * q4 + (col >> 2), 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
+              v[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
+            }
+            if constexpr (NP == 2) {
+              // k = 8 q4 + e: slots 16 st + 4 q4 + e, then the same of st + 1, in both operands
+              const u32x4 vv = {v[0].x, v[0].y, v[1].x, v[1].y};
+              o[dt] = Ty<T>::mma(vv, u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]}, o[dt]);
+              o[dt] = Ty<T>::mma(vv, u32x4{mid[0][0], mid[0][1], mid[1][0], mid[1][1]}, o[dt]);
+              o[dt] = Ty<T>::mma(vv, u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]}, o[dt]);
+            } else {
+              const s16x4 vv = __builtin_bit_cast(s16x4, v[0]);
+              o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, __builtin_bit_cast(s16x4, uint2{hi[0][0], hi[0][1]}), o[dt], 0, 0, 0);
+              o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, __builtin_bit_cast(s16x4, uint2{mid[0][0], mid[0][1]}), o[dt], 0, 0, 0);
+              o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, __builtin_bit_cast(s16x4, uint2{lo[0][0], lo[0][1]}), o[dt], 0, 0, 0);
+            }
           }
         } else {
           // step i: slot 4 q4 + i of each lane row

@@ -397,6 +397,47 @@ def test_attend_infinities_and_nan(dtype):
     c.close()
 
 
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("lens", [[1, 17, 333], [1, 700, 2100]])
+def test_attend_infinite_values(heads, lens):
+    """Every probability is above 0, so an infinity among the values gives its
+    channel that infinity, both signs NaN, and leaves the other channels and
+    KV heads alone: by one workgroup, joined, with slot weights, by a list."""
+    c = Cache(*heads, 16, lens, -(-lens[-1] // 16))
+    q = c.normal((c.B, c.nq, c.d))
+    for b, n in enumerate(lens):
+        def put(slot, channel, value):
+            c.v[int(c.table_h[b, slot // 16]), 0, slot % 16, channel] = value
+        put(n - 1, 0, float("inf"))
+        put(n // 2, 1, float("-inf"))
+        put(0, 2, float("inf"))
+        put(n - 1, 2, float("-inf"))
+        for slot in range(0, n, 3):
+            put(slot, 7, float("-inf"))
+    qh, kh, vh = f64(q), f64(c.k), f64(c.v)
+    every = torch.full((c.B, c.nkv, c.columns), -1, dtype=torch.int32, device=DEV)
+    for b, n in enumerate(lens):
+        every[b, :, : -(-n // 16)] = torch.arange(-(-n // 16), device=DEV)
+    for kw in (dict(), dict(weights=c.weights()), dict(blocks=every)):
+        out = f64(c.dr.cache_attend(c.kv(), q, max_len=lens[-1], **kw)["out"])
+        for b, n in enumerate(lens):
+            for j in range(c.nkv):
+                K, V = c.rows(kh, b, j, np.arange(n)), c.rows(vh, b, j, np.arange(n))
+                qq = qh[b, j * c.g: (j + 1) * c.g]
+                p = C.attend(qq, K, np.zeros_like(V))[1]
+                with np.errstate(invalid="ignore"):
+                    want = (p[:, :, None] * V).sum(axis=1)
+                got = out[b, j * c.g: (j + 1) * c.g]
+                fin = np.isfinite(want)
+                assert np.array_equal(got[~fin], want[~fin], equal_nan=True), (b, j)
+                delta = (c.d + 4) * U * (np.abs(qq) @ np.abs(K).T).max() / np.sqrt(c.d)
+                rel = 2 * delta + (min(n, 1024) + 64) * U
+                lim = (2.0 ** -8 if c.dt == torch.bfloat16 else 0.0) * np.abs(want[fin])
+                lim = lim + rel * (p[:, :, None] * np.abs(V)).sum(axis=1)[fin]
+                assert np.all(np.abs(got[fin] - want[fin]) <= lim), (b, j)
+    c.close()
+
+
 def test_attend_rows_beyond_four_gigabytes():
     """Blocks at the end of pools of more than 2^32 bytes."""
     nkv, d, bs = 8, 128, 16
