@@ -498,8 +498,9 @@ typedef struct {
   uint64_t scratch_bytes;
 } prism_cache_eviction;
 
-/* Scratch bytes of one call over up to `batch` sequences: attention, the same
- * with slot weights, selection, eviction.  max_len as in the call; for
+/* Scratch bytes of one call over up to `batch` sequences (the most that any
+ * smaller batch takes too): attention, the same with slot weights, selection,
+ * eviction.  max_len as in the call; for
  * attention over a block list min(n_blocks, max_blocks_per_seq) *
  * kv_block_size (whichever max_len the call has). */
 enum { PRISM_CACHE_ATTEND = 0, PRISM_CACHE_ATTEND_WEIGHTS = 1, PRISM_CACHE_SELECT = 2,

@@ -379,6 +379,27 @@ inline CachePlan cache_plan(int units, int span, bool weights) {
 }
 // row length of the scores kept for the slot weights: whole granules
 inline int cache_score_row(int span) { return (span + CACHE_GRAN - 1) / CACHE_GRAN * CACHE_GRAN; }
+// Scratch bytes of an attention call over `batch` sequences with nkv KV heads of
+// g query heads and d channels: two statistics and an output of each partial
+// (256-byte aligned runs), and the kept scores.
+inline size_t cache_attend_scratch(int batch, int nkv, int g, int d, int span, bool weights) {
+  const CachePlan p = cache_plan(batch * nkv, span, weights);
+  if (p.direct) return 0;
+  const size_t parts = (size_t)(p.waves + batch * nkv) * g, pad = 255;
+  size_t n = ((parts * 4 + pad) & ~pad) * 2 + ((parts * d * 4 + pad) & ~pad);
+  if (weights) n += (size_t)batch * nkv * g * cache_score_row(span) * 4;
+  return n;
+}
+// The most that any batch up to this one takes: a larger one may be direct, and
+// take none, where a smaller one is not.
+inline size_t cache_attend_scratch_up_to(int batch, int nkv, int g, int d, int span, bool weights) {
+  size_t most = 0;
+  for (int b = 1; b <= batch; ++b) {
+    const size_t n = cache_attend_scratch(b, nkv, g, d, span, weights);
+    most = n > most ? n : most;
+  }
+  return most;
+}
 
 // Table columns per wave of the passes over the blocks of a cache (summaries,
 // scores), for units * columns of them at most: about `waves` waves, a multiple

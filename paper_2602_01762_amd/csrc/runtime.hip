@@ -1500,18 +1500,8 @@ static prism_status check_len(prism_ctx *c, int32_t n_new, int32_t max_len, int 
   *out = max_len ? max_len : c->max_slots;
   return PRISM_OK;
 }
-static size_t cache_scratch(const prism_ctx *c, int call, int B, int span) {
-  const size_t pad = 255;
-  if (call == PRISM_CACHE_SELECT)
-    return (size_t)B * c->nkv * choose_key_row((span + c->cfg.kv_block_size - 1) / c->cfg.kv_block_size) * 4;
-  if (call == PRISM_CACHE_EVICT) return choose_scratch((size_t)B * c->nkv, span);
-  const bool weights = call == PRISM_CACHE_ATTEND_WEIGHTS;
-  const CachePlan p = cache_plan(B * c->nkv, span, weights);
-  if (p.direct) return 0;
-  const size_t parts = (size_t)(p.waves + B * c->nkv) * (c->nq / c->nkv);
-  size_t n = ((parts * 4 + pad) & ~pad) * 2 + ((parts * c->d * 4 + pad) & ~pad);
-  if (weights) n += (size_t)B * c->nq * cache_score_row(span) * 4;
-  return n;
+static size_t select_scratch(const prism_ctx *c, int B, int len) {
+  return (size_t)B * c->nkv * choose_key_row((len + c->cfg.kv_block_size - 1) / c->cfg.kv_block_size) * 4;
 }
 static prism_status check_scratch(prism_ctx *c, const void *p, uint64_t bytes, size_t need) {
   if (!need) return PRISM_OK;
@@ -1545,7 +1535,9 @@ prism_status prism_cache_scratch(prism_ctx *c, int32_t call, int32_t batch, int3
     return fail(c, PRISM_ERR_INVALID_ARG, "batch %d out of 1..%d", batch, c->cfg.max_batch);
   int len = 0;
   CHECK(check_len(c, 0, max_len, &len));
-  *bytes = cache_scratch(c, call, batch, len);
+  if (call == PRISM_CACHE_SELECT) *bytes = select_scratch(c, batch, len);
+  else if (call == PRISM_CACHE_EVICT) *bytes = choose_scratch((size_t)batch * c->nkv, len);
+  else *bytes = cache_attend_scratch_up_to(batch, c->nkv, c->nq / c->nkv, c->d, len, call == PRISM_CACHE_ATTEND_WEIGHTS);
   return PRISM_OK;
 }
 
@@ -1592,7 +1584,7 @@ prism_status prism_cache_attend(prism_ctx *c, const prism_cache_attention *io, v
   const int B = io->kv->batch;
   const int span = io->d_blocks ? std::min(io->n_blocks, c->cfg.max_blocks_per_seq) * c->cfg.kv_block_size : len;
   CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes,
-                      cache_scratch(c, io->d_weights ? PRISM_CACHE_ATTEND_WEIGHTS : PRISM_CACHE_ATTEND, B, span)));
+                      cache_attend_scratch(B, c->nkv, c->nq / c->nkv, c->d, span, io->d_weights != nullptr)));
   const CachePlan p = cache_plan(B * c->nkv, span, io->d_weights != nullptr);
   CacheAttend a{};
   a.v = cache_view(c, io->kv, io->n_new, len);
@@ -1658,7 +1650,7 @@ prism_status prism_cache_select(prism_ctx *c, const prism_cache_selection *io, v
     return fail(c, PRISM_ERR_INVALID_ARG, "n_first %d and n_last %d of n_blocks %d", io->n_first, io->n_last,
                 io->n_blocks);
   const int B = io->kv->batch;
-  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, cache_scratch(c, PRISM_CACHE_SELECT, B, len)));
+  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, select_scratch(c, B, len)));
   CacheSelect a{};
   a.v = cache_view(c, io->kv, io->n_new, len);
   a.nq = c->nq;
@@ -1700,7 +1692,7 @@ prism_status prism_cache_evict(prism_ctx *c, const prism_cache_eviction *io, voi
   if (len > CHOOSE_MAX_SEGS * CHOOSE_SEG)
     return fail(c, PRISM_ERR_SHAPE, "max_len %d exceeds the choice's %d slots", len, CHOOSE_MAX_SEGS * CHOOSE_SEG);
   const int B = io->kv->batch;
-  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, cache_scratch(c, PRISM_CACHE_EVICT, B, len)));
+  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, choose_scratch((size_t)B * c->nkv, len)));
   CacheEvict a{};
   a.v = cache_view(c, io->kv, 0, len);
   a.new_table = io->d_new_table;

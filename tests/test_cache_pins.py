@@ -220,3 +220,37 @@ int main() {
     subprocess.run(["g++", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2602_01762_amd", "csrc"), str(src),
                     "-o", str(exe)], check=True)
     assert subprocess.run([str(exe)]).returncode == 0
+
+
+def test_scratch_of_a_batch_serves_every_smaller_one(tmp_path):
+    """Some larger batches need none where smaller ones do (and the size for a
+    batch that needs none alone is not 0 then)."""
+    src, exe = tmp_path / "scratch.cc", tmp_path / "scratch"
+    src.write_text(r"""
+#include "plan.h"
+using namespace prism;
+int main() {
+  const int spans[] = {1, 64, 511, 512, 513, 700, 1000, 1023, 1024, 1025, 4096, 131072};
+  const int nkvs[] = {1, 2, 5, 8, 32}, gs[] = {1, 4, 8}, ds[] = {32, 256};
+  int grows = 0;
+  for (int span : spans)
+    for (int nkv : nkvs)
+      for (int g : gs)
+        for (int d : ds)
+          for (int weights = 0; weights < 2; ++weights) {
+            size_t most = 0;
+            for (int b = 1; b <= 64; ++b) {
+              const size_t need = cache_attend_scratch(b, nkv, g, d, span, weights);
+              const size_t size = cache_attend_scratch_up_to(b, nkv, g, d, span, weights);
+              most = need > most ? need : most;
+              if (size != most) return 1;
+              grows += need < size;
+              if (span <= 512 && !weights && size) return 2;
+            }
+          }
+  return grows ? 0 : 3;
+}
+""")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2602_01762_amd", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)]).returncode == 0

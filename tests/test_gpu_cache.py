@@ -336,6 +336,28 @@ def test_attend_sixty_four_sequences(heads):
     c.close()
 
 
+@pytest.mark.parametrize("top", [512, 513, 1000, 1024, 1025])
+def test_scratch_sized_for_the_largest_batch(top):
+    """serves the calls of every smaller one."""
+    import ctypes
+    from paper_2602_01762_amd import binding as B
+    lens = [(b * 131) % (top + 1) for b in range(64)]
+    lens[3] = top
+    c = Cache(8, 8, 32, "bf16", 16, lens, -(-top // 16))
+    q = c.normal((64, c.nq, c.d), 2.0)
+    n = B.prism_cache_scratch(c.dr.ctx, B.PRISM_CACHE_ATTEND, 64, top)
+    scratch = torch.empty(max(n, 16), dtype=torch.uint8, device=DEV)
+    for nb in (64, 33, 32, 31, 16, 5, 1):
+        kv = c.dr.cache(c.lens[:nb], c.k, c.v, c.table[:nb])
+        out = torch.empty((nb, c.nq, c.d), dtype=c.dt, device=DEV)
+        io = B.prism_cache_attention()
+        io.kv, io.max_len, io.d_q, io.d_out = ctypes.addressof(kv), top, B.ptr(q), B.ptr(out)
+        io.d_scratch, io.scratch_bytes = B.ptr(scratch), n
+        B.prism_cache_attend(c.dr.ctx, io)
+        assert torch.equal(out, c.dr.cache_attend(kv, q[:nb], max_len=top)["out"])
+    c.close()
+
+
 def test_attend_sees_the_appended_row():
     c = Cache(8, 2, 64, "bf16", 16, [0, 47, 48], 4)
     q = c.dr.cache_append(c.kv(), c.normal((3, 12 * 64)))
