@@ -525,8 +525,9 @@ prism_status prism_cache_append(prism_ctx *ctx, const prism_cache_rows *io, void
  * its channel that infinity (NaN where both signs meet; that or NaN where its
  * probability is below 2^-126).  With d_weights no block may stand twice in
  * the visible columns of the block table, in one sequence or in two.  An entry
- * of d_blocks that is out of range, or not larger than the entry before it, is
- * skipped and raises PRISM_ERR_INVALID_ARG in prism_device_status. */
+ * of d_blocks that is out of range, not larger than every entry before it, or
+ * behind a -1, is skipped and raises PRISM_ERR_INVALID_ARG in
+ * prism_device_status. */
 prism_status prism_cache_attend(prism_ctx *ctx, const prism_cache_attention *io, void *stream);
 
 /* Summaries of cache blocks: d_summary[block, head, 0 / 1, :] = the minimum /

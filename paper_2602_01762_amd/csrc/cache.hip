@@ -101,6 +101,29 @@ __device__ __forceinline__ void store8f(T *p, const float (&x)[8]) {
   }
 }
 
+// Inclusive sum over the lanes below, in a wave (DPP: within rows of 16
+// lanes, then the last lane of a row to the next row, then of the first half
+// to the second).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);    // row_shr:1
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);    // row_shr:2
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);    // row_shr:4
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);    // row_shr:8
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);   // row_bcast:31
+  return v;
+}
+// The same with the larger value for the sum.
+__device__ __forceinline__ uint32_t wave_scan_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
+  return v;
+}
+
 // ---------------------------------------------------------------- append
 // One lane group of d / 16 lanes per head: lane i holds dims 8i .. 8i+7 and
 // their rotation partners d/2 + 8i ...  The angles of a row are the same for
@@ -264,30 +287,71 @@ __device__ __forceinline__ Segment segment_at(const CacheAttend &a, const Walk &
 }
 
 // Lookup of a segment's places, in the steps that their loads allow: the
-// table column of a place (from the list, with its predecessor), the block of
-// the column, the pool row.  The loads are made for every place (past the end
-// for the last one), so that they can be issued early and counted.
+// table column of a place (from the list), the block of the column, the pool
+// row.  The loads are made for every place (past the end for the last one), so
+// that they can be issued early and counted.
+//   An entry of a list is read if it is larger than every entry before it and
+// none of them is -1, so that no block is read twice whatever the list holds.
+// A wave keeps that of 64 entries at a time: begin() looks through the list up
+// to them, advance() moves on (a load that is waited for, every 64 entries).
 struct Lookup {
   const CacheAttend &a;
   const Segment &s;
   const int32_t *table, *list;
+  int first = 0;         // entries first .. first + 63:
+  uint64_t rising = 0;   // bit i: entry first + i is to be read
+  uint32_t most = 0;     // lane i: the largest rank of entries up to first + i
   __device__ __forceinline__ Lookup(const CacheAttend &a_, const Segment &s_)
       : a(a_), s(s_), table(a_.v.kv.block_table + (size_t)s_.b * a_.v.kv.mbps),
         list(a_.blocks ? a_.blocks + ((size_t)s_.b * a_.v.nkv + s_.j) * a_.n_list : nullptr) {}
-  __device__ __forceinline__ void column(int p, int &id, int &prev) const {
-    const int bi = slot_block(a.v.kv, min(p, s.p1 - 1));
-    id = list ? list[bi] : bi;
-    prev = list && bi > 0 ? list[bi - 1] : -1;
+  __device__ __forceinline__ int entry(int p) const { return slot_block(a.v.kv, min(p, s.p1 - 1)); }
+  // an entry's place in the order: nothing is larger than -1, and what is no
+  // block is larger than nothing
+  static __device__ __forceinline__ uint32_t rank(int id) { return id >= 0 ? (uint32_t)id + 1u : id == -1 ? ~0u : 0u; }
+  __device__ __forceinline__ void window(int c, int id, uint32_t before) {
+    most = max(wave_scan_max(rank(id)), before);
+    const uint32_t below = __shfl_up(most, 1, 64);
+    rising = __ballot(id >= 0 && rank(id) > ((threadIdx.x & 63) ? below : before));
+    first = c;
   }
+  // the loads of begin(), for the entries from place p on
+  struct Start {
+    int id, early;
+  };
+  __device__ __forceinline__ Start start(int p) const {
+    if (!list) return {0, 0};
+    const int lane = threadIdx.x & 63, c = entry(p);
+    return {list[min(c + lane, entry(s.p1))], c ? list[min(lane, c - 1)] : -2};
+  }
+  __device__ __forceinline__ void begin(int p, const Start &st) {
+    if (!list) return;
+    const int lane = threadIdx.x & 63, c = entry(p);
+    uint32_t v = rank(st.early);
+#pragma unroll 4
+    for (int i = 64; i < c; i += 64) v = max(v, rank(list[min(i + lane, c - 1)]));
+    window(c, st.id, (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_max(v), 63));
+  }
+  // the entries of places p .. p + 63 at most become those at hand (p not
+  // below that of the call before)
+  __device__ __forceinline__ void advance(int p, int places) {
+    if (!list) return;
+    const int lane = threadIdx.x & 63, c = entry(p), c1 = entry(p + places - 1), end = entry(s.p1);
+    while (c >= first + 64)
+      window(first + 64, list[min(first + 64 + lane, end)], (uint32_t)__builtin_amdgcn_readlane((int)most, 63));
+    if (c1 >= first + 64)
+      window(c, list[min(c + lane, end)], (uint32_t)__builtin_amdgcn_readlane((int)most, c - 1 - first));
+  }
+  __device__ __forceinline__ int column(int p) const { return list ? list[entry(p)] : entry(p); }
   __device__ __forceinline__ int block(int id) const { return table[id >= 0 && id < a.v.kv.mbps ? id : 0]; }
-  __device__ __forceinline__ uint32_t row(int p, int id, int prev, int blk) const {
+  __device__ __forceinline__ uint32_t row(int p, int id, int blk) const {
     const KvArgs &kv = a.v.kv;
     if (p >= s.p1 || id == -1) return NO_ROW;
-    if (list && (id < 0 || id <= prev || (long)id * kv.bs >= s.n)) {
+    const int e = slot_block(kv, p);
+    if (list && (!((rising >> (e - first)) & 1) || (long)id * kv.bs >= s.n)) {
       atomicOr(a.err, ERRF_ROWS);
       return NO_ROW;
     }
-    const int off = p - slot_block(kv, p) * kv.bs;
+    const int off = p - e * kv.bs;
     if ((long)id * kv.bs + off >= s.n) return NO_ROW;
     if (blk < 0 || blk >= kv.n_blocks) {
       atomicOr(a.err, ERRF_CAPACITY);
@@ -378,7 +442,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_cache_
   while (u < last) {
     const Segment sg = segment_at(a, wk, u, last);
     u += sg.granules;
-    const Lookup lk(a, sg);
+    Lookup lk(a, sg);
     const size_t hi = (size_t)sg.b * a.nq + sg.j * g + col;   // this lane's query head (col < g)
     u32x4 kr[NI], vr[NI];
     auto load = [&](uint32_t row) {
@@ -398,7 +462,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_cache_
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk)
       qf[kk] = col < g ? *(const u32x4 *)((const T *)a.q + hi * D + (4 * kk + q4) * E) : u32x4{0, 0, 0, 0};
-    int id1, pv1, b1, id2, pv2;
+    int id1, b1, id2;
     uint32_t row = NO_ROW;
     int kept = sg.p0;                                       // first place whose scores are in LDS
     auto store_scores = [&](int to) {                       // places kept .. to - 1
@@ -411,13 +475,14 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_cache_
     constexpr int STEP = NW * TS;
     const int t0 = sg.p0 + wave * TS;
     if (t0 < sg.p1) {
-      int id0, pv0;
-      lk.column(t0 + lane, id0, pv0);
-      lk.column(t0 + STEP + lane, id1, pv1);
-      lk.column(t0 + 2 * STEP + lane, id2, pv2);
+      const int id0 = lk.column(t0 + lane);
+      const typename Lookup::Start st = lk.start(t0);
+      id1 = lk.column(t0 + STEP + lane);
+      id2 = lk.column(t0 + 2 * STEP + lane);
       const int b0 = lk.block(id0);
       b1 = lk.block(id1);
-      row = lane < TS ? lk.row(t0 + lane, id0, pv0, b0) : NO_ROW;
+      lk.begin(t0, st);
+      row = lane < TS ? lk.row(t0 + lane, id0, b0) : NO_ROW;
       load(row);
     }
     for (int t = t0; t < sg.p1; t += STEP) {
@@ -439,11 +504,11 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_cache_
         if (t - kept == most) store_scores(t);
       // the lookups of the tile after the next one, and the next one's rows
       if (t + STEP < sg.p1) {
-        row = lane < TS ? lk.row(t + STEP + lane, id1, pv1, b1) : NO_ROW;
+        lk.advance(t + STEP, TS);
+        row = lane < TS ? lk.row(t + STEP + lane, id1, b1) : NO_ROW;
         id1 = id2;
-        pv1 = pv2;
         b1 = lk.block(id1);
-        lk.column(t + 3 * STEP + lane, id2, pv2);
+        id2 = lk.column(t + 3 * STEP + lane);
         load(row);
       }
       wave_lds_sync();
@@ -670,10 +735,12 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
   const int t0 = y / a.v.nkv * JOIN_P;
   if (t0 >= places) return;
   const Segment sg{b, j, n, 0, 0, places};
-  const Lookup lk(a, sg);
-  int id[U], prev[U], blk[U];
+  Lookup lk(a, sg);
+  const int p0 = t0 + 64 * wave;                       // this wave's places: from here, and 256 on
+  int id[U], blk[U];
+  const typename Lookup::Start st = lk.start(p0);
 #pragma unroll
-  for (int i = 0; i < U; ++i) lk.column(t0 + i * 256 + tid, id[i], prev[i]);
+  for (int i = 0; i < U; ++i) id[i] = lk.column(t0 + i * 256 + tid);
 #pragma unroll
   for (int i = 0; i < U; ++i) blk[i] = lk.block(id[i]);
   __shared__ float lse[CACHE_MAXG];
@@ -684,9 +751,11 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
   }
   uint32_t row[U];
   float old[U];
+  lk.begin(p0, st);
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    row[i] = lk.row(t0 + i * 256 + tid, id[i], prev[i], blk[i]);
+    lk.advance(p0 + i * 256, 64);
+    row[i] = lk.row(t0 + i * 256 + tid, id[i], blk[i]);
     old[i] = a.weights[row[i] == NO_ROW ? 0 : row[i]];
   }
   __syncthreads();
@@ -1053,18 +1122,6 @@ __global__ __launch_bounds__(256, G > 4 ? 2 : 3) void k_cache_score(CacheSelect 
   }
 }
 
-// Inclusive sum over the lanes below, in a wave (DPP: within rows of 16
-// lanes, then the last lane of a row to the next row, then of the first half
-// to the second).
-__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);    // row_shr:1
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);    // row_shr:2
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);    // row_shr:4
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);    // row_shr:8
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);   // row_bcast:15
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);   // row_bcast:31
-  return v;
-}
 // the smallest of the wave, in every lane
 __device__ __forceinline__ uint32_t wave_least(uint32_t v) {
   v = min(v, dpp_u32<DPP_QUAD_XOR1>(v));

@@ -393,6 +393,61 @@ def test_attend_flags_what_it_cannot_read():
     c.close()
 
 
+def entries_read(lst, n_blocks):
+    """Of a block list, the entries that are larger than all before them, up
+    to the first -1; the others as -1."""
+    top, out = -1, []
+    for i in lst:
+        out.append(i if top < i < n_blocks else -1)
+        top = max(top, 2 ** 31 if i == -1 else i)
+    return out
+
+
+def check_malformed(c, lists):
+    q = c.normal((c.B, c.nq, c.d), 2.0)
+    read = np.array([[entries_read(row, -(-c.n_lens[b] // c.bs)) for row in rows] for b, rows in enumerate(lists)])
+    bl = torch.tensor(lists, dtype=torch.int32, device=DEV)
+    check_attend(c, q, c.dr.cache_attend(c.kv(), q, blocks=bl, lse=True), blocks=read)
+    assert c.dr.device_status() == -1
+    w = c.weights()
+    w0 = w.clone()
+    check_attend(c, q, c.dr.cache_attend(c.kv(), q, blocks=bl, weights=w, lse=True), blocks=read, w=w, w0=w0)
+    assert c.dr.device_status() == -1
+
+
+@pytest.mark.parametrize("bad", [[3, -1, 3, -1], [3, 1, 3, -1], [0, 5, 3, 5], [5, 3, 4, -1], [-1, 0, -1, 2], [0, 1, -5, 1],
+                                 [1, 2 ** 31 - 1, 2, -1], [6, 0, 7, 6], [-2 ** 31, 0, 0, -1]])
+def test_attend_reads_no_block_of_a_list_twice(bad):
+    """whatever stands between the repeats."""
+    c = Cache(8, 2, 64, "bf16", 16, [100, 100], 8)
+    check_malformed(c, [[bad, bad], [bad, [0, 1, 6, -1]]])
+    c.close()
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (4, 1, 128, "f32"), (2, 1, 256, "bf16")])
+@pytest.mark.parametrize("bs,n", [(1, 130), (1, 500), (1, 700), (4, 128), (4, 300), (16, 150)])
+def test_attend_long_malformed_lists(heads, bs, n):
+    """Lists of more entries than a wave looks at together, each with an entry
+    out of its order, by one workgroup each and joined."""
+    lens = [bs * 900, bs * 800 - 1, bs * 700, bs * 900, bs * 650 + 1]
+    c = Cache(*heads, bs, lens, 900)
+    lists = []
+    for b in range(c.B):
+        rows = []
+        for j in range(c.nkv):
+            m = int(c.rng.integers(n // 2, n + 1))
+            row = np.full(n, -1, np.int64)
+            row[:m] = np.sort(c.rng.choice(-(-lens[b] // bs), m, replace=False))
+            at = [int(c.rng.integers(1, m)), m - 1, m // 2, 66, 64][b]
+            row[at] = [row[int(c.rng.integers(0, at))], row[0], -1, 10 ** 6, -7][b]
+            if b == 2:
+                row[m - 1] = row[3]                          # behind the -1
+            rows.append(row.tolist())
+        lists.append(rows)
+    check_malformed(c, lists)
+    c.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attend_infinities_and_nan(dtype):
     """-inf scores take no part; a row of them gives zeros; NaN in a visible
