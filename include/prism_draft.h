@@ -410,9 +410,9 @@ prism_status prism_verify_tree(prism_ctx *ctx, int32_t batch, int32_t n_nodes,
  *     visible slots, 0 .. n_b - 1.  n_b = 0 is allowed.
  *   - max_len: an upper bound of every n_b known to the host, 1..capacity
  *     (max_blocks_per_seq * kv_block_size); 0 = the capacity.  It sizes the
- *     launches and the scratch.  A longer sequence is cut to it, and a
- *     negative length taken as 0; both raise PRISM_ERR_CAPACITY in
- *     prism_device_status.
+ *     launches and the scratch.  A longer sequence is cut to it, and one of
+ *     negative L_b has no visible slot, whatever n_new; both raise
+ *     PRISM_ERR_CAPACITY in prism_device_status.
  *   - d_scratch: device memory of the caller's, at least prism_cache_scratch()
  *     bytes (0: it may be NULL), 16-byte aligned, written and read by the one
  *     call only (calls on several streams, and captured graphs that may

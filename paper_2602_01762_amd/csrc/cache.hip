@@ -14,12 +14,13 @@ namespace prism {
 constexpr uint32_t NO_ROW = 0xffffffffu;   // a slot without storage
 
 // Slots of sequence b that a call sees: its context plus n_new, at most
-// max_len.  A negative length counts as none; a longer one is cut.  Both flag.
+// max_len.  With a negative context it sees none; a longer one is cut.  Both flag.
 __device__ __forceinline__ int visible_slots(const CacheView &v, int b, uint32_t *err) {
-  const long n = (long)v.kv.ctx_lens[b] + v.n_new;
-  if (n < 0 || n > v.max_len) {
+  const int L = v.kv.ctx_lens[b];
+  const long n = (long)L + v.n_new;
+  if (L < 0 || n > v.max_len) {
     atomicOr(err, ERRF_CAPACITY);
-    return n < 0 ? 0 : v.max_len;
+    return L < 0 ? 0 : v.max_len;
   }
   return (int)n;
 }

@@ -547,6 +547,41 @@ def test_attend_rows_beyond_four_gigabytes():
     c.close()
 
 
+@pytest.mark.parametrize("L", [-1, -3, -2 ** 31])
+@pytest.mark.parametrize("n_new", [1, 5])
+def test_a_negative_length_sees_nothing(L, n_new):
+    """also with new slots behind it, and is flagged by every call."""
+    c = Cache(8, 2, 64, "bf16", 16, [40, 40], 4)
+    q, w = c.normal((2, 8, 64)), c.weights()
+    s0 = torch.full((c.k.shape[0], c.nkv, 2, c.d), 3.0, dtype=c.dt, device=DEV)
+    c.lens.copy_(torch.tensor([40 - n_new, 40 - n_new], dtype=torch.int32))
+    ref = c.dr.cache_attend(c.kv(), q, n_new=n_new)["out"]
+    s_ref = c.dr.cache_summarize(c.kv(), s0.clone(), n_new=n_new)
+    blocks_ref = c.dr.cache_select(c.kv(), q, s_ref, 2, n_new=n_new)
+    assert c.dr.device_status() == 0
+    c.lens[0] = L
+    w0 = w.clone()
+    lst = torch.tensor([[[0, 1, -1]] * 2] * 2, dtype=torch.int32, device=DEV)
+    lst[0] = -1
+    for kw in (dict(), dict(weights=w), dict(blocks=lst), dict(max_len=40)):
+        r = c.dr.cache_attend(c.kv(), q, n_new=n_new, lse=True, **kw)
+        assert c.dr.device_status() == -7
+        assert float(r["out"][0].float().abs().max()) == 0.0 and torch.isneginf(r["lse"][0]).all()
+        if "blocks" not in kw and "weights" not in kw:
+            assert torch.equal(r["out"][1], ref[1])
+    first = torch.tensor(c.table_h[0], device=DEV)
+    assert torch.equal(w[first], w0[first])
+    s = c.dr.cache_summarize(c.kv(), s0.clone(), n_new=n_new)
+    assert c.dr.device_status() == -7
+    assert float((s[first] - 3).abs().max()) == 0.0
+    other = torch.tensor(c.table_h[1], device=DEV)
+    assert torch.equal(s[other].view(torch.int16), s_ref[other].view(torch.int16))
+    blocks = c.dr.cache_select(c.kv(), q, s_ref, 2, n_new=n_new)
+    assert c.dr.device_status() == -7
+    assert (blocks[0] == -1).all() and torch.equal(blocks[1], blocks_ref[1])
+    c.close()
+
+
 # ------------------------------------------------- summaries and selection
 @pytest.mark.parametrize("heads", HEADS)
 @pytest.mark.parametrize("bs", [16, 7])
