@@ -534,7 +534,9 @@ prism_status prism_cache_attend(prism_ctx *ctx, const prism_cache_attention *io,
  * maximum of each channel over the block's visible keys (NaN passed over),
  * [n_pool_blocks, n_kv_heads, 2, d] in the context dtype.  span > 0: only the
  * blocks that hold the last span visible slots (those that changed since the
- * last call); 0: every block. */
+ * last call); 0: every block of the capacity is looked at.  A block that stands
+ * in the tables of several sequences has one summary: every one of them sees
+ * the same number of its slots (a full block of a shared prefix, say). */
 prism_status prism_cache_summarize(prism_ctx *ctx, const prism_batch *kv, int32_t n_new,
                                    int32_t span, void *d_summary, void *stream);
 

@@ -905,6 +905,32 @@ def test_blocks_that_the_pool_does_not_hold():
     c.close()
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (6, 2, 32, "f32")])
+def test_sequences_that_share_a_prefix(heads):
+    """Full blocks in the tables of several sequences are read, summarised,
+    chosen and evicted from for each."""
+    c = Cache(*heads, 16, [150, 100, 48, 49], 10, spare=4 * 3)
+    for b in (1, 2, 3):
+        c.table_h[b, :3] = c.table_h[0, :3]
+        for i in range(3, -(-c.n_lens[b] // 16)):           # (its own blocks hold slots already)
+            assert not torch.isnan(c.k[int(c.table_h[b, i]), :, 0].float()).any()
+    c.table.copy_(torch.tensor(c.table_h, dtype=torch.int32))
+    q = c.normal((c.B, c.nq, c.d), 2.0)
+    check_attend(c, q, c.dr.cache_attend(c.kv(), q, lse=True))
+    s = c.dr.cache_summarize(c.kv(), c.dr.summary_buffer(c.kv()))
+    got, kh = f64(s), f64(c.k)
+    for b, L in enumerate(c.n_lens):
+        for j in range(c.nkv):
+            want = C.summarize(c.rows(kh, b, j, np.arange(L)), 16)
+            assert np.array_equal(got[c.table_h[b, : len(want)], j], want)
+    again = s.clone()
+    c.dr.cache_summarize(c.kv(), again, span=60)
+    assert torch.equal(again, s)
+    check_select(c, q, s, c.dr.cache_select(c.kv(), q, s, 3, 1, 1), 3, 1, 1)
+    check_evict(c, c.weights(0.1), 40, 2, 9)
+    c.close()
+
+
 def test_a_drafting_batch_serves_the_cache_calls():
     from paper_2602_01762_amd import Drafter
     from synth import SMALL_BF16_CHAIN, make_inputs
