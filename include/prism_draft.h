@@ -394,10 +394,11 @@ prism_status prism_verify_tree(prism_ctx *ctx, int32_t batch, int32_t n_nodes,
  * beside the drafting calls: rows appended with per-head norms and rotation,
  * attention of one new token per sequence over the whole cache or over a list
  * of its blocks, block summaries and the choice of blocks by them, and
- * eviction by accumulated attention weight.  They need a context's shape and
- * no weights, work on the device the context was created on (another current
- * device is refused), and take prism_batch with d_tokens and d_features unused
- * (NULL allowed).  Conventions of all of them:
+ * eviction by accumulated attention weight.  They serve a layer that the caller
+ * runs beside the library on the same pools; no drafting call uses them.  They
+ * need a context's shape and no weights, work on the device the context was
+ * created on (another current device is refused), and take prism_batch with
+ * d_tokens and d_features unused (NULL allowed).  Conventions of all of them:
  *   - Rows (projections, queries, outputs), gains and summaries are in the
  *     context dtype; sums, softmax statistics and slot weights are fp32 or
  *     wider.  Matrix and pool pointers are 16-byte aligned; tensors are
@@ -552,7 +553,10 @@ prism_status prism_cache_select(prism_ctx *ctx, const prism_cache_selection *io,
  * values and weights, in slot order, to the blocks of d_new_table.  The old
  * blocks are left as they are, and so are the slots of the new ones behind
  * d_new_lens[b].  Keys keep the rotation of their old positions: continue with
- * explicit positions (prism_cache_append, prism_draft_step). */
+ * explicit positions (prism_cache_append, prism_draft_step).  The chain and tree
+ * calls and prism_score_tree rotate at L_b, which then lies before positions
+ * that the kept keys carry.  Rows appended since d_ctx_lens was last advanced
+ * are no candidates. */
 prism_status prism_cache_evict(prism_ctx *ctx, const prism_cache_eviction *io, void *stream);
 
 /* Synchronize `stream` and report device-side flags raised since the last

@@ -418,8 +418,10 @@ class Drafter:
     def cache_evict(self, kv, new_table, weights, n_keep: int, n_first: int = 0, n_recent: int = 0,
                     max_len: int = 0):
         """Copy the n_keep slots of largest weight to the blocks of new_table
-        [B, max_blocks_per_seq].  Returns kept [B, n_kv, n_keep] (old slots)
-        and lens [B], the lengths of the new cache."""
+        [B, max_blocks_per_seq].  Advance lens over appended rows before: the
+        candidates are the slots below them.  Returns kept [B, n_kv, n_keep]
+        (old slots) and lens [B], the lengths of the new cache; kept keys keep
+        the rotation of their old positions (continue with explicit ones)."""
         nb = kv.nb
         io = self._io[3]
         io.kv = ctypes.addressof(kv)

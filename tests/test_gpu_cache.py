@@ -856,6 +856,48 @@ def test_drafting_goes_on_over_an_evicted_cache():
     dr.close()
 
 
+def test_drafting_at_the_true_positions_after_an_eviction():
+    """The kept keys carry the rotation of their old positions: draft steps at
+    the positions that follow those, in the slots that follow the kept ones,
+    equal the oracle's."""
+    from harness import LOGIT_TOL, check_draft_kv, check_token, oracle_for
+    from paper_2602_01762_amd import Drafter
+    from synth import SMALL_BF16_CHAIN, make_inputs, make_weights
+    cfg = SMALL_BF16_CHAIN.with_(batch=2, ctx_range=(200, 333), n_steps=3)
+    wt, inp = make_weights(cfg, DEV), make_inputs(cfg, DEV, extra_blocks=2 * 6)
+    dr = Drafter(cfg)
+    dr.load(wt)
+    used = set(inp.block_table.flatten().tolist())
+    free = [i for i in range(inp.k_pool.shape[0]) if i not in used]
+    new = torch.full_like(inp.block_table, -1)
+    new[:, :6] = torch.tensor(free[:12], dtype=torch.int32).view(2, 6)
+    w = torch.rand(inp.k_pool.shape[:3], device=DEV)
+    kv = dr.cache(inp.ctx_lens, inp.k_pool, inp.v_pool, inp.block_table)
+    r = dr.cache_evict(kv, new, w, 77, n_first=4, n_recent=20)
+    old = inp.ctx_lens.clone()
+    inp.block_table, inp.ctx_lens = new, r["lens"]
+    assert (old > inp.ctx_lens).all()
+    orc, hi = oracle_for(cfg, wt, inp)
+    caches = [orc.new_cache(hi, b) for b in range(2)]
+    tokens, feat, want_feat = inp.tokens, inp.features, f64(inp.features)
+    for k in range(3):
+        rows = {"tokens": tokens, "feat": feat, "seq": torch.arange(2, dtype=torch.int32, device=DEV),
+                "pos": old + k, "slot": inp.ctx_lens + k}
+        st = dr.step(k + 1, inp, rows, logits=True)
+        torch.cuda.synchronize()
+        assert dr.device_status() == 0
+        slots = [int(n) + k for n in inp.ctx_lens]
+        h, lg = orc.forward(cfg.fmap[k], tokens.tolist(), want_feat, [int(n) + k for n in old], caches, [0, 1], slots,
+                            [list(range(s + 1)) for s in slots])
+        got = st["logits"].cpu().numpy()
+        assert np.max(np.abs(got - lg)) <= LOGIT_TOL[cfg.dtype]
+        for b in range(2):
+            check_token(lg[b], int(st["ids"][b, 0]), "seq %d step %d" % (b, k + 1))
+        tokens, feat, want_feat = st["ids"][:, 0].contiguous(), st["hidden"], h
+    check_draft_kv(cfg, inp, {b: caches[b]["draft"] for b in range(2)}, [0, 1])
+    dr.close()
+
+
 @pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (8, 1, 128, "f32")])
 def test_a_batch_without_any_slot(heads):
     c = Cache(*heads, 16, [0, 0, 0], 4, spare=6)
