@@ -898,6 +898,22 @@ def test_drafting_at_the_true_positions_after_an_eviction():
     dr.close()
 
 
+def test_a_row_appended_in_the_same_step_is_kept():
+    """Append, attention and eviction of one decoding step: once the lengths
+    have been advanced, the new row is a candidate, and the most recent one."""
+    c = Cache(8, 2, 64, "bf16", 16, [100, 47], 8, spare=4)
+    w = torch.zeros(c.k.shape[:3], device=DEV)
+    kv = c.kv()
+    q = c.dr.cache_append(kv, c.normal((2, 12 * 64)), weights=w)
+    c.dr.cache_attend(kv, q, n_new=1, weights=w)
+    c.lens += 1
+    c.n_lens = [101, 48]
+    r, _ = check_evict(c, w, 32, 4, 8)
+    assert r["lens"].tolist() == [32, 32]
+    assert (r["kept"][0, :, -1] == 100).all() and (r["kept"][1, :, -1] == 47).all()
+    c.close()
+
+
 @pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (8, 1, 128, "f32")])
 def test_a_batch_without_any_slot(heads):
     c = Cache(*heads, 16, [0, 0, 0], 4, spare=6)
