@@ -250,7 +250,7 @@ __device__ __forceinline__ Walk walk_of(const CacheAttend &a) {
   const bool has = lane < a.v.kv.n_seq;
   Walk w;
   w.n = has ? visible_slots(a.v, lane, a.err) : 0;
-  w.count = has ? (places_of(a, w.n) + CACHE_GRAN - 1) / CACHE_GRAN : 0;
+  w.count = has ? cache_granules(places_of(a, w.n)) : 0;
   if (a.direct && has) w.count = 1;            // an empty sequence writes its zeros itself
   w.end = w.count * a.v.nkv;
   for (int x = 1; x < a.v.kv.n_seq; x *= 2) {
@@ -260,7 +260,7 @@ __device__ __forceinline__ Walk walk_of(const CacheAttend &a) {
   w.total = __builtin_amdgcn_readlane(w.end, a.v.kv.n_seq - 1);
   if (!has) w.end = w.total;
   w.begin = w.end - w.count * a.v.nkv;
-  w.per = max(1, (w.total + a.waves - 1) / a.waves);
+  w.per = cache_run(w.total, a.waves);
   return w;
 }
 // Where the score of place p and head h of a KV head is kept: 16 places of all
@@ -279,11 +279,11 @@ __device__ __forceinline__ Segment segment_at(const CacheAttend &a, const Walk &
   const int count = __builtin_amdgcn_readlane(w.count, s.b);
   const int at = u - __builtin_amdgcn_readlane(w.begin, s.b);
   s.n = __builtin_amdgcn_readlane(w.n, s.b);
-  s.j = at / count;
-  const int first = at - s.j * count;
-  s.granules = min(last - u, count - first);
-  s.p0 = first * CACHE_GRAN;                   // (0 in a direct call, whose one granule is the segment)
-  s.p1 = a.direct ? places_of(a, s.n) : min(places_of(a, s.n), (first + s.granules) * CACHE_GRAN);
+  const CacheRun run = cache_run_at(at, count, last - u);
+  s.j = run.head;
+  s.granules = run.granules;
+  s.p0 = run.first * CACHE_GRAN;               // (0 in a direct call, whose one granule is the segment)
+  s.p1 = a.direct ? places_of(a, s.n) : min(places_of(a, s.n), (run.first + s.granules) * CACHE_GRAN);
   return s;
 }
 
@@ -635,7 +635,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_cache_
       return;                                          // one segment per workgroup
     }
     if (col >= g) continue;
-    const size_t part = (size_t)(blockIdx.x + sg.b * a.v.nkv + sg.j) * g + col;
+    const size_t part = (size_t)cache_partial(blockIdx.x, sg.b * a.v.nkv + sg.j) * g + col;
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(a.po + part * D + 16 * dt + 4 * q4) = o[dt];
     if (q4 == 0) {
@@ -652,8 +652,8 @@ struct Parts {
 };
 __device__ __forceinline__ Parts parts_of(const CacheAttend &a, const Walk &w, int b, int j, int h) {
   const int count = __builtin_amdgcn_readlane(w.count, b);
-  const int u = __builtin_amdgcn_readlane(w.begin, b) + j * count, w0 = u / w.per;
-  return {(size_t)(w0 + b * a.v.nkv + j) * a.g + h, count ? (u + count - 1) / w.per - w0 + 1 : 0};
+  const CacheParts p = cache_parts(__builtin_amdgcn_readlane(w.begin, b) + j * count, count, w.per);
+  return {(size_t)cache_partial(p.wave, b * a.v.nkv + j) * a.g + h, p.n};
 }
 // From every lane of a wave: the largest maximum M (0 if there is none) and
 // the sum l of 2^(m_c - M) l_c.

@@ -368,24 +368,49 @@ constexpr int CACHE_WAVES = 2048;   // 8 waves on each of 256 CUs, the most that
 // 10.8), and up to CACHE_DIRECT_MANY where CACHE_DIRECT_UNITS segments fill the
 // chip (256 segments of 1024: 25.7 us, joined 29.7; of 1 .. 1024: 22.8 and 21.6).
 constexpr int CACHE_DIRECT = 512, CACHE_DIRECT_MANY = 1024, CACHE_DIRECT_UNITS = 256;
+// The arithmetic of the runs, which kernels, runtime and tests share.  Granules
+// of a segment (a sequence's KV head) and of a wave's run:
+constexpr int cache_granules(int places) { return (places + CACHE_GRAN - 1) / CACHE_GRAN; }
+constexpr int cache_run(int total, int waves) { return total > waves ? (total - 1) / waves + 1 : 1; }
 struct CachePlan {
   int waves;
   bool direct;
 };
 inline CachePlan cache_plan(int units, int span, bool weights) {
   if (span <= (units >= CACHE_DIRECT_UNITS ? CACHE_DIRECT_MANY : CACHE_DIRECT) && !weights) return {units, true};
-  const long granules = (long)units * ((span + CACHE_GRAN - 1) / CACHE_GRAN);
+  const long granules = (long)units * cache_granules(span);
   return {(int)(granules < CACHE_WAVES ? granules : CACHE_WAVES), false};
 }
+// The part of a segment that the run with `left` granules to go begins with, at
+// granule `at` of a sequence whose heads have `count` each.
+struct CacheRun {
+  int head, first, granules;
+};
+constexpr CacheRun cache_run_at(int at, int count, int left) {
+  const int head = at / count, first = at - head * count;
+  return {head, first, left < count - first ? left : count - first};
+}
+// Partial of a wave for a segment (units: segments before it): along the runs
+// each step moves on one wave or one segment, so no two share one.
+constexpr int cache_partial(int wave, int segment) { return wave + segment; }
+constexpr int cache_partials(int waves, int units) { return waves + units; }
+// The waves whose runs touch the segment of `count` granules from `begin` on.
+struct CacheParts {
+  int wave, n;
+};
+constexpr CacheParts cache_parts(int begin, int count, int run) {
+  const int wave = begin / run;
+  return {wave, count ? (begin + count - 1) / run - wave + 1 : 0};
+}
 // row length of the scores kept for the slot weights: whole granules
-inline int cache_score_row(int span) { return (span + CACHE_GRAN - 1) / CACHE_GRAN * CACHE_GRAN; }
+inline int cache_score_row(int span) { return cache_granules(span) * CACHE_GRAN; }
 // Scratch bytes of an attention call over `batch` sequences with nkv KV heads of
 // g query heads and d channels: two statistics and an output of each partial
 // (256-byte aligned runs), and the kept scores.
 inline size_t cache_attend_scratch(int batch, int nkv, int g, int d, int span, bool weights) {
   const CachePlan p = cache_plan(batch * nkv, span, weights);
   if (p.direct) return 0;
-  const size_t parts = (size_t)(p.waves + batch * nkv) * g, pad = 255;
+  const size_t parts = (size_t)cache_partials(p.waves, batch * nkv) * g, pad = 255;
   size_t n = ((parts * 4 + pad) & ~pad) * 2 + ((parts * d * 4 + pad) & ~pad);
   if (weights) n += (size_t)batch * nkv * g * cache_score_row(span) * 4;
   return n;

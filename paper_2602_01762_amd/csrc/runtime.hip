@@ -1598,7 +1598,7 @@ prism_status prism_cache_attend(prism_ctx *c, const prism_cache_attention *io, v
   a.waves = p.waves;
   a.direct = p.direct;
   a.scale = 1.4426950408889634f / sqrtf((float)c->d);
-  const size_t parts = (size_t)(p.waves + B * c->nkv) * a.g;
+  const size_t parts = (size_t)cache_partials(p.waves, B * c->nkv) * a.g;
   char *ws = (char *)io->d_scratch;
   carve(ws, (void **)&a.pm, parts * 4);
   carve(ws, (void **)&a.pl, parts * 4);

@@ -254,3 +254,71 @@ int main() {
     subprocess.run(["g++", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2602_01762_amd", "csrc"), str(src),
                     "-o", str(exe)], check=True)
     assert subprocess.run([str(exe)]).returncode == 0
+
+
+def test_attention_runs_by_the_functions_that_the_kernels_call(tmp_path):
+    """Over random lengths, with plan.h's own numbering: every granule is one
+    run's, no two runs share a partial, all lie inside the scratch, and the
+    join's range of a segment holds its partials, in order and no others."""
+    src, exe = tmp_path / "runs.cc", tmp_path / "runs"
+    src.write_text(r"""
+#include <cstdlib>
+#include <vector>
+#include "plan.h"
+using namespace prism;
+int main() {
+  srand(2);
+  for (int it = 0; it < 4000; ++it) {
+    const int B = 1 + rand() % 64, nkv = 1 + rand() % 8, top = 1 << (rand() % 18), g = 1 + rand() % 8, d = 32 << (rand() % 4);
+    std::vector<int> len(B);
+    int span = 1;
+    for (int &n : len) { n = rand() % 3 ? rand() % (top + 1) : 0; span = n > span ? n : span; }
+    const bool weights = rand() % 2;
+    const CachePlan p = cache_plan(B * nkv, span, weights);
+    std::vector<int> begin(B), count(B);
+    int total = 0;
+    for (int b = 0; b < B; ++b) {
+      count[b] = p.direct ? 1 : cache_granules(len[b]);
+      begin[b] = total;
+      total += count[b] * nkv;
+    }
+    const int run = cache_run(total, p.waves);
+    if ((long)run * p.waves < total) return 1;
+    std::vector<int> owner(cache_partials(p.waves, B * nkv), -1), seen(total, 0);
+    const size_t bytes = cache_attend_scratch(B, nkv, g, d, span, weights);
+    if (p.direct ? bytes : bytes < owner.size() * g * (d + 2) * 4 + (weights ? (size_t)B * nkv * g * span * 4 : 0)) return 2;
+    for (int w = 0; w < p.waves; ++w) {
+      int u = w * run;
+      const int last = u + run < total ? u + run : total;
+      while (u < last) {
+        int b = 0;
+        while (begin[b] + count[b] * nkv <= u) ++b;
+        const CacheRun r = cache_run_at(u - begin[b], count[b], last - u);
+        if (r.granules < 1 || r.head >= nkv) return 3;
+        for (int i = 0; i < r.granules; ++i) {
+          if (begin[b] + r.head * count[b] + r.first + i != u + i) return 4;
+          ++seen[u + i];
+        }
+        const int part = cache_partial(w, b * nkv + r.head);
+        if (part >= (int)owner.size() || owner[part] != -1) return 5;
+        owner[part] = b * nkv + r.head;
+        u += r.granules;
+      }
+    }
+    for (int s : seen) if (s != 1) return 6;
+    int joined = 0;
+    for (int b = 0; b < B; ++b)
+      for (int j = 0; j < nkv; ++j) {
+        const CacheParts c = cache_parts(begin[b] + j * count[b], count[b], run);
+        for (int i = 0; i < c.n; ++i, ++joined)
+          if (owner[cache_partial(c.wave, b * nkv + j) + i] != b * nkv + j) return 7;
+      }
+    for (int o : owner) joined -= o >= 0;
+    if (joined) return 8;
+  }
+  return 0;
+}
+""")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2602_01762_amd", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)]).returncode == 0
