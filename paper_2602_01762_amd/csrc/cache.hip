@@ -6,6 +6,7 @@
 //
 // Pools are [block, KV head, slot in block, d]: row (block, head, slot) of a
 // pool seen as [rows, d] has a 32-bit index (the runtime refuses larger pools).
+#include "cache.h"
 #include "device.h"
 #include "rotation.h"
 

@@ -13,7 +13,7 @@
 #include <vector>
 
 #include "prism_draft.h"
-#include "internal.h"
+#include "cache.h"
 
 using namespace prism;
 

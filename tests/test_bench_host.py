@@ -1,5 +1,6 @@
 """Host-side logic of bench.py: the LM head's launch plan and algorithmic
 bytes, the counter-figure digest, and the refusal of several GPUs."""
+import json
 import os
 import subprocess
 import sys
@@ -90,3 +91,15 @@ def test_reported_kernels_exist():
     defined = set(re.findall(r"\b(k_\w+)\s*\(", src))
     named = set(re.findall(r"\bk_[a-z]\w*", open(os.path.join(ROOT, "bench.py")).read())) - {"k_lmhead_traffic"}
     assert named and named <= defined, sorted(named - defined)
+
+
+def test_counter_figures_belong_to_the_present_kernel():
+    """The figures that the benchmark reports were taken on this LM-head code,
+    whose headers hold nothing of the long-context cache (its changes would
+    make the figures stale)."""
+    with open(bench.TRAFFIC_FILE) as f:
+        assert bench.lm_traffic(L3_8B_BS1) == json.load(f)["bytes_per_launch"]
+    for name in ("internal.h", "plan.h"):
+        with open(os.path.join(ROOT, "paper_2602_01762_amd", "csrc", name)) as f:
+            code = [ln.split("//", 1)[0] for ln in f]
+        assert not any("Cache" in ln or "CACHE" in ln for ln in code), name
