@@ -9,13 +9,18 @@ namespace prism {
 // a KV head of up to `span` places: the waves that share the granules of
 // CACHE_GRAN places.
 constexpr int CACHE_GRAN = 64;      // whole tiles of every attention kernel
-constexpr int CACHE_WAVES = 2048;   // 8 waves on each of 256 CUs, the most that are resident: each
-                                    // pays its first lookups once.  32 sequences of 32768 slots:
-                                    // 670 us, with 4096 waves 691, with 8192 724
+// That many are resident at once (8 on each of 256 CUs, two per SIMD; 4 where a
+// row of 1024 bytes, fp32 and d = 256, takes more than half a SIMD's registers),
+// and each pays its first lookups once.  32 sequences of 32768 slots, 64 query
+// heads: 669 us, with 1024 waves 680, 4096 690, 8192 726; fp32 with d = 256, one
+// sequence of 32768: 72 us, with 2048 waves 90.
+constexpr int CACHE_WAVES = 2048;
+constexpr int cache_waves(int row_bytes) { return row_bytes > 512 ? CACHE_WAVES / 2 : CACHE_WAVES; }
 // A direct call gives each segment to one workgroup, which needs no join: up to
-// CACHE_DIRECT places (8 segments of 512: 10.4 us, joined 10.9; of 768: 14.0 and
-// 10.8), and up to CACHE_DIRECT_MANY where CACHE_DIRECT_UNITS segments fill the
-// chip (256 segments of 1024: 25.7 us, joined 29.7; of 1 .. 1024: 22.8 and 21.6).
+// CACHE_DIRECT places (128 segments of 512: 13.0 us, joined 14.4; 8 of 512: 10.6
+// and 10.5, of 768: 14.4 and 11.2), and up to CACHE_DIRECT_MANY where CACHE_DIRECT_UNITS segments fill
+// the chip (256 segments of 1024: 25.7 us, joined 30.1; of 1 .. 1024, whose
+// lengths the host does not know: 23.0 and 21.9).
 constexpr int CACHE_DIRECT = 512, CACHE_DIRECT_MANY = 1024, CACHE_DIRECT_UNITS = 256;
 // The arithmetic of the runs, which kernels, runtime and tests share.  Granules
 // of a segment (a sequence's KV head) and of a wave's run:
@@ -25,10 +30,10 @@ struct CachePlan {
   int waves;
   bool direct;
 };
-inline CachePlan cache_plan(int units, int span, bool weights) {
+inline CachePlan cache_plan(int units, int span, bool weights, int waves = CACHE_WAVES) {
   if (span <= (units >= CACHE_DIRECT_UNITS ? CACHE_DIRECT_MANY : CACHE_DIRECT) && !weights) return {units, true};
   const long granules = (long)units * cache_granules(span);
-  return {(int)(granules < CACHE_WAVES ? granules : CACHE_WAVES), false};
+  return {(int)(granules < waves ? granules : waves), false};
 }
 // The part of a segment that the run with `left` granules to go begins with, at
 // granule `at` of a sequence whose heads have `count` each.
@@ -54,10 +59,10 @@ constexpr CacheParts cache_parts(int begin, int count, int run) {
 // row length of the scores kept for the slot weights: whole granules
 inline int cache_score_row(int span) { return cache_granules(span) * CACHE_GRAN; }
 // Scratch bytes of an attention call over `batch` sequences with nkv KV heads of
-// g query heads and d channels: two statistics and an output of each partial
+// g query heads and d channels, shared by at most `waves` waves: two statistics and an output of each partial
 // (256-byte aligned runs), and the kept scores.
-inline size_t cache_attend_scratch(int batch, int nkv, int g, int d, int span, bool weights) {
-  const CachePlan p = cache_plan(batch * nkv, span, weights);
+inline size_t cache_attend_scratch(int batch, int nkv, int g, int d, int span, bool weights, int waves = CACHE_WAVES) {
+  const CachePlan p = cache_plan(batch * nkv, span, weights, waves);
   if (p.direct) return 0;
   const size_t parts = (size_t)cache_partials(p.waves, batch * nkv) * g, pad = 255;
   size_t n = ((parts * 4 + pad) & ~pad) * 2 + ((parts * d * 4 + pad) & ~pad);
@@ -66,10 +71,11 @@ inline size_t cache_attend_scratch(int batch, int nkv, int g, int d, int span, b
 }
 // The most that any batch up to this one takes: a larger one may be direct, and
 // take none, where a smaller one is not.
-inline size_t cache_attend_scratch_up_to(int batch, int nkv, int g, int d, int span, bool weights) {
+inline size_t cache_attend_scratch_up_to(int batch, int nkv, int g, int d, int span, bool weights,
+                                         int waves = CACHE_WAVES) {
   size_t most = 0;
   for (int b = 1; b <= batch; ++b) {
-    const size_t n = cache_attend_scratch(b, nkv, g, d, span, weights);
+    const size_t n = cache_attend_scratch(b, nkv, g, d, span, weights, waves);
     most = n > most ? n : most;
   }
   return most;

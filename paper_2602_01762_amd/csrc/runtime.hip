@@ -1537,7 +1537,8 @@ prism_status prism_cache_scratch(prism_ctx *c, int32_t call, int32_t batch, int3
   CHECK(check_len(c, 0, max_len, &len));
   if (call == PRISM_CACHE_SELECT) *bytes = select_scratch(c, batch, len);
   else if (call == PRISM_CACHE_EVICT) *bytes = choose_scratch((size_t)batch * c->nkv, len);
-  else *bytes = cache_attend_scratch_up_to(batch, c->nkv, c->nq / c->nkv, c->d, len, call == PRISM_CACHE_ATTEND_WEIGHTS);
+  else *bytes = cache_attend_scratch_up_to(batch, c->nkv, c->nq / c->nkv, c->d, len, call == PRISM_CACHE_ATTEND_WEIGHTS,
+                                           cache_waves(c->d * c->esz));
   return PRISM_OK;
 }
 
@@ -1583,9 +1584,11 @@ prism_status prism_cache_attend(prism_ctx *c, const prism_cache_attention *io, v
     return fail(c, PRISM_ERR_INVALID_ARG, "n_blocks %d", io->n_blocks);
   const int B = io->kv->batch;
   const int span = io->d_blocks ? std::min(io->n_blocks, c->cfg.max_blocks_per_seq) * c->cfg.kv_block_size : len;
+  const bool weights = io->d_weights != nullptr;
+  const int waves = cache_waves(c->d * c->esz);
   CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes,
-                      cache_attend_scratch(B, c->nkv, c->nq / c->nkv, c->d, span, io->d_weights != nullptr)));
-  const CachePlan p = cache_plan(B * c->nkv, span, io->d_weights != nullptr);
+                      cache_attend_scratch(B, c->nkv, c->nq / c->nkv, c->d, span, weights, waves)));
+  const CachePlan p = cache_plan(B * c->nkv, span, weights, waves);
   CacheAttend a{};
   a.v = cache_view(c, io->kv, io->n_new, len);
   a.nq = c->nq;

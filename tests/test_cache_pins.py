@@ -274,7 +274,9 @@ int main() {
     int span = 1;
     for (int &n : len) { n = rand() % 3 ? rand() % (top + 1) : 0; span = n > span ? n : span; }
     const bool weights = rand() % 2;
-    const CachePlan p = cache_plan(B * nkv, span, weights);
+    const int waves = cache_waves(d * (rand() % 2 ? 4 : 2));
+    const CachePlan p = cache_plan(B * nkv, span, weights, waves);
+    if (p.waves > (p.direct ? B * nkv : waves)) return 9;
     std::vector<int> begin(B), count(B);
     int total = 0;
     for (int b = 0; b < B; ++b) {
@@ -285,7 +287,7 @@ int main() {
     const int run = cache_run(total, p.waves);
     if ((long)run * p.waves < total) return 1;
     std::vector<int> owner(cache_partials(p.waves, B * nkv), -1), seen(total, 0);
-    const size_t bytes = cache_attend_scratch(B, nkv, g, d, span, weights);
+    const size_t bytes = cache_attend_scratch(B, nkv, g, d, span, weights, waves);
     if (p.direct ? bytes : bytes < owner.size() * g * (d + 2) * 4 + (weights ? (size_t)B * nkv * g * span * 4 : 0)) return 2;
     for (int w = 0; w < p.waves; ++w) {
       int u = w * run;
