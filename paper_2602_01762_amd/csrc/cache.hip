@@ -671,8 +671,8 @@ __device__ __forceinline__ void join_stats(const CacheAttend &a, const Parts &p,
 
 // Join: T threads per query head add its partial outputs, each weighted by
 // 2^(its maximum - the largest one), in an order that only the lengths set:
-// a wave where a head has few partials, so that no barrier is needed, a
-// workgroup where it has many.  The first loads go out before the statistics
+// a wave where the heads have few partials on average, so that no barrier is
+// needed, a workgroup where they have many.  The first loads go out before the statistics
 // are known.  Workgroups past the heads (with slot weights) take JOIN_P places
 // of one KV head each: the sum over its g heads of 2^(score - log-sum) is
 // added to the place's slot, which one thread owns.
@@ -776,7 +776,10 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttend a) {
 }
 template <typename T, int D>
 static void join_d(const CacheAttend &a, hipStream_t s) {
-  // partials of a head on average: a wave adds 64 / (D / 4) at a time
+  // partials of a head on average (a wave adds 64 / (D / 4) at a time; the host
+  // does not know the lengths).  A wave each: 32 sequences of 32768 slots 665 us,
+  // by workgroups 671; but one of 131072 among 63 of 256, whose heads have
+  // hundreds where the average is 4, 120 and 113
   const bool few = a.waves / (a.v.nkv * a.v.kv.n_seq) <= 16;
   const int per = few ? 4 : 1;
   const dim3 g((a.nq + per - 1) / per + (a.weights ? a.v.nkv * ((a.span + JOIN_P - 1) / JOIN_P) : 0), a.v.kv.n_seq);
@@ -1152,9 +1155,9 @@ __device__ __forceinline__ uint32_t sum_before(const uint32_t *v, int entries, i
 // that add to one counter queue); else every pass streams
 // them (from the L2 after the first).  WEIGHTS (with LDS): the keys are made
 // here from the slot weights.
-//   One workgroup's instructions bound it: 512 cycles per instruction of a
-// pass over 131072 keys.  8192 blocks 10 us (13 with a loop per digit over all
-// keys and sums over the waves in loops).
+//   One workgroup's instructions and its barriers bound it: 8 of 256 CUs are at
+// work for 8 heads.  128 of 8192 blocks 8.7 us, 1024 of 4096 slots (keys from
+// the weights) 9.8.
 constexpr int CHOOSE_T = 1024, CHOOSE_W = CHOOSE_T / 64;
 constexpr int CHOOSE_LIST = 8192;
 // One key's digit counted.  Many lanes with one digit (equal keys: unweighted
