@@ -1048,6 +1048,60 @@ def test_calls_repeat_bit_for_bit_and_replay_in_a_graph():
     c.close()
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (8, 1, 128, "f32")])
+def test_a_decoding_step_replays_in_two_graphs(heads):
+    """Append, weighted attention, summaries, selection and the attention over
+    the chosen blocks, captured once for each of two halves of a batch that
+    share the pools; replayed at once on two streams, over growing lengths,
+    with eager steps of a copy between the replays."""
+    lens = [0, 700, 15, 333]
+    a, b = (Cache(*heads, 16, lens, 48, seed=5) for _ in range(2))
+    width = (a.nq + 2 * a.nkv) * a.d
+    qkv = a.normal((6, 4, width))
+    w = [torch.zeros(c.k.shape[:3], device=DEV) for c in (a, b)]
+    s = [c.dr.cache_summarize(c.kv(), c.dr.summary_buffer(c.kv())) for c in (a, b)]
+    kvs = [[c.dr.cache(c.lens[i: i + 2], c.k, c.v, c.table[i: i + 2]) for i in (0, 2)] for c in (a, b)]
+    rows = [torch.empty((2, width), dtype=a.dt, device=DEV) for _ in range(2)]
+
+    def step(c, x, half, src):
+        kv = kvs[x][half]
+        q = c.dr.cache_append(kv, src, weights=w[x])
+        full = c.dr.cache_attend(kv, q, n_new=1, weights=w[x], lse=True)
+        c.dr.cache_summarize(kv, s[x], n_new=1, span=1)
+        blocks = c.dr.cache_select(kv, q, s[x], 5, 1, 1, n_new=1)
+        part = c.dr.cache_attend(kv, q, n_new=1, blocks=blocks)["out"]
+        return [q, full["out"], full["lse"], blocks, part]
+
+    def same(x, y):
+        return torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for half in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step(a, 0, half, rows[half]))
+        graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i in range(6):
+        for half in range(2):
+            rows[half].copy_(qkv[i, 2 * half: 2 * half + 2])
+        torch.cuda.synchronize()
+        for half, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                graphs[half].replay()
+        torch.cuda.synchronize()
+        for half in range(2):
+            want = step(b, 1, half, qkv[i, 2 * half: 2 * half + 2].contiguous())
+            assert all(same(x, y) for x, y in zip(outs[half], want)), (i, half)
+        for x, y in ((a.k, b.k), (a.v, b.v), (w[0], w[1]), (s[0], s[1])):
+            assert same(x, y), i
+        a.lens += 1
+        b.lens += 1
+    a.close()
+    b.close()
+
+
 def test_two_streams_at_once():
     """Calls of one context on two streams do not share anything."""
     c = Cache(8, 2, 64, "bf16", 16, [3000, 2000], 190)
