@@ -559,12 +559,109 @@ prism_status prism_cache_select(prism_ctx *ctx, const prism_cache_selection *io,
  * are no candidates. */
 prism_status prism_cache_evict(prism_ctx *ctx, const prism_cache_eviction *io, void *stream);
 
+/* ---- The cache in 8 bits, and attention of several rows --------------------
+ * A second form of the paged cache beside the pools of the context dtype: codes
+ * of 8 bits (e4m3: 1 sign, 4 exponent and 3 fraction bits, largest 448, no
+ * infinity) and one scale per pool block, KV head and pool.  A block's scale is
+ * 2^e with the least e in -110..119 for which the largest finite magnitude of its
+ * rows is at most 448 * 2^e; a code is value / scale rounded to the nearest, ties
+ * to even.  A value that is not finite is held as NaN; larger ones than 448 *
+ * 2^119 as that.  When rows are written behind others of a block, its scale stays
+ * or grows; if it grows, the codes that it holds are rounded again to the new scale
+ * (which changes none but those that become subnormal, below 2^-6 of it).
+ * The conventions of the long-context draft cache hold, and:
+ *   - Codes and scales are 16-byte aligned; scales of blocks that hold rows are as
+ *     these calls write them.
+ *   - No other call takes this cache: drafting, block lists, slot weights and
+ *     eviction need the context dtype (prism_cache8_unpack). */
+typedef struct {
+  int32_t batch;                /* B <= max_batch                            */
+  const int32_t *d_ctx_lens;    /* [B] slots held L_b                        */
+  void *d_k_codes, *d_v_codes;  /* [n_pool_blocks, n_kv_heads, kv_block_size,
+                                   d] e4m3                                   */
+  float *d_scales;              /* [n_pool_blocks, n_kv_heads, 2] of keys and
+                                   of values                                 */
+  const int32_t *d_block_table; /* [B, max_blocks_per_seq]                   */
+  int32_t n_pool_blocks;
+} prism_cache8;
+
+/* prism_cache_rows without slot weights. */
+typedef struct {
+  const prism_cache8 *kv8;
+  int32_t rows;                 /* T >= 1                                    */
+  const int32_t *d_offsets;     /* [B + 1], or NULL: one row each, T = B     */
+  const int32_t *d_positions;   /* [B], or NULL: L_b                         */
+  const void *d_qkv;            /* [T, (n_q_heads + 2 n_kv_heads) * d]       */
+  const void *d_q_gain;         /* [d], or NULL: no norm                     */
+  const void *d_k_gain;
+  void *d_q;                    /* [T, n_q_heads * d] queries out            */
+} prism_cache8_rows;
+
+/* Slots d_start[b] .. n_b - 1 of every sequence, n_b = L_b + n_new of kv8. */
+typedef struct {
+  const prism_cache8 *kv8;
+  const prism_batch *kv;        /* the same sequences, in blocks of their own;
+                                   its lengths are not read                  */
+  int32_t n_new, max_len;
+  const int32_t *d_start;       /* [B] >= 0 (from n_b on: nothing), or NULL: 0 */
+} prism_cache8_move;
+
+/* Attention of d_offsets[b+1] - d_offsets[b] rows of each sequence. */
+typedef struct {
+  const prism_batch *kv;        /* the cache of the context dtype, or        */
+  const prism_cache8 *kv8;      /* the 8-bit one: the other is NULL          */
+  int32_t rows;                 /* T >= 1                                    */
+  const int32_t *d_offsets;     /* [B + 1] as in prism_cache_rows, or NULL:
+                                   one row each, T = B                       */
+  int32_t n_new;                /* row i of sequence b sees the slots below
+                                   v = L_b + n_new + i: 1 where the rows are
+                                   in the cache and L_b does not count them  */
+  int32_t max_len;              /* bound of every v                          */
+  int32_t window;               /* 0: all those slots; else those from v -
+                                   window on, and                            */
+  int32_t n_first;              /* the first n_first                         */
+  const void *d_q;              /* [T, n_q_heads * d], rotated               */
+  void *d_out;                  /* [T, n_q_heads * d]                        */
+  float *d_lse;                 /* [T, n_q_heads] log of the sum of exp(q.k /
+                                   sqrt(d)), or NULL                         */
+  void *d_scratch;              /* prism_cache_rows_scratch                  */
+  uint64_t scratch_bytes;
+} prism_cache_row_attention;
+
+/* prism_cache_append to the 8-bit cache: normalised and rotated keys, and values,
+ * as codes; the arithmetic of the keys is fp64, so each is rounded once. */
+prism_status prism_cache8_append(prism_ctx *ctx, const prism_cache8_rows *io, void *stream);
+
+/* Write slots of the cache of the context dtype to the 8-bit one, at the same slots
+ * (d_start[b] inside a block: the rows before it stay, at the scale that the
+ * block then has), and back.  Reading back gives code * scale, which the context
+ * dtype holds exactly.  Other slots stay as they are.  A block that receives
+ * slots stands once in the block table that they go to.  A negative d_start
+ * raises PRISM_ERR_INVALID_ARG in prism_device_status and moves nothing. */
+prism_status prism_cache8_pack(prism_ctx *ctx, const prism_cache8_move *io, void *stream);
+prism_status prism_cache8_unpack(prism_ctx *ctx, const prism_cache8_move *io, void *stream);
+
+/* Scratch bytes of one prism_cache_attend_rows call over up to `batch` sequences
+ * and `rows` rows (the most that any smaller call takes too, whatever its window). */
+prism_status prism_cache_rows_scratch(prism_ctx *ctx, int32_t batch, int32_t rows,
+                                      int32_t max_len, uint64_t *bytes);
+
+/* out = softmax(q K^T / sqrt(d)) V of every row over the slots that it sees: a
+ * token, drafts to be scored, prompts, in one batch.  A row that sees nothing, or
+ * whose every score is -inf, gives zeros and a log-sum of -inf.  What a row does
+ * not see does not reach it, also where it is infinite or NaN; infinite values as
+ * in prism_cache_attend.  Rows behind the last sequence are left alone.  A
+ * malformed d_offsets raises PRISM_ERR_INVALID_ARG in prism_device_status and
+ * writes nothing. */
+prism_status prism_cache_attend_rows(prism_ctx *ctx, const prism_cache_row_attention *io,
+                                     void *stream);
+
 /* Synchronize `stream` and report device-side flags raised since the last
  * call, the first that applies of: PRISM_ERR_NONFINITE (a row whose logits
  * are all NaN, or a NaN tree score: the tokens of such a row are
  * unspecified and may lie outside 0..V-1; other rows are unaffected),
  * PRISM_ERR_INVALID_ARG (malformed catch-up offsets, tree-scoring rows, cache
- * offsets or block lists),
+ * offsets, starts or block lists),
  * PRISM_ERR_CAPACITY
  * (block table / pool / slot out of range), PRISM_ERR_INVALID_ARG (token id
  * out of range), else PRISM_OK.  Clears the flags. */

@@ -27,6 +27,8 @@ EXPORTS = ("prism_create", "prism_destroy", "prism_last_error", "prism_draft_loa
            "prism_verify_tree",
            "prism_cache_scratch", "prism_cache_append", "prism_cache_attend",
            "prism_cache_summarize", "prism_cache_select", "prism_cache_evict",
+           "prism_cache8_append", "prism_cache8_pack", "prism_cache8_unpack",
+           "prism_cache_rows_scratch", "prism_cache_attend_rows",
            "prism_device_status",
            "prism_profile_enable", "prism_profile_read", "prism_profile_pairs",
            "prism_graph_cache")
@@ -99,6 +101,27 @@ class prism_cache_eviction(ctypes.Structure):
                 ("d_kept", c_vp), ("d_new_lens", c_vp), ("d_scratch", c_vp), ("scratch_bytes", c_u64)]
 
 
+class prism_cache8(ctypes.Structure):
+    _fields_ = [("batch", c_i32), ("d_ctx_lens", c_vp), ("d_k_codes", c_vp), ("d_v_codes", c_vp),
+                ("d_scales", c_vp), ("d_block_table", c_vp), ("n_pool_blocks", c_i32)]
+
+
+# kv8, kv: ctypes.addressof() of structs that outlive the call
+class prism_cache8_rows(ctypes.Structure):
+    _fields_ = [("kv8", c_vp), ("rows", c_i32), ("d_offsets", c_vp), ("d_positions", c_vp),
+                ("d_qkv", c_vp), ("d_q_gain", c_vp), ("d_k_gain", c_vp), ("d_q", c_vp)]
+
+
+class prism_cache8_move(ctypes.Structure):
+    _fields_ = [("kv8", c_vp), ("kv", c_vp), ("n_new", c_i32), ("max_len", c_i32), ("d_start", c_vp)]
+
+
+class prism_cache_row_attention(ctypes.Structure):
+    _fields_ = [("kv", c_vp), ("kv8", c_vp), ("rows", c_i32), ("d_offsets", c_vp), ("n_new", c_i32),
+                ("max_len", c_i32), ("window", c_i32), ("n_first", c_i32), ("d_q", c_vp),
+                ("d_out", c_vp), ("d_lse", c_vp), ("d_scratch", c_vp), ("scratch_bytes", c_u64)]
+
+
 class PrismError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__("%s: %s" % (STATUS.get(status, status), msg))
@@ -145,6 +168,11 @@ def lib():
         L.prism_cache_summarize.argtypes = [c_vp, P(prism_batch), c_i32, c_i32, c_vp, c_vp]
         L.prism_cache_select.argtypes = [c_vp, P(prism_cache_selection), c_vp]
         L.prism_cache_evict.argtypes = [c_vp, P(prism_cache_eviction), c_vp]
+        L.prism_cache8_append.argtypes = [c_vp, P(prism_cache8_rows), c_vp]
+        L.prism_cache8_pack.argtypes = [c_vp, P(prism_cache8_move), c_vp]
+        L.prism_cache8_unpack.argtypes = [c_vp, P(prism_cache8_move), c_vp]
+        L.prism_cache_rows_scratch.argtypes = [c_vp, c_i32, c_i32, c_i32, P(c_u64)]
+        L.prism_cache_attend_rows.argtypes = [c_vp, P(prism_cache_row_attention), c_vp]
         L.prism_device_status.argtypes = [c_vp, c_vp]
         L.prism_profile_enable.argtypes = [c_vp, c_i32]
         L.prism_profile_read.argtypes = [c_vp, P(c_f32), P(c_i32)]
@@ -298,6 +326,29 @@ def prism_cache_select(ctx, io: prism_cache_selection, stream=None):
 
 def prism_cache_evict(ctx, io: prism_cache_eviction, stream=None):
     _check(lib().prism_cache_evict(ctx, ctypes.byref(io), cur_stream() if stream is None else stream), ctx)
+
+
+def prism_cache8_append(ctx, io: prism_cache8_rows, stream=None):
+    _check(lib().prism_cache8_append(ctx, ctypes.byref(io), cur_stream() if stream is None else stream), ctx)
+
+
+def prism_cache8_pack(ctx, io: prism_cache8_move, stream=None):
+    _check(lib().prism_cache8_pack(ctx, ctypes.byref(io), cur_stream() if stream is None else stream), ctx)
+
+
+def prism_cache8_unpack(ctx, io: prism_cache8_move, stream=None):
+    _check(lib().prism_cache8_unpack(ctx, ctypes.byref(io), cur_stream() if stream is None else stream), ctx)
+
+
+def prism_cache_rows_scratch(ctx, batch: int, rows: int, max_len: int = 0) -> int:
+    """Scratch bytes of a prism_cache_attend_rows call."""
+    n = c_u64()
+    _check(lib().prism_cache_rows_scratch(ctx, batch, rows, max_len, ctypes.byref(n)), ctx)
+    return n.value
+
+
+def prism_cache_attend_rows(ctx, io: prism_cache_row_attention, stream=None):
+    _check(lib().prism_cache_attend_rows(ctx, ctypes.byref(io), cur_stream() if stream is None else stream), ctx)
 
 
 def prism_device_status(ctx, stream=None) -> int:

@@ -1,5 +1,5 @@
 // Declarations of the long-context draft cache, shared by its kernels
-// (cache.hip) and the runtime.
+// (cache.hip, cache8.hip, rows.hip) and the runtime.
 #pragma once
 #include "internal.h"
 
@@ -87,5 +87,48 @@ struct CacheEvict {
   uint32_t *err;
 };
 void launch_cache_evict(bool bf16, const CacheEvict &a, int d, hipStream_t s);
+
+// ---- the 8-bit cache: the pools of a view are codes (e4m3), beside them the
+// scales of the pool blocks, [n_blocks, nkv, 2] (keys, values)
+struct Cache8Append {
+  CacheView v;
+  float *scales;
+  int rows, nq;
+  const int32_t *offsets, *positions;   // [B + 1] / [B], or NULL
+  const void *qkv;                      // [rows, (nq + 2 nkv) d]
+  const void *q_gain, *k_gain;          // [d] or NULL
+  void *q;                              // [rows, nq d]
+  const double *inv_freq;
+  float eps;
+  uint32_t *err;
+};
+void launch_cache8_append(bool bf16, const Cache8Append &a, int d, hipStream_t s);
+struct Cache8Move {
+  CacheView v;                          // the 8-bit cache
+  KvArgs kv;                            // the cache of the context's type
+  float *scales;
+  const int32_t *start;                 // [B] first slot, or NULL
+  uint32_t *err;
+};
+void launch_cache8_pack(bool bf16, const Cache8Move &a, int d, hipStream_t s);
+void launch_cache8_unpack(bool bf16, const Cache8Move &a, int d, hipStream_t s);
+
+// ---- attention of several rows per sequence
+struct RowsAttend {
+  CacheView v;
+  const float *scales;                  // of an 8-bit cache, or NULL
+  int rows;
+  const int32_t *offsets;               // [B + 1], or NULL: one row each
+  int window, n_first;                  // window 0: every slot
+  int nq, g, d;
+  const void *q;                        // [rows, nq, d]
+  int waves, segments;                  // rows_plan
+  bool direct;
+  float scale;                          // log2(e) / sqrt(d)
+  float *pm, *pl, *po;                  // partials [waves + segments][columns] / [.., d]
+  void *out; float *lse;                // [rows, nq, d] / [rows, nq] or NULL
+  uint32_t *err;
+};
+void launch_rows_attend(bool bf16, const RowsAttend &a, hipStream_t s);
 
 }  // namespace prism

@@ -81,6 +81,45 @@ inline size_t cache_attend_scratch_up_to(int batch, int nkv, int g, int d, int s
   return most;
 }
 
+// Attention of several rows per sequence: rows whose (row, head) pairs of a KV head
+// fill the 16 columns of a matrix-core tile, and the tiles (segments, over all KV
+// heads) that T rows of B sequences can make: a sequence's last one may be short.
+constexpr int rows_per_tile(int g) { return 16 / g; }
+inline long rows_segments(int nkv, int g, int batch, int rows) {
+  const long tiles = (long)rows / rows_per_tile(g) + batch;
+  return (tiles < rows ? tiles : rows) * nkv;
+}
+// Places of a segment at most.
+inline int rows_span(int g, int max_len, int window, int n_first) {
+  const long w = window ? (long)window + n_first + rows_per_tile(g) - 1 : max_len;
+  return (int)(w < max_len ? w : max_len);
+}
+// A workgroup for each segment, and no join, where segments are short or fill the
+// chip by themselves; else equal runs of granules for all waves, as above.
+constexpr int ROWS_DIRECT_SEGMENTS = 2048;
+struct RowsPlan {
+  int segments, waves;
+  bool direct;
+};
+inline RowsPlan rows_plan(int nkv, int g, int batch, int rows, int span, int waves) {
+  const long n = rows_segments(nkv, g, batch, rows);
+  if (span <= CACHE_DIRECT || n >= ROWS_DIRECT_SEGMENTS) return {(int)n, (int)n, true};
+  const long granules = n * cache_granules(span);
+  return {(int)n, (int)(granules < waves ? granules : waves), false};
+}
+inline size_t rows_scratch(int g, int d, const RowsPlan &p) {
+  if (p.direct) return 0;
+  const size_t parts = (size_t)cache_partials(p.waves, p.segments) * rows_per_tile(g) * g, pad = 255;
+  return ((parts * 4 + pad) & ~pad) * 2 + ((parts * d * 4 + pad) & ~pad);
+}
+// The most that any call over up to `batch` sequences and `rows` rows takes.
+inline size_t rows_scratch_up_to(int nkv, int g, int d, int batch, int rows, int max_len, int waves) {
+  if (max_len <= CACHE_DIRECT) return 0;
+  const long n = rows_segments(nkv, g, batch, rows);
+  const int most = (int)(n < ROWS_DIRECT_SEGMENTS ? n : ROWS_DIRECT_SEGMENTS - 1);
+  return rows_scratch(g, d, {most, waves, false});
+}
+
 // Table columns per wave of the passes over the blocks of a cache (summaries,
 // scores), for units * columns of them at most: about `waves` waves, a multiple
 // of `step` columns (those of one load), at most `top` <= 64 (one lane looks up

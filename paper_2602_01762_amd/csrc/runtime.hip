@@ -1719,6 +1719,156 @@ prism_status prism_cache_evict(prism_ctx *c, const prism_cache_eviction *io, voi
   return PRISM_OK;
 }
 
+// ---- the 8-bit cache
+static prism_status check_cache8(prism_ctx *c, const prism_cache8 *k) {
+  if (!k) return fail(c, PRISM_ERR_INVALID_ARG, "kv8 is NULL");
+  if (k->batch < 1 || k->batch > c->cfg.max_batch)
+    return fail(c, PRISM_ERR_INVALID_ARG, "batch %d out of 1..%d", k->batch, c->cfg.max_batch);
+  if (!k->d_ctx_lens || !k->d_k_codes || !k->d_v_codes || !k->d_scales || !k->d_block_table || k->n_pool_blocks < 1)
+    return fail(c, PRISM_ERR_INVALID_ARG, "incomplete description of the 8-bit cache");
+  if (((uintptr_t)k->d_k_codes | (uintptr_t)k->d_v_codes | (uintptr_t)k->d_scales) & 15)
+    return fail(c, PRISM_ERR_INVALID_ARG, "codes and scales must be 16-byte aligned");
+  if ((double)k->n_pool_blocks * c->nkv * c->cfg.kv_block_size >= 4294967295.0)
+    return fail(c, PRISM_ERR_SHAPE, "KV pools of 2^32 rows or more");
+  int dev = -1;
+  HIPCHK(c, hipGetDevice(&dev));
+  if (dev != c->dev)
+    return fail(c, PRISM_ERR_INVALID_ARG, "current device %d, but the context is on device %d", dev, c->dev);
+  return PRISM_OK;
+}
+// the view of an 8-bit cache: its pools are the codes
+static CacheView cache8_view(const prism_ctx *c, const prism_cache8 *k, int n_new, int max_len) {
+  prism_batch b{};
+  b.batch = k->batch;
+  b.d_ctx_lens = k->d_ctx_lens;
+  b.d_k_pool = k->d_k_codes;
+  b.d_v_pool = k->d_v_codes;
+  b.d_block_table = k->d_block_table;
+  b.n_pool_blocks = k->n_pool_blocks;
+  return cache_view(c, &b, n_new, max_len);
+}
+
+prism_status prism_cache8_append(prism_ctx *c, const prism_cache8_rows *io, void *stream) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  if (!io) return fail(c, PRISM_ERR_INVALID_ARG, "io is NULL");
+  CHECK(check_cache8(c, io->kv8));
+  if (io->rows < 1) return fail(c, PRISM_ERR_INVALID_ARG, "rows %d", io->rows);
+  if (!io->d_offsets && io->rows != io->kv8->batch)
+    return fail(c, PRISM_ERR_INVALID_ARG, "%d rows without offsets for a batch of %d", io->rows, io->kv8->batch);
+  CHECK(check_rows(c, io->d_qkv, "d_qkv"));
+  CHECK(check_rows(c, io->d_q, "d_q"));
+  if (((uintptr_t)io->d_q_gain | (uintptr_t)io->d_k_gain) & 15)
+    return fail(c, PRISM_ERR_INVALID_ARG, "gains must be 16-byte aligned");
+  Cache8Append a{};
+  a.v = cache8_view(c, io->kv8, 0, c->max_slots);
+  a.scales = io->kv8->d_scales;
+  a.rows = io->rows;
+  a.nq = c->nq;
+  a.offsets = io->d_offsets;
+  a.positions = io->d_positions;
+  a.qkv = io->d_qkv;
+  a.q_gain = io->d_q_gain;
+  a.k_gain = io->d_k_gain;
+  a.q = io->d_q;
+  a.inv_freq = c->inv_freq;
+  a.eps = c->cfg.rms_eps;
+  a.err = c->err;
+  launch_cache8_append(c->bf16, a, c->d, (hipStream_t)stream);
+  HIPCHK(c, hipGetLastError());
+  return PRISM_OK;
+}
+
+static prism_status cache8_move(prism_ctx *c, const prism_cache8_move *io, bool unpack, void *stream) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  if (!io) return fail(c, PRISM_ERR_INVALID_ARG, "io is NULL");
+  CHECK(check_cache8(c, io->kv8));
+  CHECK(check_cache(c, io->kv));
+  if (io->kv->batch != io->kv8->batch)
+    return fail(c, PRISM_ERR_INVALID_ARG, "%d sequences in one cache, %d in the other", io->kv->batch, io->kv8->batch);
+  int len = 0;
+  CHECK(check_len(c, io->n_new, io->max_len, &len));
+  Cache8Move a{};
+  a.v = cache8_view(c, io->kv8, io->n_new, len);
+  a.kv = kv_of(c, io->kv);
+  a.scales = io->kv8->d_scales;
+  a.start = io->d_start;
+  a.err = c->err;
+  if (unpack) launch_cache8_unpack(c->bf16, a, c->d, (hipStream_t)stream);
+  else launch_cache8_pack(c->bf16, a, c->d, (hipStream_t)stream);
+  HIPCHK(c, hipGetLastError());
+  return PRISM_OK;
+}
+prism_status prism_cache8_pack(prism_ctx *c, const prism_cache8_move *io, void *stream) {
+  return cache8_move(c, io, false, stream);
+}
+prism_status prism_cache8_unpack(prism_ctx *c, const prism_cache8_move *io, void *stream) {
+  return cache8_move(c, io, true, stream);
+}
+
+// ---- attention of several rows per sequence
+prism_status prism_cache_rows_scratch(prism_ctx *c, int32_t batch, int32_t rows, int32_t max_len, uint64_t *bytes) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  if (!bytes) return fail(c, PRISM_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = 0;
+  if (batch < 1 || batch > c->cfg.max_batch)
+    return fail(c, PRISM_ERR_INVALID_ARG, "batch %d out of 1..%d", batch, c->cfg.max_batch);
+  if (rows < 1) return fail(c, PRISM_ERR_INVALID_ARG, "rows %d", rows);
+  int len = 0;
+  CHECK(check_len(c, 0, max_len, &len));
+  *bytes = rows_scratch_up_to(c->nkv, c->nq / c->nkv, c->d, batch, rows, len, cache_waves(c->d * c->esz));
+  return PRISM_OK;
+}
+
+prism_status prism_cache_attend_rows(prism_ctx *c, const prism_cache_row_attention *io, void *stream) {
+  if (!c) return PRISM_ERR_INVALID_ARG;
+  if (!io) return fail(c, PRISM_ERR_INVALID_ARG, "io is NULL");
+  if (!io->kv == !io->kv8) return fail(c, PRISM_ERR_INVALID_ARG, "one of kv and kv8 is given");
+  if (io->kv8) CHECK(check_cache8(c, io->kv8));
+  else CHECK(check_cache(c, io->kv));
+  const int B = io->kv8 ? io->kv8->batch : io->kv->batch, g = c->nq / c->nkv;
+  int len = 0;
+  CHECK(check_len(c, io->n_new, io->max_len, &len));
+  if (io->rows < 1) return fail(c, PRISM_ERR_INVALID_ARG, "rows %d", io->rows);
+  if (!io->d_offsets && io->rows != B)
+    return fail(c, PRISM_ERR_INVALID_ARG, "%d rows without offsets for a batch of %d", io->rows, B);
+  if (io->window < 0 || io->n_first < 0)
+    return fail(c, PRISM_ERR_INVALID_ARG, "window %d, n_first %d", io->window, io->n_first);
+  if ((long)io->rows * c->nq >= 1l << 30) return fail(c, PRISM_ERR_SHAPE, "%d rows of %d heads", io->rows, c->nq);
+  CHECK(check_rows(c, io->d_q, "d_q"));
+  CHECK(check_rows(c, io->d_out, "d_out"));
+  const RowsPlan p = rows_plan(c->nkv, g, B, io->rows, rows_span(g, len, io->window, io->n_first),
+                               cache_waves(c->d * c->esz));
+  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, rows_scratch(g, c->d, p)));
+  RowsAttend a{};
+  a.v = io->kv8 ? cache8_view(c, io->kv8, io->n_new, len) : cache_view(c, io->kv, io->n_new, len);
+  a.scales = io->kv8 ? io->kv8->d_scales : nullptr;
+  a.rows = io->rows;
+  a.offsets = io->d_offsets;
+  a.window = io->window;
+  a.n_first = io->n_first;
+  a.nq = c->nq;
+  a.g = g;
+  a.d = c->d;
+  a.q = io->d_q;
+  a.waves = p.waves;
+  a.segments = p.segments;
+  a.direct = p.direct;
+  a.scale = 1.4426950408889634f / sqrtf((float)c->d);
+  if (!p.direct) {
+    const size_t parts = (size_t)cache_partials(p.waves, p.segments) * rows_per_tile(g) * g;
+    char *ws = (char *)io->d_scratch;
+    carve(ws, (void **)&a.pm, parts * 4);
+    carve(ws, (void **)&a.pl, parts * 4);
+    carve(ws, (void **)&a.po, parts * c->d * 4);
+  }
+  a.out = io->d_out;
+  a.lse = io->d_lse;
+  a.err = c->err;
+  launch_rows_attend(c->bf16, a, (hipStream_t)stream);
+  HIPCHK(c, hipGetLastError());
+  return PRISM_OK;
+}
+
 prism_status prism_device_status(prism_ctx *c, void *stream) {
   if (!c) return PRISM_ERR_INVALID_ARG;
   HIPCHK(c, hipStreamSynchronize((hipStream_t)stream));
@@ -1728,7 +1878,7 @@ prism_status prism_device_status(prism_ctx *c, void *stream) {
   if (flags & ERRF_NONFINITE)
     return fail(c, PRISM_ERR_NONFINITE, "NaN logits or tree scores (NaN in a feature row or a weight)");
   if (flags & ERRF_ROWS)
-    return fail(c, PRISM_ERR_INVALID_ARG, "malformed catch-up offsets, tree-scoring rows, cache offsets or block lists");
+    return fail(c, PRISM_ERR_INVALID_ARG, "malformed catch-up offsets, tree-scoring rows, cache offsets, starts or block lists");
   if (flags & ERRF_CAPACITY) return fail(c, PRISM_ERR_CAPACITY, "KV slot, block or pool out of range");
   if (flags & ERRF_TOKEN) return fail(c, PRISM_ERR_INVALID_ARG, "token id out of range");
   return PRISM_OK;

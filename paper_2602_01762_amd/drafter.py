@@ -256,7 +256,8 @@ class Drafter:
         self._bs, self._columns = c.kv_block_size, c.max_blocks_per_seq
         self._qkv = (self._nq + 2 * self._nkv) * self._d
         self._io = (B.prism_cache_rows(), B.prism_cache_attention(), B.prism_cache_selection(),
-                    B.prism_cache_eviction())
+                    B.prism_cache_eviction(), B.prism_cache8_rows(), B.prism_cache8_move(),
+                    B.prism_cache_row_attention())
         self._scratch_bytes = {}
 
     def _stream(self) -> int:
@@ -280,11 +281,20 @@ class Drafter:
             raise ValueError("%s must be contiguous" % name)
         return t.data_ptr()          # a subclass of Tensor
 
-    def _scratch(self, call: int, batch: int, max_len: int, like):
-        key = (call, batch, max_len)
+    @staticmethod
+    def _kind(kv, cls):
+        """A call's sequences, of the cache it works on."""
+        if type(kv) is not cls:
+            raise TypeError("a %s is needed, not %s" % (cls.__name__, type(kv).__name__))
+        return kv
+
+    def _scratch(self, call, batch: int, max_len: int, like, rows: int = 0):
+        """call: PRISM_CACHE_*, or None: the attention of `rows` rows."""
+        key = (call, batch, max_len, rows)
         n = self._scratch_bytes.get(key)
         if n is None:
-            n = B.prism_cache_scratch(self.ctx, call, batch, max_len)
+            n = (B.prism_cache_rows_scratch(self.ctx, batch, rows, max_len) if call is None
+                 else B.prism_cache_scratch(self.ctx, call, batch, max_len))
             if len(self._scratch_bytes) >= 1024:      # callers that pass a new bound at every step
                 self._scratch_bytes.clear()
             self._scratch_bytes[key] = n
@@ -322,7 +332,7 @@ class Drafter:
         queries [T, n_q, d]."""
         dt, T = self._dt, qkv.shape[0]
         io = self._io[0]
-        io.kv = ctypes.addressof(kv)
+        io.kv = ctypes.addressof(self._kind(kv, B.prism_batch))
         io.rows = T
         io.d_qkv = self._expect(qkv, "qkv", (T, self._qkv), dt)
         io.d_q_gain = None if q_gain is None else self._expect(q_gain, "q_gain", (self._d,), dt)
@@ -350,7 +360,7 @@ class Drafter:
         dt, nb = self._dt, kv.nb
         shape = (nb, self._nq, self._d)
         io = self._io[1]
-        io.kv = ctypes.addressof(kv)
+        io.kv = ctypes.addressof(self._kind(kv, B.prism_batch))
         io.n_new = n_new
         io.max_len = span = max_len
         io.d_q = self._expect(q, "q", shape, dt)
@@ -386,7 +396,7 @@ class Drafter:
     def cache_summarize(self, kv, summary, n_new: int = 0, span: int = 0):
         """Write the key minima and maxima of the blocks that hold the last
         span slots (0: of every block) into summary [blocks, n_kv, 2, d]."""
-        self._expect(summary, "summary", kv.summary, self._dt)
+        self._expect(summary, "summary", self._kind(kv, B.prism_batch).summary, self._dt)
         B.prism_cache_summarize(self.ctx, kv, n_new, span, summary, self._stream())
         return summary
 
@@ -396,7 +406,7 @@ class Drafter:
         head, [B, n_kv, n_blocks] int32: increasing, then -1."""
         nb = kv.nb
         io = self._io[2]
-        io.kv = ctypes.addressof(kv)
+        io.kv = ctypes.addressof(self._kind(kv, B.prism_batch))
         io.n_new = n_new
         io.max_len = max_len
         io.d_q = self._expect(q, "q", (nb, self._nq, self._d), self._dt)
@@ -424,7 +434,7 @@ class Drafter:
         the rotation of their old positions (continue with explicit ones)."""
         nb = kv.nb
         io = self._io[3]
-        io.kv = ctypes.addressof(kv)
+        io.kv = ctypes.addressof(self._kind(kv, B.prism_batch))
         io.max_len = max_len
         io.d_new_table = self._expect(new_table, "new_table", (nb, self._columns), torch.int32)
         io.d_weights = self._expect(weights, "weights", kv.slots, torch.float32)
@@ -439,6 +449,107 @@ class Drafter:
         io.d_scratch = scratch.data_ptr()
         B.prism_cache_evict(self.ctx, io, self._stream())
         return {"kept": kept, "lens": lens}
+
+    # the cache in 8 bits, attention of several rows -----------------------------
+    def cache8_buffers(self, n_blocks: int):
+        """Pools of an 8-bit cache: k and v codes [n_blocks, n_kv, kv_block_size,
+        head_dim] (torch.float8_e4m3fn) and scales [n_blocks, n_kv, 2] fp32."""
+        k, v = (torch.zeros((n_blocks, self._nkv, self._bs, self._d), dtype=torch.uint8,
+                            device=self.device).view(torch.float8_e4m3fn) for _ in range(2))
+        return k, v, torch.ones((n_blocks, self._nkv, 2), dtype=torch.float32, device=self.device)
+
+    def cache8(self, lens, k_codes, v_codes, scales, block_table) -> B.prism_cache8:
+        """The sequences of a call over an 8-bit cache: lens [B] int32 slots held,
+        pools as cache8_buffers() makes them, block_table [B, max_blocks_per_seq]
+        int32.  Keeps the tensors alive."""
+        nb, n = int(lens.shape[0]), int(k_codes.shape[0])
+        pool = (n, self._nkv, self._bs, self._d)
+        kv = B.prism_cache8()
+        kv.batch = nb
+        kv.d_ctx_lens = self._expect(lens, "lens", (nb,), torch.int32)
+        kv.d_k_codes = self._expect(k_codes, "k_codes", pool, torch.float8_e4m3fn)
+        kv.d_v_codes = self._expect(v_codes, "v_codes", pool, torch.float8_e4m3fn)
+        kv.d_scales = self._expect(scales, "scales", (n, self._nkv, 2), torch.float32)
+        kv.d_block_table = self._expect(block_table, "block_table", (nb, self._columns), torch.int32)
+        kv.n_pool_blocks = n
+        kv.tensors = (lens, k_codes, v_codes, scales, block_table)
+        kv.nb = nb
+        return kv
+
+    def cache8_append(self, kv8, qkv, q_gain=None, k_gain=None, offsets=None, positions=None, out=None):
+        """cache_append() to an 8-bit cache: rows normalised, rotated and quantised
+        as they are written.  Returns the queries [T, n_q, d]."""
+        dt, T = self._dt, qkv.shape[0]
+        io = self._io[4]
+        io.kv8 = ctypes.addressof(self._kind(kv8, B.prism_cache8))
+        io.rows = T
+        io.d_qkv = self._expect(qkv, "qkv", (T, self._qkv), dt)
+        io.d_q_gain = None if q_gain is None else self._expect(q_gain, "q_gain", (self._d,), dt)
+        io.d_k_gain = None if k_gain is None else self._expect(k_gain, "k_gain", (self._d,), dt)
+        io.d_offsets = (None if offsets is None
+                        else self._expect(offsets, "offsets", (kv8.nb + 1,), torch.int32))
+        io.d_positions = (None if positions is None
+                          else self._expect(positions, "positions", (kv8.nb,), torch.int32))
+        shape = (T, self._nq, self._d)
+        if out is None:
+            out = qkv.new_empty(shape)
+            io.d_q = out.data_ptr()
+        else:
+            io.d_q = self._expect(out, "out", shape, dt)
+        B.prism_cache8_append(self.ctx, io, self._stream())
+        return out
+
+    def _move(self, call, kv8, kv, start, n_new, max_len):
+        io = self._io[5]
+        io.kv8 = ctypes.addressof(self._kind(kv8, B.prism_cache8))
+        io.kv = ctypes.addressof(self._kind(kv, B.prism_batch))
+        io.n_new = n_new
+        io.max_len = max_len
+        io.d_start = None if start is None else self._expect(start, "start", (kv8.nb,), torch.int32)
+        call(self.ctx, io, self._stream())
+
+    def cache8_pack(self, kv8, kv, start=None, n_new: int = 0, max_len: int = 0):
+        """Write slots start[b] (None: 0) .. lens[b] + n_new - 1 of the cache kv to
+        the 8-bit cache kv8, whose lengths count."""
+        self._move(B.prism_cache8_pack, kv8, kv, start, n_new, max_len)
+
+    def cache8_unpack(self, kv8, kv, start=None, n_new: int = 0, max_len: int = 0):
+        """Read the same slots of the 8-bit cache kv8 back to the cache kv."""
+        self._move(B.prism_cache8_unpack, kv8, kv, start, n_new, max_len)
+
+    def cache_attend_rows(self, kv, q, offsets=None, n_new: int = 0, window: int = 0, n_first: int = 0,
+                          max_len: int = 0, lse: bool = False, out=None):
+        """Attention of rows q [T, n_q, d] (of sequence b offsets[b] .. offsets[b+1] -
+        1; None: one each) over a cache() or cache8(): row i of a sequence sees the
+        slots below lens[b] + n_new + i, or of them the last `window` and the first
+        n_first.  Returns out [T, n_q, d] and, if asked for, lse [T, n_q]."""
+        dt, T = self._dt, q.shape[0]
+        shape = (T, self._nq, self._d)
+        io = self._io[6]
+        if type(kv) is B.prism_cache8:
+            io.kv, io.kv8 = None, ctypes.addressof(kv)
+        else:
+            io.kv, io.kv8 = ctypes.addressof(self._kind(kv, B.prism_batch)), None
+        nb = kv.nb
+        io.rows = T
+        io.d_q = self._expect(q, "q", shape, dt)
+        io.d_offsets = (None if offsets is None
+                        else self._expect(offsets, "offsets", (nb + 1,), torch.int32))
+        io.n_new = n_new
+        io.max_len = max_len
+        io.window = window
+        io.n_first = n_first
+        if out is None:
+            out = q.new_empty(shape)
+            io.d_out = out.data_ptr()
+        else:
+            io.d_out = self._expect(out, "out", shape, dt)
+        sums = torch.empty(shape[:2], dtype=torch.float32, device=self.device) if lse else None
+        io.d_lse = None if sums is None else sums.data_ptr()
+        io.scratch_bytes, scratch = self._scratch(None, nb, max_len, q, T)
+        io.d_scratch = None if scratch is None else scratch.data_ptr()
+        B.prism_cache_attend_rows(self.ctx, io, self._stream())
+        return {"out": out, "lse": sums}
 
     def device_status(self) -> int:
         return B.prism_device_status(self.ctx)
