@@ -122,10 +122,14 @@ struct RowsAttend {
   int window, n_first;                  // window 0: every slot
   int nq, g, d;
   const void *q;                        // [rows, nq, d]
-  int waves, segments;                  // rows_plan
+  int few;                              // sequences of up to so many rows are one kernel's, others
+                                        // the prompts' kernel's
+  int waves, segments;                  // rows_plan (segments, prompt_segments 0: no such kernel)
   bool direct;
+  int prompt_segments, splits;
   float scale;                          // log2(e) / sqrt(d)
   float *pm, *pl, *po;                  // partials [waves + segments][columns] / [.., d]
+  float *pm2, *pl2, *po2;               // of prompts, [splits][rows][nq] / [.., d]
   void *out; float *lse;                // [rows, nq, d] / [rows, nq] or NULL
   uint32_t *err;
 };

@@ -97,27 +97,72 @@ inline int rows_span(int g, int max_len, int window, int n_first) {
 // A workgroup for each segment, and no join, where segments are short or fill the
 // chip by themselves; else equal runs of granules for all waves, as above.
 constexpr int ROWS_DIRECT_SEGMENTS = 2048;
+// In bf16 contexts, sequences of more rows than ROWS_FEW columns hold go to the
+// kernel of prompts, in tiles of PROMPT_COLUMNS; where those are fewer than
+// PROMPT_FILL over all KV heads, each is split along its places into at most
+// PROMPT_SPLITS parts of PROMPT_PART at least, up to twice PROMPT_FILL in all.
+constexpr int ROWS_FEW = 32, PROMPT_COLUMNS = 128;
+constexpr int PROMPT_FILL = 256, PROMPT_SPLITS = 16, PROMPT_PART = 256;
+constexpr int prompt_rows(int g) { return PROMPT_COLUMNS / g; }
 struct RowsPlan {
-  int segments, waves;
+  int few;                        // rows of a sequence that the first kernel takes
+  int segments, waves;            // of it (segments 0: it is not needed)
   bool direct;
+  int prompt_segments, splits;    // of the other (0: not needed)
 };
-inline RowsPlan rows_plan(int nkv, int g, int batch, int rows, int span, int waves) {
-  const long n = rows_segments(nkv, g, batch, rows);
-  if (span <= CACHE_DIRECT || n >= ROWS_DIRECT_SEGMENTS) return {(int)n, (int)n, true};
+inline RowsPlan rows_plan(bool bf16, int nkv, int g, int batch, int rows, int span, int waves) {
+  RowsPlan p{0x7fffffff, 0, 0, true, 0, 1};
+  const int few = ROWS_FEW / g;
+  const bool prompts = bf16 && rows > few;
+  if (prompts) {
+    const long tiles = (long)rows / prompt_rows(g) + batch, full = (rows + prompt_rows(g) - 1l) / prompt_rows(g) * nkv;
+    p.few = few;
+    p.prompt_segments = (int)((tiles < rows ? tiles : rows) * nkv);
+    if (full < PROMPT_FILL) {
+      const long most = (2 * PROMPT_FILL + full - 1) / full, parts = span / PROMPT_PART;
+      const long n = most < parts ? most : parts;
+      p.splits = (int)(n < 1 ? 1 : n > PROMPT_SPLITS ? PROMPT_SPLITS : n);
+    }
+    if (batch == 1) return p;     // the kernel of prompts takes a lone sequence however short it is
+  }
+  long n = rows_segments(nkv, g, batch, rows);
+  // short sequences among prompts have few / rows_per_tile tiles at most
+  const long top = prompts ? (long)batch * ((few + rows_per_tile(g) - 1) / rows_per_tile(g)) * nkv : n;
+  n = n < top ? n : top;
+  p.segments = (int)n;
+  p.direct = span <= CACHE_DIRECT || n >= ROWS_DIRECT_SEGMENTS;
   const long granules = n * cache_granules(span);
-  return {(int)n, (int)(granules < waves ? granules : waves), false};
+  p.waves = (int)(p.direct ? n : granules < waves ? granules : waves);
+  return p;
 }
-inline size_t rows_scratch(int g, int d, const RowsPlan &p) {
-  if (p.direct) return 0;
-  const size_t parts = (size_t)cache_partials(p.waves, p.segments) * rows_per_tile(g) * g, pad = 255;
+// Scratch bytes: of the first kernel, of the other (each run 256-byte aligned).
+inline size_t rows_part_bytes(size_t parts, int d) {
+  const size_t pad = 255;
   return ((parts * 4 + pad) & ~pad) * 2 + ((parts * d * 4 + pad) & ~pad);
 }
-// The most that any call over up to `batch` sequences and `rows` rows takes.
-inline size_t rows_scratch_up_to(int nkv, int g, int d, int batch, int rows, int max_len, int waves) {
-  if (max_len <= CACHE_DIRECT) return 0;
-  const long n = rows_segments(nkv, g, batch, rows);
-  const int most = (int)(n < ROWS_DIRECT_SEGMENTS ? n : ROWS_DIRECT_SEGMENTS - 1);
-  return rows_scratch(g, d, {most, waves, false});
+inline size_t rows_scratch(int g, int d, const RowsPlan &p) {
+  if (p.direct || !p.segments) return 0;
+  return rows_part_bytes((size_t)cache_partials(p.waves, p.segments) * rows_per_tile(g) * g, d);
+}
+inline size_t prompt_scratch(int nq, int d, int rows, const RowsPlan &p) {
+  return p.prompt_segments && p.splits > 1 ? rows_part_bytes((size_t)p.splits * rows * nq, d) : 0;
+}
+// The most that any call over up to `batch` sequences and `rows` rows takes: of
+// splits * rows, with splits <= 2 PROMPT_FILL / full + 1, full >= rows / prompt_rows *
+// nkv and < PROMPT_FILL.
+inline size_t rows_scratch_up_to(bool bf16, int nkv, int g, int d, int batch, int rows, int max_len, int waves) {
+  size_t bytes = 0;
+  if (max_len > CACHE_DIRECT) {
+    const long n = rows_segments(nkv, g, batch, rows);
+    const int most = (int)(n < ROWS_DIRECT_SEGMENTS ? n : ROWS_DIRECT_SEGMENTS - 1);
+    bytes += rows_part_bytes((size_t)cache_partials(waves, most) * rows_per_tile(g) * g, d);
+  }
+  if (bf16 && max_len >= 2 * PROMPT_PART) {
+    const long fill = (long)PROMPT_FILL * prompt_rows(g) / nkv + 1, all = 2 * fill + (rows < fill ? rows : fill);
+    const long each = (long)PROMPT_SPLITS * rows;
+    bytes += rows_part_bytes((size_t)(all < each ? all : each) * nkv * g, d);
+  }
+  return bytes;
 }
 
 // Table columns per wave of the passes over the blocks of a cache (summaries,

@@ -46,7 +46,7 @@ __device__ __forceinline__ RowWalk row_walk(const RowsAttend &a) {
   if (w.n > 0 && (L < 0 || v0 + w.n - 1 > a.v.max_len)) atomicOr(a.err, ERRF_CAPACITY);
   w.v0 = L < 0 ? NO_SLOTS : (int)min(v0, (long)a.v.max_len);
   const int rt = rows_per_tile(a.g);
-  w.tiles = (w.n + rt - 1) / rt;
+  w.tiles = w.n > a.few ? 0 : (w.n + rt - 1) / rt;   // (k_rows_prompt's)
   if (a.direct) {
     w.count = 1;                           // an empty segment writes its zeros itself
   } else {
@@ -512,8 +512,408 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttend a) {
   if (t == 0 && a.lse) a.lse[hi] = l == 0.f ? -INFINITY : (top + log2f(l)) * LN2;
 }
 
+// ---------------------------------------------------------------- prompts
+// Sequences of more than a.few rows in bf16 contexts.  A workgroup takes a tile of
+// PROMPT_COLUMNS (row, head) pairs of one KV head, 32 columns a wave, and walks its
+// places BN at a time: S = K Q^T and O = V^T P as MFMAs of 32 x 32, so that a lane
+// holds one column's probabilities just where the second product takes them.
+// Probabilities are rounded to bf16 for it (2^-9 of each on average over a sum of
+// many, as much as the rounding of the output; the sum of a row takes them
+// unrounded): in three parts they would double the work of the larger product.
+//   The maximum that is subtracted follows the scores only when one is 2^8 above
+// it: sums and outputs are fp32, so nothing is lost, and outputs are seldom
+// rescaled.
+//   Rows of K and V go through registers (8-bit ones become bf16 on the way) to one
+// of two LDS buffers, one tile ahead of the products, their loads two tiles ahead
+// and block-table lookups three: one barrier per tile.
+//   Where a masked tile holds a value that is not finite, its outputs are taken on
+// the vector units (see above).
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+constexpr float PROMPT_SLACK = 8.f;
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+}
+// LDS written by the workgroup is there, with global loads still in flight
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+template <int D>
+struct PromptTile {
+  static constexpr int BN = D == 256 ? 32 : 64;             // places
+  static constexpr int LPR = D / 8;                         // 16-byte pieces of a row
+  static constexpr int BYTES = BN * D * 2;
+  // byte of piece c of row s (k_at(8 r + s, 8 x + c) = k_at(s, c) + step(r, x), and
+  // the same of v_at: a lane keeps few addresses): permuted so that the rows that are read together
+  // (keys: 8 rows, one piece; values: 4 rows, two pieces) lie in all banks
+  __device__ static int k_at(int s, int c) { return (s * LPR + (c ^ (LPR >= 8 ? s & 7 : (s >> 1) & 3))) * 16; }
+  __device__ static int v_at(int s, int c) { return (s * LPR + (c ^ (LPR >= 8 ? 2 * (s & 3) : s & 2))) * 16; }
+  __device__ static constexpr int step(int r, int x) { return (8 * r * LPR + 8 * x) * 16; }
+};
+template <int D, bool Q8>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAttend a) {
+  using PT = PromptTile<D>;
+  constexpr int BN = PT::BN, NS = BN / 32, NK = D / 16, ND = D / 32;
+  constexpr int LPR = Q8 ? D / 16 : D / 8, RPI = 256 / LPR, NI = (BN + RPI - 1) / RPI;   // lanes per stored row, rows per load, loads
+  __shared__ __attribute__((aligned(16))) char s_k[2][PT::BYTES], s_v[2][PT::BYTES];
+  __shared__ float s_p[4][16 * 32];
+  __shared__ uint64_t s_bad[3];                             // places without storage, of the tiles in turn
+  __shared__ int s_odd[3];                                  // whether a masked tile holds what is not finite
+  const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, half = lane >> 5, g = a.g, nkv = a.v.nkv;
+  const KvArgs &kv = a.v.kv;
+  // the segment: KV heads fastest (workgroups of one head meet in the XCDs' L2
+  // where there are 8 of them), the tiles that see most first
+  int b, j, tile;
+  RowSegment sg;
+  {
+    const RowWalk w = row_walk(a);
+    if (w.bad) return;
+    const int tiles = w.n > a.few ? (w.n + prompt_rows(g) - 1) / prompt_rows(g) : 0;
+    const uint32_t end = wave_scan((uint32_t)(lane < kv.n_seq ? tiles * nkv : 0));
+    b = __popcll(__ballot(end <= blockIdx.x));
+    if (b >= kv.n_seq) return;
+    const int nt = __builtin_amdgcn_readlane(tiles, b);
+    const int at = (int)blockIdx.x - ((int)__builtin_amdgcn_readlane(end, b) - nt * nkv);
+    tile = nt - 1 - at / nkv;
+    j = at % nkv;
+    sg.v0 = __builtin_amdgcn_readlane(w.v0, b);
+    sg.i0 = tile * prompt_rows(g);
+    sg.rows = min(prompt_rows(g), __builtin_amdgcn_readlane(w.n, b) - sg.i0);
+    sg.r = __builtin_amdgcn_readlane(w.r0, b) + sg.i0;
+  }
+  int places;
+  segment_places(a, sg, places);
+  const int granules = (places + BN - 1) / BN;
+  const int p_begin = (int)((long)granules * blockIdx.y / gridDim.y) * BN;
+  const int p_end = min(places, (int)((long)granules * (blockIdx.y + 1) / gridDim.y) * BN);
+  const int sink = sg.sink, shift = sg.lo - sink;
+  auto slot_of = [&](int p) { return p < sink ? p : p + shift; };
+
+  // this lane's column, and what the wave's columns see
+  const int cid = 32 * wave + (lane & 31), crow = cid / g, chead = cid - crow * g;
+  const bool used = crow < sg.rows && crow < prompt_rows(g);
+  const size_t hi = (size_t)(sg.r + crow) * a.nq + j * g + chead;
+  const int vis = used ? visible_of(sg.v0, sg.i0 + crow, a.v.max_len) : 0, win = a.window ? vis - a.window : 0;
+  const int row_a = 32 * wave / g, row_b = min(sg.rows, prompt_rows(g)) - 1;
+  const bool some = row_a <= row_b;
+  const int vis_a = visible_of(sg.v0, sg.i0 + row_a, a.v.max_len);
+  const int vis_b = visible_of(sg.v0, sg.i0 + min(row_b, (32 * wave + 31) / g), a.v.max_len);
+  const int seg_a = visible_of(sg.v0, sg.i0, a.v.max_len), seg_b = visible_of(sg.v0, sg.i0 + row_b, a.v.max_len);
+  // whether rows that see va .. vb slots all see every place of the tile at t
+  auto whole_for = [&](int t, int va, int vb) {
+    return t + BN <= p_end && slot_of(t + BN - 1) < va && (!a.window || slot_of(t) >= vb - a.window || t + BN <= sink);
+  };
+
+  u32x4 qf[NK];
+#pragma unroll
+  for (int kk = 0; kk < NK; ++kk)
+    qf[kk] = used ? *(const u32x4 *)((const bf16_t *)a.q + hi * D + 16 * kk + 8 * half) : u32x4{0, 0, 0, 0};
+  f32x16 o[ND];
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;                     // l_run: over this lane's half of the places
+
+  // loads: row grp of each pass, piece li
+  const int32_t *table = kv.block_table + (size_t)b * kv.mbps;
+  const int grp = tid / LPR, li = tid % LPR;
+  const bool loads = RPI <= BN || grp < BN;                 // a load may cover more than a tile (d = 32, 8 bits)
+  static_assert(RPI % 8 == 0, "rows of the loads of a thread differ by multiples of 8");
+  constexpr int PP = Q8 ? 2 : 1;                            // pieces in LDS of a loaded one
+  int put_k[PP], put_v[PP];
+#pragma unroll
+  for (int h = 0; h < PP; ++h) {
+    put_k[h] = PT::k_at(grp, PP * li + h);
+    put_v[h] = PT::v_at(grp, PP * li + h);
+  }
+  // the operands' pieces: keys of place lane % 32, values of the places and dims
+  // that the transposing read takes from this lane
+  constexpr int KA = NK < 4 ? NK : 4, VA = ND < 2 ? ND : 2;
+  int get_k[KA], get_v[VA];
+#pragma unroll
+  for (int x = 0; x < KA; ++x) get_k[x] = PT::k_at(lane & 31, 2 * x + half);
+#pragma unroll
+  for (int x = 0; x < VA; ++x) {
+    const int c = lane & 15;
+    get_v[x] = PT::v_at(4 * half + (c >> 2), 4 * x + 2 * ((lane >> 4) & 1) + ((c & 3) >> 1)) + 8 * (c & 1);
+  }
+  u32x4 kr[NI], vr[NI];
+  float ks[NI], vs[NI];
+  int blk[NI];
+  uint32_t ok = 0, lost = 0;                                // bit i: pass i has a row; has none but should
+  auto look_up = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = slot_block(kv, slot_of(min(t + i * RPI + grp, p_end - 1)));
+      blk[i] = c < kv.mbps ? table[c] : -1;
+    }
+  };
+  auto load = [&](int t) {
+    ok = lost = 0;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int p = t + i * RPI + grp, slot = slot_of(min(p, p_end - 1));
+      const bool there = blk[i] >= 0 && blk[i] < kv.n_blocks, due = p < p_end && loads;
+      if (due && there) ok |= 1u << i;
+      if (due && !there) {
+        atomicOr(a.err, ERRF_CAPACITY);
+        lost |= 1u << i;
+      }
+      const uint32_t hb = there ? (uint32_t)blk[i] * nkv + j : 0u;
+      const size_t at = ((size_t)hb * kv.bs + (there ? slot - slot_block(kv, slot) * kv.bs : 0)) * (D * (Q8 ? 1 : 2)) + 16 * li;
+      kr[i] = *(const u32x4 *)((const char *)kv.k_pool + at);
+      vr[i] = *(const u32x4 *)((const char *)kv.v_pool + at);
+      if constexpr (Q8) {
+        const float2 sc = *(const float2 *)(a.scales + 2 * (size_t)hb);
+        ks[i] = sc.x;
+        vs[i] = sc.y;
+      }
+    }
+  };
+  auto put = [&](int t, int buf, int turn) {
+    const bool masked = !whole_for(t, seg_a, seg_b);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int s = i * RPI + grp;
+      if (!loads) continue;
+      if (!((ok >> i) & 1)) vr[i] = u32x4{0, 0, 0, 0};
+      if ((lost >> i) & 1) atomicOr((unsigned long long *)&s_bad[turn], 1ull << s);
+      if (masked) odd |= Loader<bf16_t, D, Q8>::odd(vr[i]);
+      if constexpr (Q8) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 x, y;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            x[2 * k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)kr[i][2 * h + k], ks[i], false));
+            x[2 * k + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)kr[i][2 * h + k], ks[i], true));
+            y[2 * k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)vr[i][2 * h + k], vs[i], false));
+            y[2 * k + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)vr[i][2 * h + k], vs[i], true));
+          }
+          *(u32x4 *)(s_k[buf] + put_k[h] + PT::step(i * RPI / 8, 0)) = x;
+          *(u32x4 *)(s_v[buf] + put_v[h] + PT::step(i * RPI / 8, 0)) = y;
+        }
+      } else {
+        *(u32x4 *)(s_k[buf] + put_k[0] + PT::step(i * RPI / 8, 0)) = kr[i];
+        *(u32x4 *)(s_v[buf] + put_v[0] + PT::step(i * RPI / 8, 0)) = vr[i];
+      }
+    }
+    if (masked && odd) s_odd[turn] = 1;
+  };
+
+  if (tid < 3) {
+    s_bad[tid] = 0;
+    s_odd[tid] = 0;
+  }
+  __syncthreads();
+  if (p_begin < p_end) {
+    look_up(p_begin);
+    load(p_begin);
+    look_up(p_begin + BN);
+    put(p_begin, 0, 0);
+    if (p_begin + BN < p_end) {
+      load(p_begin + BN);
+      look_up(p_begin + 2 * BN);
+    }
+  }
+  int buf = 0, turn = 0;                                    // tile / BN modulo 2 and 3
+  for (int t = p_begin; t < p_end; t += BN, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) {
+    lds_barrier();
+    const int next = turn == 2 ? 0 : turn + 1, after = next == 2 ? 0 : next + 1;
+    if (tid == 0) {                                         // of the tile before; put() sets them behind the next barrier
+      s_bad[after] = 0;
+      s_odd[after] = 0;
+    }
+    if (t + BN < p_end) {
+      put(t + BN, buf ^ 1, next);
+      if (t + 2 * BN < p_end) {
+        load(t + 2 * BN);
+        look_up(t + 3 * BN);
+      }
+    }
+    const uint64_t bad = s_bad[turn];
+    const bool odd = s_odd[turn] != 0;
+    const char *bk = s_k[buf], *bv = s_v[buf];
+    const int first = slot_of(t), last_slot = slot_of(min(t + BN, p_end) - 1);
+    const bool skip = !some || first >= vis_b || (a.window && last_slot < vis_a - a.window && first >= a.n_first);
+    const bool whole = whole_for(t, vis_a, vis_b) && !bad;
+    if (!skip) {
+      // scores S[place 32 st + 8 jj + 4 half + i][column lane % 32]
+      f32x16 sc[NS];
+#pragma unroll
+      for (int st = 0; st < NS; ++st) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[st][i] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk)
+          sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              __builtin_bit_cast(bf16x8, *(const u32x4 *)(bk + get_k[kk % KA] + PT::step(4 * st, kk / KA))),
+              __builtin_bit_cast(bf16x8, qf[kk]), sc[st], 0, 0, 0);
+      }
+      uint32_t sees = ~0u;                                  // bit 16 st + i
+      if (!whole) {
+        sees = 0;
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int x = 32 * st + 8 * (i >> 2) + 4 * half + (i & 3), p = t + x, slot = slot_of(p);
+            const bool see = p < p_end && slot < vis && (slot >= win || slot < a.n_first) && !((bad >> x) & 1);
+            sees |= (uint32_t)see << (16 * st + i);
+            sc[st][i] = see ? sc[st][i] : -INFINITY;
+          }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[st][i]);
+      mx = fmaxf(mx, xor32_f(mx)) * a.scale;
+      if (__ballot(mx > m_run + PROMPT_SLACK)) {            // (from -inf: any score that is not)
+        const float mn = fmaxf(m_run, mx);
+        const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - mn);
+        m_run = mn;
+        l_run *= al;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[dt][i] *= al;
+      }
+      const float ms = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          sc[st][i] = __builtin_amdgcn_exp2f(fmaf(sc[st][i], a.scale, -ms));
+          l_run += sc[st][i];
+        }
+      // O[dim 32 dt + 8 jj + 4 half + i][column lane % 32]
+      if (odd && !whole) {
+        float *ps = s_p[wave];
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+          for (int h2 = 0; h2 < 2; ++h2) {                  // places 32 st + 16 h2 + 8 jj + 4 half + i
+            wave_lds_sync();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int x = 16 * st + 8 * h2 + i;
+              ps[(8 * (i >> 2) + 4 * half + (i & 3)) * 32 + (lane & 31)] = (sees >> x) & 1 ? sc[st][8 * h2 + i] : -1.f;
+            }
+            wave_lds_sync();
+#pragma unroll 1
+            for (int p = 0; p < 16; ++p) {
+              const float w = ps[p * 32 + (lane & 31)];
+              const int s = 32 * st + 16 * h2 + p;
+#pragma unroll
+              for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  const int dim = 32 * dt + 8 * (i >> 2) + 4 * half + (i & 3);
+                  const float v = bf2f(*(const uint16_t *)(bv + PT::v_at(s, dim >> 3) + 2 * (dim & 7)));
+                  o[dt][i] += w < 0.f ? 0.f : w * v;
+                }
+            }
+          }
+      } else {
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+          for (int h2 = 0; h2 < 2; ++h2) {
+            u32x4 pb;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) pb[k] = pack_bf16(sc[st][8 * h2 + 2 * k], sc[st][8 * h2 + 2 * k + 1]);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) {
+              uint2 v[2];
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const char *pv = bv + get_v[dt % VA] + PT::step(4 * st + 2 * h2 + x, dt / VA);
+                v[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
+              }
+              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                  __builtin_bit_cast(bf16x8, u32x4{v[0].x, v[0].y, v[1].x, v[1].y}), __builtin_bit_cast(bf16x8, pb), o[dt], 0, 0, 0);
+            }
+          }
+      }
+    }
+  }
+  const float l = l_run + xor32_f(l_run);
+  if (!used) return;
+  if (gridDim.y > 1) {
+    const size_t part = (size_t)blockIdx.y * a.rows * a.nq + hi;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj)
+        *(f32x4 *)(a.po2 + part * D + 32 * dt + 8 * jj + 4 * half) =
+            f32x4{o[dt][4 * jj], o[dt][4 * jj + 1], o[dt][4 * jj + 2], o[dt][4 * jj + 3]};
+    if (half == 0) {
+      a.pm2[part] = m_run;
+      a.pl2[part] = l;
+    }
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) {
+      const float z[4] = {o[dt][4 * jj] * inv, o[dt][4 * jj + 1] * inv, o[dt][4 * jj + 2] * inv, o[dt][4 * jj + 3] * inv};
+      store_n<bf16_t, 4>((bf16_t *)a.out + hi * D + 32 * dt + 8 * jj + 4 * half, z);
+    }
+  if (a.lse && half == 0) a.lse[hi] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * LN2;
+}
+// Join of a prompt's splits: D / 4 threads per (row, head), in the order of the
+// splits.
+template <int D>
+__global__ __launch_bounds__(256) void k_prompt_join(RowsAttend a, int splits) {
+  const RowWalk w = row_walk(a);
+  if (w.bad) return;
+  const long id = (long)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);
+  const int q = threadIdx.x % (D / 4);
+  const long row = id / a.nq;
+  // rows of sequences with more than a.few
+  bool mine = false;
+  for (int b = 0; b < a.v.kv.n_seq; ++b) {
+    const int r0 = __builtin_amdgcn_readlane(w.r0, b), n = __builtin_amdgcn_readlane(w.n, b);
+    mine |= n > a.few && row >= r0 && row < (long)r0 + n;
+  }
+  if (!mine) return;
+  float top = -INFINITY;
+  for (int c = 0; c < splits; ++c) top = fmaxf(top, a.pm2[(size_t)c * a.rows * a.nq + id]);
+  top = top == -INFINITY ? 0.f : top;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int c = 0; c < splits; ++c) {
+    const size_t part = (size_t)c * a.rows * a.nq + id;
+    const float wt = exp2f(a.pm2[part] - top);
+    l += a.pl2[part] * wt;
+    o += *(const f32x4 *)(a.po2 + part * D + 4 * q) * wt;
+  }
+  const float z[4] = {l == 0.f ? 0.f : o[0] / l, l == 0.f ? 0.f : o[1] / l, l == 0.f ? 0.f : o[2] / l, l == 0.f ? 0.f : o[3] / l};
+  store_n<bf16_t, 4>((bf16_t *)a.out + (size_t)id * D + 4 * q, z);
+  if (q == 0 && a.lse) a.lse[id] = l == 0.f ? -INFINITY : (top + log2f(l)) * LN2;
+}
+
 template <typename T, int D, bool Q8>
 static void rows_d(const RowsAttend &a, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (a.prompt_segments) {
+      RowsAttend p = a;
+      p.few = a.segments ? a.few : 0;                      // alone it takes every sequence
+      hipLaunchKernelGGL((k_rows_prompt<D, Q8>), dim3(p.prompt_segments, p.splits), dim3(256), 0, s, p);
+      if (p.splits > 1) {
+        const long per = 256 / (D / 4), n = (long)p.rows * p.nq;
+        hipLaunchKernelGGL((k_prompt_join<D>), dim3((n + per - 1) / per), dim3(256), 0, s, p, p.splits);
+      }
+    }
+  }
+  if (!a.segments) return;
   constexpr int NW = D * sizeof(T) > 512 ? 2 : 4;      // 64 KB of LDS
   const dim3 g(a.waves);
   if (a.direct) {

@@ -1815,7 +1815,7 @@ prism_status prism_cache_rows_scratch(prism_ctx *c, int32_t batch, int32_t rows,
   if (rows < 1) return fail(c, PRISM_ERR_INVALID_ARG, "rows %d", rows);
   int len = 0;
   CHECK(check_len(c, 0, max_len, &len));
-  *bytes = rows_scratch_up_to(c->nkv, c->nq / c->nkv, c->d, batch, rows, len, cache_waves(c->d * c->esz));
+  *bytes = rows_scratch_up_to(c->bf16, c->nkv, c->nq / c->nkv, c->d, batch, rows, len, cache_waves(c->d * c->esz));
   return PRISM_OK;
 }
 
@@ -1836,9 +1836,10 @@ prism_status prism_cache_attend_rows(prism_ctx *c, const prism_cache_row_attenti
   if ((long)io->rows * c->nq >= 1l << 30) return fail(c, PRISM_ERR_SHAPE, "%d rows of %d heads", io->rows, c->nq);
   CHECK(check_rows(c, io->d_q, "d_q"));
   CHECK(check_rows(c, io->d_out, "d_out"));
-  const RowsPlan p = rows_plan(c->nkv, g, B, io->rows, rows_span(g, len, io->window, io->n_first),
+  const RowsPlan p = rows_plan(c->bf16, c->nkv, g, B, io->rows, rows_span(g, len, io->window, io->n_first),
                                cache_waves(c->d * c->esz));
-  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, rows_scratch(g, c->d, p)));
+  const size_t first = rows_scratch(g, c->d, p), second = prompt_scratch(c->nq, c->d, io->rows, p);
+  CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, first + second));
   RowsAttend a{};
   a.v = io->kv8 ? cache8_view(c, io->kv8, io->n_new, len) : cache_view(c, io->kv, io->n_new, len);
   a.scales = io->kv8 ? io->kv8->d_scales : nullptr;
@@ -1850,13 +1851,22 @@ prism_status prism_cache_attend_rows(prism_ctx *c, const prism_cache_row_attenti
   a.g = g;
   a.d = c->d;
   a.q = io->d_q;
+  a.few = p.few;
   a.waves = p.waves;
   a.segments = p.segments;
   a.direct = p.direct;
+  a.prompt_segments = p.prompt_segments;
+  a.splits = p.splits;
   a.scale = 1.4426950408889634f / sqrtf((float)c->d);
-  if (!p.direct) {
+  char *ws = (char *)io->d_scratch;
+  if (second) {
+    const size_t parts = (size_t)p.splits * io->rows * c->nq;
+    carve(ws, (void **)&a.pm2, parts * 4);
+    carve(ws, (void **)&a.pl2, parts * 4);
+    carve(ws, (void **)&a.po2, parts * c->d * 4);
+  }
+  if (first) {
     const size_t parts = (size_t)cache_partials(p.waves, p.segments) * rows_per_tile(g) * g;
-    char *ws = (char *)io->d_scratch;
     carve(ws, (void **)&a.pm, parts * 4);
     carve(ws, (void **)&a.pl, parts * 4);
     carve(ws, (void **)&a.po, parts * c->d * 4);

@@ -222,32 +222,49 @@ int main() {
   for (int it = 0; it < 20000; ++it) {
     const int B = 1 + rand() % 64, nkv = 1 + rand() % 8, g = 1 + rand() % 8, d = 32 << (rand() % 4);
     const int top = 1 << (rand() % 12), max_len = 1 + rand() % (1 << (rand() % 18 + 1));
-    long T = 0, tiles = 0;
+    long T = 0;
+    std::vector<int> counts;
     const int rt = rows_per_tile(g);
     if (rt < 1 || rt * g > 16) return 1;
     for (int b = 0; b < B; ++b) {
       const int n = rand() % 4 ? rand() % (top + 1) : 0;
       T += n;
-      tiles += (n + rt - 1) / rt;
+      counts.push_back(n);
     }
     T += rand() % 3;
     if (T < 1) T = 1;
     const int window = rand() % 2 ? 1 + rand() % 5000 : 0, n_first = rand() % 40, waves = cache_waves(d * 2);
+    const bool bf16 = rand() % 2;
     const int span = rows_span(g, max_len, window, n_first);
     if (span < 1 || span > max_len) return 2;
-    const RowsPlan p = rows_plan(nkv, g, B, (int)T, span, waves);
-    if (tiles * nkv > p.segments) return 3;
-    if (p.direct && p.waves != p.segments) return 4;
-    if (!p.direct && (p.waves < 1 || p.waves > waves || (long)p.segments * cache_granules(max_len) >= 1l << 31)) return 5;
-    const size_t need = rows_scratch(g, d, p), up = rows_scratch_up_to(nkv, g, d, B, (int)T, max_len, waves);
-    if (need > up) return 6;
-    if (!p.direct && need < (size_t)cache_partials(p.waves, p.segments) * rt * g * (d + 2) * 4) return 7;
-    if (rows_scratch_up_to(nkv, g, d, 1 + rand() % B, 1 + rand() % (int)T, 1 + rand() % max_len, waves) > up) return 8;
+    const RowsPlan p = rows_plan(bf16, nkv, g, B, (int)T, span, waves);
+    long few = 0, many = 0;                       // segments of each kernel
+    int longest = 0;
+    for (int b = 0; b < B; ++b) {
+      if (counts[b] > p.few) many += (counts[b] + prompt_rows(g) - 1) / prompt_rows(g) * nkv;
+      else few += (counts[b] + rt - 1) / rt * nkv;
+      longest = counts[b] > longest ? counts[b] : longest;
+    }
+    if (!p.segments) {                            // the prompts' kernel alone: one sequence
+      if (B != 1 || !p.prompt_segments) return 3;
+      many = (longest + prompt_rows(g) - 1) / prompt_rows(g) * nkv;
+      few = 0;
+    }
+    if (few > p.segments || many > p.prompt_segments) return 4;
+    if (!bf16 && p.prompt_segments) return 5;
+    if (p.splits < 1 || p.splits > PROMPT_SPLITS || (p.splits > 1 && span < p.splits * PROMPT_PART)) return 6;
+    if (p.segments && p.direct && p.waves != p.segments) return 7;
+    if (p.segments && !p.direct && (p.waves < 1 || p.waves > waves || (long)p.segments * cache_granules(max_len) >= 1l << 31)) return 8;
+    const size_t need = rows_scratch(g, d, p) + prompt_scratch(nkv * g, d, (int)T, p);
+    const size_t up = rows_scratch_up_to(bf16, nkv, g, d, B, (int)T, max_len, waves);
+    if (need > up) return 9;
+    if (p.segments && !p.direct && need < (size_t)cache_partials(p.waves, p.segments) * rt * g * (d + 2) * 4) return 10;
+    if (rows_scratch_up_to(bf16, nkv, g, d, 1 + rand() % B, 1 + rand() % (int)T, 1 + rand() % max_len, waves) > up) return 11;
   }
   return 0;
 }
 """)
-    assert r.returncode == 0
+    assert r.returncode == 0, r.returncode
 
 
 def test_fp64_rotation(tmp_path):
