@@ -9,6 +9,7 @@
 // those from the first row's window on.
 #include "cache.h"
 #include "cache_device.h"
+#include <type_traits>
 
 namespace prism {
 
@@ -158,10 +159,33 @@ struct Loader {
     }
   }
 };
-template <typename T>
-__device__ __forceinline__ float lds_value(const char *p) {
-  if constexpr (sizeof(T) == 2) return bf2f(*(const uint16_t *)p);
-  else return *(const float *)p;
+// A value that is not finite must not meet the probability 0 of a column that does
+// not see it (0 times it is NaN).  Masked tiles that hold one multiply their values
+// with 0 in its place, and count what each column sees of them by a second product
+// (the prompts' kernel, whose registers have no room for it, keeps masks in LDS):
+// operands 1 for +inf, 128 for -inf, 2^14 for NaN, times 1 where the column sees
+// the place, exact for the up to 64 places of a tile.
+constexpr float ODD_POS = 1.f, ODD_NEG = 128.f, ODD_NAN = 16384.f;
+__device__ __forceinline__ void split_odd(float v, float &fin, float &code) {
+  const bool odd = !(fabsf(v) < INFINITY);
+  fin = odd ? 0.f : v;
+  code = !odd ? 0.f : v != v ? ODD_NAN : v > 0.f ? ODD_POS : ODD_NEG;
+}
+template <int N>
+__device__ __forceinline__ void split_odd_bf16(const uint32_t (&v)[N], uint32_t (&fin)[N], uint32_t (&code)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float a, b, x, y;
+    split_odd(__uint_as_float(v[i] << 16), a, x);
+    split_odd(__uint_as_float(v[i] & 0xffff0000u), b, y);
+    fin[i] = pack_upper(a, b);
+    code[i] = pack_upper(x, y);
+  }
+}
+// What the counted values add to a sum.
+__device__ __forceinline__ float odd_sum(float n) {
+  const int c = (int)n, pos = c & 127, neg = (c >> 7) & 127;
+  return c >> 14 || (pos && neg) ? NAN : pos ? INFINITY : neg ? -INFINITY : 0.f;
 }
 
 // A wave takes tiles of TS places, as in the attention of one row per sequence
@@ -170,13 +194,9 @@ __device__ __forceinline__ float lds_value(const char *p) {
 // holding one column's softmax state.  A column is a (row, head) pair, so a tile's
 // rows share what is loaded; where not every row sees every place of a tile, the
 // scores are masked place by place.
-//   A value that is not finite must not meet a probability of 0 of a column that
-// does not see it; tiles that hold one and are masked take their outputs on the
-// vector units.
 template <typename T, int D, bool Q8, int NW>
 __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_attend(RowsAttend a) {
   using M = Tile<T, D>;
-  static_assert(M::LPR * 16 >= 64, "a row of 16 probabilities fits a row of the K tile");
   using Ld = Loader<T, D, Q8>;
   constexpr int TS = M::TS, LPR = Ld::LPR, RPI = Ld::RPI, NI = Ld::NI, E = 16 / sizeof(T);
   constexpr int NS = TS / 16, NK = M::LPR / 4, ND = D / 16;
@@ -261,9 +281,10 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
       const uint64_t mask = __ballot(row.row != NO_ROW);
       constexpr uint64_t FULL = TS == 64 ? ~0ull : (1ull << (TS & 63)) - 1;
       if (mask != FULL) {
+        const uint64_t mine = mask >> grp;
 #pragma unroll
         for (int i = 0; i < NI; ++i)
-          if (!((mask >> (i * RPI + grp)) & 1)) vr[i] = u32x4{0, 0, 0, 0};
+          if (!((uint32_t)(mine >> (i * RPI)) & 1)) vr[i] = u32x4{0, 0, 0, 0};
       }
       // whether every row sees every place of the tile that has a row
       const int top = slot_of(t + TS - 1);
@@ -301,14 +322,14 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
       }
       uint32_t sees = 0;                                   // bit 4 st + i: this column sees that place
       float mx = -INFINITY;
+      const uint64_t mine = mask >> (4 * q4);              // from this lane's first place on
 #pragma unroll
       for (int st = 0; st < NS; ++st)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int p = 16 * st + 4 * q4 + i;
-          bool see = (mask >> p) & 1;
+          bool see = (uint32_t)(mine >> (16 * st)) & (1u << i);
           if (!whole) {
-            const int slot = slot_of(t + p);
+            const int slot = slot_of(t + 4 * q4 + 16 * st + i);
             see &= slot < vis && (slot >= win || slot < a.n_first);
           }
           sees |= (uint32_t)see << (4 * st + i);
@@ -339,68 +360,89 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
         for (int dt = 0; dt < ND; ++dt) o[dt] *= al;
       }
       // O[dim 16 dt + 4 q4 + i][column col]
-      if (odd) {
-        // the probabilities by way of the K tile, whose scores are done; -1: not seen
-        float *ps = (float *)s_k;
-        wave_lds_sync();
+      constexpr int NP = sizeof(T) == 2 && NS > 1 ? 2 : 1;   // groups of 16 places per bf16 MFMA (32 places, or 16)
+      auto product = [&](auto masked) {
+        constexpr bool ODD = decltype(masked)::value;
+        f32x4 count[ODD ? ND : 1];
+        if constexpr (ODD) {
 #pragma unroll
-        for (int st = 0; st < NS; ++st)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            ps[(16 * st + 4 * q4 + i) * 16 + col] = (sees >> (4 * st + i)) & 1 ? sc[st][i] : -1.f;
-        wave_lds_sync();
-#pragma unroll 1
-        for (int p = 0; p < TS; ++p) {
-          const float w = ps[p * 16 + col];
-#pragma unroll
-          for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int dim = 16 * dt + 4 * q4 + e;
-              const float v = lds_value<T>(s_v + M::at(p, dim / E) + dim % E * sizeof(T));
-              o[dt][e] += w < 0.f ? 0.f : w * v;
-            }
+          for (int dt = 0; dt < ND; ++dt) count[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        wave_lds_sync();
-        continue;
-      }
-      constexpr int NP = sizeof(T) == 2 && NS > 1 ? 2 : 1;
 #pragma unroll
-      for (int st = 0; st < NS; st += NP) {
-        if constexpr (sizeof(T) == 2) {
-          uint32_t hi3[NP][2], mid[NP][2], lo[NP][2];
-#pragma unroll
-          for (int x = 0; x < NP; ++x) split_bf16(sc[st + x], hi3[x], mid[x], lo[x]);
-#pragma unroll
-          for (int dt = 0; dt < ND; ++dt) {
-            uint2 v[NP];
+        for (int st = 0; st < NS; st += NP) {
+          if constexpr (sizeof(T) == 2) {
+            uint32_t hi3[2 * NP], mid[2 * NP], lo[2 * NP], one[2 * NP];
 #pragma unroll
             for (int x = 0; x < NP; ++x) {
-              const char *pv = s_v + M::at(16 * (st + x) + 4 * q4 + (col >> 2), 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
-              v[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
+              uint32_t h[2], m[2], l[2];
+              split_bf16(sc[st + x], h, m, l);
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                hi3[2 * x + y] = h[y];
+                mid[2 * x + y] = m[y];
+                lo[2 * x + y] = l[y];
+                const uint32_t b = sees >> (4 * (st + x) + 2 * y);
+                one[2 * x + y] = (b & 1 ? 0x3f80u : 0u) | (b & 2 ? 0x3f800000u : 0u);
+              }
             }
-            if constexpr (NP == 2) {
-              const u32x4 vv = {v[0].x, v[0].y, v[1].x, v[1].y};
-              o[dt] = Ty<T>::mma(vv, u32x4{hi3[0][0], hi3[0][1], hi3[1][0], hi3[1][1]}, o[dt]);
-              o[dt] = Ty<T>::mma(vv, u32x4{mid[0][0], mid[0][1], mid[1][0], mid[1][1]}, o[dt]);
-              o[dt] = Ty<T>::mma(vv, u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]}, o[dt]);
-            } else {
-              const s16x4 vv = __builtin_bit_cast(s16x4, v[0]);
-              o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, __builtin_bit_cast(s16x4, uint2{hi3[0][0], hi3[0][1]}), o[dt], 0, 0, 0);
-              o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, __builtin_bit_cast(s16x4, uint2{mid[0][0], mid[0][1]}), o[dt], 0, 0, 0);
-              o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, __builtin_bit_cast(s16x4, uint2{lo[0][0], lo[0][1]}), o[dt], 0, 0, 0);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) {
+              uint32_t v[2 * NP];
+#pragma unroll
+              for (int x = 0; x < NP; ++x) {
+                const char *pv = s_v + M::at(16 * (st + x) + 4 * q4 + (col >> 2), 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
+                const uint2 r = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
+                v[2 * x] = r.x;
+                v[2 * x + 1] = r.y;
+              }
+              uint32_t code[2 * NP];
+              if constexpr (ODD) {
+                uint32_t fin[2 * NP];
+                split_odd_bf16<2 * NP>(v, fin, code);
+#pragma unroll
+                for (int x = 0; x < 2 * NP; ++x) v[x] = fin[x];
+              }
+              // k = 8 q4 + e: places 16 st + 4 q4 + e, then the same of st + 1, in both operands
+              auto mma = [&](const uint32_t(&x)[2 * NP], const uint32_t(&y)[2 * NP], f32x4 acc) {
+                if constexpr (NP == 2)
+                  return Ty<T>::mma(u32x4{x[0], x[1], x[2], x[3]}, u32x4{y[0], y[1], y[2], y[3]}, acc);
+                else
+                  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, uint2{x[0], x[1]}),
+                                                                  __builtin_bit_cast(s16x4, uint2{y[0], y[1]}), acc, 0, 0, 0);
+              };
+              o[dt] = mma(v, hi3, o[dt]);
+              o[dt] = mma(v, mid, o[dt]);
+              o[dt] = mma(v, lo, o[dt]);
+              if constexpr (ODD) count[dt] = mma(code, one, count[dt]);
             }
+          } else {
+            // step i: place 4 q4 + i of each lane row
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const char *pv = s_v + M::at(16 * st + 4 * q4 + i, 4 * dt + (col >> 2)) + 4 * (col & 3);
+                float v = *(const float *)pv, code;
+                if constexpr (ODD) {
+                  float fin;
+                  split_odd(v, fin, code);
+                  v = fin;
+                }
+                o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[st][i], o[dt], 0, 0, 0);
+                if constexpr (ODD)
+                  count[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(code, (sees >> (4 * st + i)) & 1 ? 1.f : 0.f, count[dt], 0, 0, 0);
+              }
           }
-        } else {
+        }
+        if constexpr (ODD) {
 #pragma unroll
           for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const char *pv = s_v + M::at(16 * st + 4 * q4 + i, 4 * dt + (col >> 2)) + 4 * (col & 3);
-              o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(*(const float *)pv, sc[st][i], o[dt], 0, 0, 0);
-            }
+            for (int i = 0; i < 4; ++i) o[dt][i] += odd_sum(count[dt][i]);
         }
-      }
+      };
+      if (odd) product(std::true_type{});
+      else product(std::false_type{});
       wave_lds_sync();                                 // reads done before the next tile's writes
     }
     if constexpr (NW > 1) {
@@ -526,8 +568,6 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttend a) {
 //   Rows of K and V go through registers (8-bit ones become bf16 on the way) to one
 // of two LDS buffers, one tile ahead of the products, their loads two tiles ahead
 // and block-table lookups three: one barrier per tile.
-//   Where a masked tile holds a value that is not finite, its outputs are taken on
-// the vector units (see above).
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr float PROMPT_SLACK = 8.f;
@@ -558,9 +598,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
   constexpr int BN = PT::BN, NS = BN / 32, NK = D / 16, ND = D / 32;
   constexpr int LPR = Q8 ? D / 16 : D / 8, RPI = 256 / LPR, NI = (BN + RPI - 1) / RPI;   // lanes per stored row, rows per load, loads
   __shared__ __attribute__((aligned(16))) char s_k[2][PT::BYTES], s_v[2][PT::BYTES];
-  __shared__ float s_p[4][16 * 32];
-  __shared__ uint64_t s_bad[3];                             // places without storage, of the tiles in turn
-  __shared__ int s_odd[3];                                  // whether a masked tile holds what is not finite
+  __shared__ uint64_t s_mask[D][3];                         // places with +inf, -inf, NaN in each dim
+  __shared__ int s_odd[3];                                  // of the tiles in turn: whether a masked one holds
+                                                            // what is not finite
   const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, half = lane >> 5, g = a.g, nkv = a.v.nkv;
   const KvArgs &kv = a.v.kv;
   // the segment: KV heads fastest (workgroups of one head meet in the XCDs' L2
@@ -607,9 +647,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
   };
 
   u32x4 qf[NK];
+  {
+    const bf16_t *q = (const bf16_t *)a.q + (used ? hi : 0) * D + 8 * half;   // (a column of no row: another's)
 #pragma unroll
-  for (int kk = 0; kk < NK; ++kk)
-    qf[kk] = used ? *(const u32x4 *)((const bf16_t *)a.q + hi * D + 16 * kk + 8 * half) : u32x4{0, 0, 0, 0};
+    for (int kk = 0; kk < NK; ++kk) qf[kk] = *(const u32x4 *)(q + 16 * kk);
+  }
   f32x16 o[ND];
 #pragma unroll
   for (int dt = 0; dt < ND; ++dt)
@@ -617,10 +659,48 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;                     // l_run: over this lane's half of the places
 
-  // loads: row grp of each pass, piece li
+  // Loads: a lane of each wave looks up one place of a tile, and takes piece li of
+  // row grp of each pass.
   const int32_t *table = kv.block_table + (size_t)b * kv.mbps;
   const int grp = tid / LPR, li = tid % LPR;
   const bool loads = RPI <= BN || grp < BN;                 // a load may cover more than a tile (d = 32, 8 bits)
+  const float inv_bs = 1.f / (float)kv.bs;
+  // table column of a slot (below 2^20): the quotient by way of fp32 is off by one at
+  // most
+  auto column = [&](int slot) {
+    int c = (int)((float)slot * inv_bs);
+    c -= c * kv.bs > slot;
+    return c + ((c + 1) * kv.bs <= slot);
+  };
+  u32x4 kr[NI], vr[NI];
+  uint32_t exps[Q8 ? NI : 1];                               // scales of keys and values: their upper halves
+  int col_next, blk_next;                                   // of this lane's place of the tile to be loaded
+  uint64_t m_load = 0;                                      // places of the loaded tile with a row
+  auto look_up = [&](int t) {
+    col_next = column(slot_of(min(t + lane, p_end - 1)));
+    blk_next = table[min(col_next, kv.mbps - 1)];
+  };
+  auto load = [&](int t) {
+    const int p = t + lane;
+    const bool due = lane < BN && p < p_end, there = due && blk_next >= 0 && blk_next < kv.n_blocks;
+    m_load = __ballot(there);
+    if (__ballot(due && !there)) atomicOr(a.err, ERRF_CAPACITY);
+    const uint32_t hb = there ? (uint32_t)blk_next * nkv + j : 0u;
+    const uint32_t row = there ? hb * kv.bs + (uint32_t)(slot_of(p) - col_next * kv.bs) : 0u;   // (row 0: masked)
+    uint32_t ex = 0;
+    if constexpr (Q8) {
+      const uint2 sc = *(const uint2 *)(a.scales + 2 * (size_t)hb);
+      ex = there ? (sc.x >> 16) | (sc.y & 0xffff0000u) : 0x3f803f80u;   // (a scale of 1: the 0 of a masked place stays 0)
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int from = i * RPI + grp;
+      const size_t at = (size_t)__shfl(row, from, 64) * (D * (Q8 ? 1 : 2)) + 16 * li;
+      kr[i] = *(const u32x4 *)((const char *)kv.k_pool + at);
+      vr[i] = *(const u32x4 *)((const char *)kv.v_pool + at);
+      if constexpr (Q8) exps[i] = __shfl(ex, from, 64);
+    }
+  };
   static_assert(RPI % 8 == 0, "rows of the loads of a thread differ by multiples of 8");
   constexpr int PP = Q8 ? 2 : 1;                            // pieces in LDS of a loaded one
   int put_k[PP], put_v[PP];
@@ -640,81 +720,55 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
     const int c = lane & 15;
     get_v[x] = PT::v_at(4 * half + (c >> 2), 4 * x + 2 * ((lane >> 4) & 1) + ((c & 3) >> 1)) + 8 * (c & 1);
   }
-  u32x4 kr[NI], vr[NI];
-  float ks[NI], vs[NI];
-  int blk[NI];
-  uint32_t ok = 0, lost = 0;                                // bit i: pass i has a row; has none but should
-  auto look_up = [&](int t) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int c = slot_block(kv, slot_of(min(t + i * RPI + grp, p_end - 1)));
-      blk[i] = c < kv.mbps ? table[c] : -1;
-    }
-  };
-  auto load = [&](int t) {
-    ok = lost = 0;
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int p = t + i * RPI + grp, slot = slot_of(min(p, p_end - 1));
-      const bool there = blk[i] >= 0 && blk[i] < kv.n_blocks, due = p < p_end && loads;
-      if (due && there) ok |= 1u << i;
-      if (due && !there) {
-        atomicOr(a.err, ERRF_CAPACITY);
-        lost |= 1u << i;
-      }
-      const uint32_t hb = there ? (uint32_t)blk[i] * nkv + j : 0u;
-      const size_t at = ((size_t)hb * kv.bs + (there ? slot - slot_block(kv, slot) * kv.bs : 0)) * (D * (Q8 ? 1 : 2)) + 16 * li;
-      kr[i] = *(const u32x4 *)((const char *)kv.k_pool + at);
-      vr[i] = *(const u32x4 *)((const char *)kv.v_pool + at);
-      if constexpr (Q8) {
-        const float2 sc = *(const float2 *)(a.scales + 2 * (size_t)hb);
-        ks[i] = sc.x;
-        vs[i] = sc.y;
-      }
-    }
-  };
+  constexpr uint64_t FULL = BN == 64 ? ~0ull : (1ull << (BN & 63)) - 1;
   auto put = [&](int t, int buf, int turn) {
-    const bool masked = !whole_for(t, seg_a, seg_b);
-    bool odd = false;
+    if (m_load != FULL) {
+      const uint64_t mine = m_load >> (grp & 63);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        if (!((uint32_t)(mine >> (i * RPI & 63)) & 1)) vr[i] = u32x4{0, 0, 0, 0};
+    }
+    if (!whole_for(t, seg_a, seg_b)) {
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) odd |= Loader<bf16_t, D, Q8>::odd(vr[i]);
+      if (odd) s_odd[turn] = 1;
+    }
+    if (!loads) return;
+    char *bk = s_k[buf], *bv = s_v[buf];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int s = i * RPI + grp;
-      if (!loads) continue;
-      if (!((ok >> i) & 1)) vr[i] = u32x4{0, 0, 0, 0};
-      if ((lost >> i) & 1) atomicOr((unsigned long long *)&s_bad[turn], 1ull << s);
-      if (masked) odd |= Loader<bf16_t, D, Q8>::odd(vr[i]);
       if constexpr (Q8) {
+        const float ks = __uint_as_float(exps[i] << 16), vs = __uint_as_float(exps[i] & 0xffff0000u);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           u32x4 x, y;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            x[2 * k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)kr[i][2 * h + k], ks[i], false));
-            x[2 * k + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)kr[i][2 * h + k], ks[i], true));
-            y[2 * k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)vr[i][2 * h + k], vs[i], false));
-            y[2 * k + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)vr[i][2 * h + k], vs[i], true));
+            x[2 * k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)kr[i][2 * h + k], ks, false));
+            x[2 * k + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)kr[i][2 * h + k], ks, true));
+            y[2 * k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)vr[i][2 * h + k], vs, false));
+            y[2 * k + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)vr[i][2 * h + k], vs, true));
           }
-          *(u32x4 *)(s_k[buf] + put_k[h] + PT::step(i * RPI / 8, 0)) = x;
-          *(u32x4 *)(s_v[buf] + put_v[h] + PT::step(i * RPI / 8, 0)) = y;
+          *(u32x4 *)(bk + put_k[h] + PT::step(i * RPI / 8, 0)) = x;
+          *(u32x4 *)(bv + put_v[h] + PT::step(i * RPI / 8, 0)) = y;
         }
       } else {
-        *(u32x4 *)(s_k[buf] + put_k[0] + PT::step(i * RPI / 8, 0)) = kr[i];
-        *(u32x4 *)(s_v[buf] + put_v[0] + PT::step(i * RPI / 8, 0)) = vr[i];
+        *(u32x4 *)(bk + put_k[0] + PT::step(i * RPI / 8, 0)) = kr[i];
+        *(u32x4 *)(bv + put_v[0] + PT::step(i * RPI / 8, 0)) = vr[i];
       }
     }
-    if (masked && odd) s_odd[turn] = 1;
   };
 
-  if (tid < 3) {
-    s_bad[tid] = 0;
-    s_odd[tid] = 0;
-  }
+  if (tid < 3) s_odd[tid] = 0;
   __syncthreads();
+  uint64_t m_tile = 0;
   if (p_begin < p_end) {
     look_up(p_begin);
     load(p_begin);
     look_up(p_begin + BN);
     put(p_begin, 0, 0);
+    m_tile = m_load;
     if (p_begin + BN < p_end) {
       load(p_begin + BN);
       look_up(p_begin + 2 * BN);
@@ -724,23 +778,34 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
   for (int t = p_begin; t < p_end; t += BN, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) {
     lds_barrier();
     const int next = turn == 2 ? 0 : turn + 1, after = next == 2 ? 0 : next + 1;
-    if (tid == 0) {                                         // of the tile before; put() sets them behind the next barrier
-      s_bad[after] = 0;
-      s_odd[after] = 0;
-    }
+    if (tid == 0) s_odd[after] = 0;                         // of the tile before; set again behind the next barrier
+    const uint64_t held = m_tile;                           // places of this tile with a row
     if (t + BN < p_end) {
       put(t + BN, buf ^ 1, next);
+      m_tile = m_load;
       if (t + 2 * BN < p_end) {
         load(t + 2 * BN);
         look_up(t + 3 * BN);
       }
     }
-    const uint64_t bad = s_bad[turn];
     const bool odd = s_odd[turn] != 0;
     const char *bk = s_k[buf], *bv = s_v[buf];
+    if (odd) {                                              // the same for the workgroup
+      for (int i = tid; i < 3 * D; i += 256) s_mask[i / 3][i % 3] = 0;
+      lds_barrier();
+      for (int i = tid; i < BN * D; i += 256) {
+        const int s = i / D, dim = i % D;
+        uint16_t *v = (uint16_t *)(s_v[buf] + PT::v_at(s, dim >> 3) + 2 * (dim & 7));
+        const uint32_t x = *v;
+        if ((x & 0x7f80u) != 0x7f80u) continue;
+        atomicOr((unsigned long long *)&s_mask[dim][(x & 0x7fu) ? 2 : x >> 15], 1ull << s);
+        *v = 0;
+      }
+      lds_barrier();
+    }
     const int first = slot_of(t), last_slot = slot_of(min(t + BN, p_end) - 1);
     const bool skip = !some || first >= vis_b || (a.window && last_slot < vis_a - a.window && first >= a.n_first);
-    const bool whole = whole_for(t, vis_a, vis_b) && !bad;
+    const bool whole = whole_for(t, vis_a, vis_b) && held == FULL;
     if (!skip) {
       // scores S[place 32 st + 8 jj + 4 half + i][column lane % 32]
       f32x16 sc[NS];
@@ -757,12 +822,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
       uint32_t sees = ~0u;                                  // bit 16 st + i
       if (!whole) {
         sees = 0;
+        const uint64_t mine = held >> (4 * half);           // from this lane's first place on
+        const int p0 = t + 4 * half;
 #pragma unroll
         for (int st = 0; st < NS; ++st)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int x = 32 * st + 8 * (i >> 2) + 4 * half + (i & 3), p = t + x, slot = slot_of(p);
-            const bool see = p < p_end && slot < vis && (slot >= win || slot < a.n_first) && !((bad >> x) & 1);
+            const int x = 8 * (i >> 2) + (i & 3), slot = slot_of(p0 + 32 * st + x);
+            const bool see = ((uint32_t)(mine >> (32 * st)) & (1u << x)) && slot < vis && (slot >= win || slot < a.n_first);
             sees |= (uint32_t)see << (16 * st + i);
             sc[st][i] = see ? sc[st][i] : -INFINITY;
           }
@@ -792,52 +859,39 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
           l_run += sc[st][i];
         }
       // O[dim 32 dt + 8 jj + 4 half + i][column lane % 32]
-      if (odd && !whole) {
-        float *ps = s_p[wave];
 #pragma unroll
-        for (int st = 0; st < NS; ++st)
+      for (int x = 0; x < 2 * NS; ++x) {                    // places 16 x .. 16 x + 15
+        u32x4 pb;
 #pragma unroll
-          for (int h2 = 0; h2 < 2; ++h2) {                  // places 32 st + 16 h2 + 8 jj + 4 half + i
-            wave_lds_sync();
+        for (int k = 0; k < 4; ++k) pb[k] = pack_bf16(sc[x >> 1][8 * (x & 1) + 2 * k], sc[x >> 1][8 * (x & 1) + 2 * k + 1]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int x = 16 * st + 8 * h2 + i;
-              ps[(8 * (i >> 2) + 4 * half + (i & 3)) * 32 + (lane & 31)] = (sees >> x) & 1 ? sc[st][8 * h2 + i] : -1.f;
-            }
-            wave_lds_sync();
-#pragma unroll 1
-            for (int p = 0; p < 16; ++p) {
-              const float w = ps[p * 32 + (lane & 31)];
-              const int s = 32 * st + 16 * h2 + p;
+        for (int dt = 0; dt < ND; ++dt) {
+          uint2 v[2];
 #pragma unroll
-              for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  const int dim = 32 * dt + 8 * (i >> 2) + 4 * half + (i & 3);
-                  const float v = bf2f(*(const uint16_t *)(bv + PT::v_at(s, dim >> 3) + 2 * (dim & 7)));
-                  o[dt][i] += w < 0.f ? 0.f : w * v;
-                }
-            }
+          for (int y = 0; y < 2; ++y) {
+            const char *pv = bv + get_v[dt % VA] + PT::step(2 * x + y, dt / VA);
+            v[y] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
           }
-      } else {
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              __builtin_bit_cast(bf16x8, u32x4{v[0].x, v[0].y, v[1].x, v[1].y}), __builtin_bit_cast(bf16x8, pb), o[dt], 0, 0, 0);
+        }
+      }
+      if (odd) {
+        // the places that this column sees, those of both halves of the lanes
+        uint64_t see = 0;
 #pragma unroll
         for (int st = 0; st < NS; ++st)
 #pragma unroll
-          for (int h2 = 0; h2 < 2; ++h2) {
-            u32x4 pb;
+          for (int jj = 0; jj < 4; ++jj) see |= (uint64_t)((sees >> (16 * st + 4 * jj)) & 15) << (32 * st + 8 * jj + 4 * half);
+        see |= __shfl_xor(see, 32, 64);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) pb[k] = pack_bf16(sc[st][8 * h2 + 2 * k], sc[st][8 * h2 + 2 * k + 1]);
+        for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) {
-              uint2 v[2];
-#pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                const char *pv = bv + get_v[dt % VA] + PT::step(4 * st + 2 * h2 + x, dt / VA);
-                v[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
-              }
-              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                  __builtin_bit_cast(bf16x8, u32x4{v[0].x, v[0].y, v[1].x, v[1].y}), __builtin_bit_cast(bf16x8, pb), o[dt], 0, 0, 0);
-            }
+          for (int i = 0; i < 16; ++i) {
+            const uint64_t(&m)[3] = s_mask[32 * dt + 8 * (i >> 2) + 4 * half + (i & 3)];
+            const bool pos = m[0] & see, neg = m[1] & see, nan = m[2] & see;
+            o[dt][i] += nan || (pos && neg) ? NAN : pos ? INFINITY : neg ? -INFINITY : 0.f;
+            __builtin_amdgcn_sched_barrier(0);              // few registers rather than overlap
           }
       }
     }
