@@ -585,12 +585,12 @@ struct PromptTile {
   static constexpr int BN = D == 256 ? 32 : 64;             // places
   static constexpr int LPR = D / 8;                         // 16-byte pieces of a row
   static constexpr int BYTES = BN * D * 2;
-  // byte of piece c of row s (k_at(8 r + s, 8 x + c) = k_at(s, c) + step(r, x), and
-  // the same of v_at: a lane keeps few addresses): permuted so that the rows that are read together
-  // (keys: 8 rows, one piece; values: 4 rows, two pieces) lie in all banks
-  __device__ static int k_at(int s, int c) { return (s * LPR + (c ^ (LPR >= 8 ? s & 7 : (s >> 1) & 3))) * 16; }
-  __device__ static int v_at(int s, int c) { return (s * LPR + (c ^ (LPR >= 8 ? 2 * (s & 3) : s & 2))) * 16; }
-  __device__ static constexpr int step(int r, int x) { return (8 * r * LPR + 8 * x) * 16; }
+  // byte of piece c of row s: permuted so that what is read together lies in all 64
+  // banks (keys: one piece of 16 rows; values: four pieces of 4 rows).  At rows and
+  // pieces 16 further it is the same by step(), so a lane keeps few addresses.
+  __device__ static int k_at(int s, int c) { return (s * LPR + (c ^ (LPR >= 16 ? s & 15 : LPR == 8 ? (s >> 1) & 7 : (s >> 2) & 3))) * 16; }
+  __device__ static int v_at(int s, int c) { return (s * LPR + (c ^ (LPR >= 16 ? 4 * (s & 3) : LPR == 8 ? 4 * ((s >> 1) & 1) : 0))) * 16; }
+  __device__ static constexpr int step(int rows, int pieces) { return (rows * LPR + pieces) * 16; }
 };
 template <int D, bool Q8>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAttend a) {
@@ -701,17 +701,18 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
       if constexpr (Q8) exps[i] = __shfl(ex, from, 64);
     }
   };
-  static_assert(RPI % 8 == 0, "rows of the loads of a thread differ by multiples of 8");
-  constexpr int PP = Q8 ? 2 : 1;                            // pieces in LDS of a loaded one
-  int put_k[PP], put_v[PP];
+  constexpr int PP = Q8 ? 2 : 1, PR = RPI % 16 ? 2 : 1;      // pieces in LDS of a loaded one; loads per 16 rows
+  static_assert(RPI % 8 == 0, "a thread's rows repeat modulo 16");
+  int put_k[PR][PP], put_v[PP];
 #pragma unroll
   for (int h = 0; h < PP; ++h) {
-    put_k[h] = PT::k_at(grp, PP * li + h);
+#pragma unroll
+    for (int i = 0; i < PR; ++i) put_k[i][h] = PT::k_at(grp + i * RPI, PP * li + h) - PT::step(i * RPI, 0);
     put_v[h] = PT::v_at(grp, PP * li + h);
   }
   // the operands' pieces: keys of place lane % 32, values of the places and dims
   // that the transposing read takes from this lane
-  constexpr int KA = NK < 4 ? NK : 4, VA = ND < 2 ? ND : 2;
+  constexpr int KA = NK < 8 ? NK : 8, VA = ND < 4 ? ND : 4;
   int get_k[KA], get_v[VA];
 #pragma unroll
   for (int x = 0; x < KA; ++x) get_k[x] = PT::k_at(lane & 31, 2 * x + half);
@@ -750,12 +751,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
             y[2 * k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)vr[i][2 * h + k], vs, false));
             y[2 * k + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)vr[i][2 * h + k], vs, true));
           }
-          *(u32x4 *)(bk + put_k[h] + PT::step(i * RPI / 8, 0)) = x;
-          *(u32x4 *)(bv + put_v[h] + PT::step(i * RPI / 8, 0)) = y;
+          *(u32x4 *)(bk + put_k[i % PR][h] + PT::step(i * RPI, 0)) = x;
+          *(u32x4 *)(bv + put_v[h] + PT::step(i * RPI, 0)) = y;
         }
       } else {
-        *(u32x4 *)(bk + put_k[0] + PT::step(i * RPI / 8, 0)) = kr[i];
-        *(u32x4 *)(bv + put_v[0] + PT::step(i * RPI / 8, 0)) = vr[i];
+        *(u32x4 *)(bk + put_k[i % PR][0] + PT::step(i * RPI, 0)) = kr[i];
+        *(u32x4 *)(bv + put_v[0] + PT::step(i * RPI, 0)) = vr[i];
       }
     }
   };
@@ -816,7 +817,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk)
           sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              __builtin_bit_cast(bf16x8, *(const u32x4 *)(bk + get_k[kk % KA] + PT::step(4 * st, kk / KA))),
+              __builtin_bit_cast(bf16x8, *(const u32x4 *)(bk + get_k[kk % KA] + PT::step(32 * st, 16 * (kk / KA)))),
               __builtin_bit_cast(bf16x8, qf[kk]), sc[st], 0, 0, 0);
       }
       uint32_t sees = ~0u;                                  // bit 16 st + i
@@ -869,7 +870,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
           uint2 v[2];
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const char *pv = bv + get_v[dt % VA] + PT::step(2 * x + y, dt / VA);
+            const char *pv = bv + get_v[dt % VA] + PT::step(16 * x + 8 * y, 16 * (dt / VA));
             v[y] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
           }
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
