@@ -122,6 +122,7 @@ struct RowsAttend {
   int window, n_first;                  // window 0: every slot
   int nq, g, d;
   const void *q;                        // [rows, nq, d]
+  int cols;                             // columns of a tile
   int few;                              // sequences of up to so many rows are one kernel's, others
                                         // the prompts' kernel's
   int waves, segments;                  // rows_plan (segments, prompt_segments 0: no such kernel)

@@ -77,7 +77,7 @@ __device__ __forceinline__ float to_odd(double x) {
 // lanes hold a head of a row as the rotation pairs it: dims 8i .. 8i+7 and d/2 +
 // 8i ...  Keys are normalised and rotated in fp64, as the angles are, so that a key
 // next to the border of two codes takes the nearer one; the rounding to fp32 in
-// between keeps the side (to_odd).  Up to 16 new rows of a block stay in registers
+// between keeps the side (to_odd).  Queries, which have no such borders, in fp32.  Up to 16 new rows of a block stay in registers
 // between the maximum and the codes; of more (larger blocks), the rows are read
 // twice.
 constexpr int APPEND8_ROWS = 16;
@@ -86,6 +86,7 @@ __global__ __launch_bounds__(512) void k_cache8_append(Cache8Append a) {
   constexpr int LPH = D / 16, HPW = 64 / LPH, IT = (APPEND8_ROWS + HPW - 1) / HPW;
   const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, NW = blockDim.x >> 6;
   __shared__ double cs[APPEND8_ROWS][D / 2], sn[APPEND8_ROWS][D / 2];
+  __shared__ __attribute__((aligned(16))) float cq[APPEND8_ROWS][D / 2], sq[APPEND8_ROWS][D / 2];   // of the queries
   const KvArgs &kv = a.v.kv;
   const int bs = kv.bs, nkv = a.v.nkv, nh = a.nq + 2 * nkv, B = kv.n_seq;
   // the sequence and the block of this workgroup, from one lane per sequence
@@ -136,6 +137,8 @@ __global__ __launch_bounds__(512) void k_cache8_append(Cache8Append a) {
         for (int i = tid; i < nr * (D / 2); i += blockDim.x) {
           const int r = i / (D / 2), k = i % (D / 2);
           rotation_cos_sin64((double)(pos0 + c0 + r) * a.inv_freq[k], cs[r][k], sn[r][k]);
+          cq[r][k] = (float)cs[r][k];
+          sq[r][k] = (float)sn[r][k];
         }
         __syncthreads();
 #pragma unroll 1
@@ -156,16 +159,37 @@ __global__ __launch_bounds__(512) void k_cache8_append(Cache8Append a) {
             float x1[8], x2[8];
             load8f<T>(src, x1);
             load8f<T>(src + D / 2, x2);
-            if (!is_v) {
-              const T *gain = (const T *)(is_q ? a.q_gain : a.k_gain);
-              const int rc = has ? r : 0;
+            const int rc = has ? r : 0;
+            if (is_q) {
+              if (a.q_gain) {
+                float ss = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ss += x1[i] * x1[i] + x2[i] * x2[i];
+                ss = group_sum(ss, LPH == 2 ? 1 : LPH == 4 ? 2 : LPH == 8 ? 3 : 4);
+                const float rs = 1.0f / sqrtf(ss / (float)D + a.eps);
+                float g1[8], g2[8];
+                load8f<T>((const T *)a.q_gain + 8 * li, g1);
+                load8f<T>((const T *)a.q_gain + D / 2 + 8 * li, g2);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  x1[i] *= rs * g1[i];
+                  x2[i] *= rs * g2[i];
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float c = cq[rc][8 * li + i], s = sq[rc][8 * li + i], u = x1[i], w = x2[i];
+                x1[i] = u * c - w * s;
+                x2[i] = w * c + u * s;
+              }
+            } else if (!is_v) {
               double y1[8], y2[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 y1[i] = x1[i];
                 y2[i] = x2[i];
               }
-              if (gain) {
+              if (a.k_gain) {
                 double ss = 0.0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) ss += y1[i] * y1[i] + y2[i] * y2[i];
@@ -173,8 +197,8 @@ __global__ __launch_bounds__(512) void k_cache8_append(Cache8Append a) {
                 for (int m = 1; m < LPH; m *= 2) ss += __shfl_xor(ss, m, 64);
                 const double rs = 1.0 / sqrt(ss / D + (double)a.eps);
                 float g1[8], g2[8];
-                load8f<T>(gain + 8 * li, g1);
-                load8f<T>(gain + D / 2 + 8 * li, g2);
+                load8f<T>((const T *)a.k_gain + 8 * li, g1);
+                load8f<T>((const T *)a.k_gain + D / 2 + 8 * li, g2);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                   y1[i] *= rs * g1[i];
@@ -184,9 +208,8 @@ __global__ __launch_bounds__(512) void k_cache8_append(Cache8Append a) {
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 const double c = cs[rc][8 * li + i], s = sn[rc][8 * li + i];
-                const double u = y1[i] * c - y2[i] * s, w = y2[i] * c + y1[i] * s;
-                x1[i] = is_q ? (float)u : to_odd(u);
-                x2[i] = is_q ? (float)w : to_odd(w);
+                x1[i] = to_odd(y1[i] * c - y2[i] * s);
+                x2[i] = to_odd(y2[i] * c + y1[i] * s);
               }
             }
             if (is_q) {
@@ -295,7 +318,7 @@ __global__ __launch_bounds__(256) void k_cache8_pack(Cache8Move a) {
   const Moved m = moved_slots(a, b, blockIdx.x);
   if (m.from >= m.to) return;
   const bool once = m.to - m.from <= KEEP;
-  for (int job = wave_id(); job < 2 * nkv; job += 4) {
+  for (int job = 4 * blockIdx.z + wave_id(); job < 2 * nkv; job += 4 * gridDim.z) {
     const int j = job >> 1, is_v = job & 1;
     const T *src = (const T *)(is_v ? a.kv.v_pool : a.kv.k_pool) + (size_t)(m.blk + j) * bs * D + 8 * li;
     uint8_t *codes = (uint8_t *)(is_v ? a.v.kv.v_pool : a.v.kv.k_pool) + (size_t)(m.blk8 + j) * bs * D;
@@ -336,38 +359,56 @@ __global__ __launch_bounds__(256) void k_cache8_pack(Cache8Move a) {
   }
 }
 
-// Unpack: a workgroup per block, which both pools hold in one piece; 16 codes per
-// thread.
+// Unpack: a share of the heads of a block, which both pools hold in one piece, per
+// workgroup; a thread turns as many codes as make 16 bytes, so that loads and stores
+// of a wave are one run of memory each.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_cache8_unpack(Cache8Move a) {
+  constexpr int N = 16 / sizeof(T), LPR = D / N;             // codes of a thread, threads of a row
   const int b = blockIdx.y, nkv = a.v.nkv, bs = a.v.kv.bs;
   const Moved m = moved_slots(a, b, blockIdx.x);
   if (m.from >= m.to) return;
-  const int per = bs * (D / 16);                             // pieces of a head
-  for (int p = threadIdx.x; p < nkv * per; p += 256) {
-    const int j = p / per, s = (p - j * per) / (D / 16);
-    if (s < m.from || s >= m.to) continue;
+  const int per = (m.to - m.from) * LPR;                     // pieces of a head
+  for (int j = blockIdx.z; j < nkv; j += gridDim.z) {
     const float2 sc = *(const float2 *)(a.scales + 2 * (size_t)(m.blk8 + j));
-    const size_t from = (size_t)m.blk8 * bs * D + 16 * (size_t)p, to = (size_t)m.blk * bs * D + 16 * (size_t)p;
+    const size_t from = ((size_t)(m.blk8 + j) * bs + m.from) * D, to = ((size_t)(m.blk + j) * bs + m.from) * D;
+    const uint8_t *ck = (const uint8_t *)a.v.kv.k_pool + from, *cv = (const uint8_t *)a.v.kv.v_pool + from;
+    T *ok = (T *)a.kv.k_pool + to, *ov = (T *)a.kv.v_pool + to;
+    for (int p = threadIdx.x; p < per; p += 256) {
+      uint32_t c[2][N / 4];
 #pragma unroll
-    for (int is_v = 0; is_v < 2; ++is_v) {
-      const u32x4 c = *(const u32x4 *)((const uint8_t *)(is_v ? a.v.kv.v_pool : a.v.kv.k_pool) + from);
-      T *o = (T *)(is_v ? a.kv.v_pool : a.kv.k_pool) + to;
-      const float f = is_v ? sc.y : sc.x;
+      for (int i = 0; i < N / 4; ++i) {
+        c[0][i] = *(const uint32_t *)(ck + (size_t)p * N + 4 * i);
+        c[1][i] = *(const uint32_t *)(cv + (size_t)p * N + 4 * i);
+      }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)c[k], f, false);
-        const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)c[k], f, true);
-        const float y[4] = {lo[0], lo[1], hi[0], hi[1]};
-        store_n<T, 4>(o + 4 * k, y);
+      for (int w = 0; w < 2; ++w) {
+        const float f = w ? sc.y : sc.x;
+        u32x4 y;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            y[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[w][i], f, false));
+            y[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c[w][i], f, true));
+          }
+        } else {
+          const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)c[w][0], f, false);
+          const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)c[w][0], f, true);
+          y = u32x4{__float_as_uint(lo[0]), __float_as_uint(lo[1]), __float_as_uint(hi[0]), __float_as_uint(hi[1])};
+        }
+        *(u32x4 *)((w ? ov : ok) + (size_t)p * N) = y;
       }
     }
   }
 }
 
+constexpr int MOVE_FILL = 4096;
 template <typename T>
 static void pack_d(const Cache8Move &a, int d, bool unpack, hipStream_t s) {
-  const dim3 g((a.v.max_len + a.v.kv.bs - 1) / a.v.kv.bs, a.v.kv.n_seq), t(256);
+  const int columns = (a.v.max_len + a.v.kv.bs - 1) / a.v.kv.bs, nkv = a.v.nkv;
+  // heads over workgroups until those fill the chip
+  const long fill = MOVE_FILL / ((long)columns * a.v.kv.n_seq) + 1;
+  const dim3 g(columns, a.v.kv.n_seq, (int)min(fill, unpack ? (long)nkv : (nkv + 1l) / 2)), t(256);
 #define PRISM_MOVE(D)                                                             \
   if (unpack) hipLaunchKernelGGL((k_cache8_unpack<T, D>), g, t, 0, s, a);         \
   else hipLaunchKernelGGL((k_cache8_pack<T, D>), g, t, 0, s, a)

@@ -81,17 +81,21 @@ inline size_t cache_attend_scratch_up_to(int batch, int nkv, int g, int d, int s
   return most;
 }
 
-// Attention of several rows per sequence: rows whose (row, head) pairs of a KV head
-// fill the 16 columns of a matrix-core tile, and the tiles (segments, over all KV
-// heads) that T rows of B sequences can make: a sequence's last one may be short.
-constexpr int rows_per_tile(int g) { return 16 / g; }
-inline long rows_segments(int nkv, int g, int batch, int rows) {
-  const long tiles = (long)rows / rows_per_tile(g) + batch;
+// Attention of several rows per sequence.  A wave's tile has `cols` columns, (row,
+// head) pairs of a KV head: 16, and 32 where the rows are more than the sequences and
+// two tiles of outputs fit the registers (six rows of 4 heads over 8-bit caches of
+// 512 .. 16384 slots, 16 sequences: 105 us with 16, PENDING with 32).
+constexpr int rows_per_tile(int g, int cols) { return cols / g; }
+constexpr int rows_cols(bool bf16, int d, int batch, int rows) { return bf16 && d <= 128 && rows > batch ? 32 : 16; }
+// The tiles (segments, over all KV heads) that T rows of B sequences can make: a
+// sequence's last one may be short.
+inline long rows_segments(int nkv, int g, int cols, int batch, int rows) {
+  const long tiles = (long)rows / rows_per_tile(g, cols) + batch;
   return (tiles < rows ? tiles : rows) * nkv;
 }
 // Places of a segment at most.
-inline int rows_span(int g, int max_len, int window, int n_first) {
-  const long w = window ? (long)window + n_first + rows_per_tile(g) - 1 : max_len;
+inline int rows_span(int g, int cols, int max_len, int window, int n_first) {
+  const long w = window ? (long)window + n_first + rows_per_tile(g, cols) - 1 : max_len;
   return (int)(w < max_len ? w : max_len);
 }
 // A workgroup for each segment, and no join, where segments are short or fill the
@@ -105,13 +109,16 @@ constexpr int ROWS_FEW = 32, PROMPT_COLUMNS = 128;
 constexpr int PROMPT_FILL = 256, PROMPT_SPLITS = 16, PROMPT_PART = 256;
 constexpr int prompt_rows(int g) { return PROMPT_COLUMNS / g; }
 struct RowsPlan {
+  int cols;                       // columns of a tile of the first kernel
   int few;                        // rows of a sequence that the first kernel takes
   int segments, waves;            // of it (segments 0: it is not needed)
   bool direct;
   int prompt_segments, splits;    // of the other (0: not needed)
 };
-inline RowsPlan rows_plan(bool bf16, int nkv, int g, int batch, int rows, int span, int waves) {
-  RowsPlan p{0x7fffffff, 0, 0, true, 0, 1};
+inline RowsPlan rows_plan(bool bf16, int nkv, int g, int d, int batch, int rows, int max_len, int window, int n_first,
+                          int waves) {
+  RowsPlan p{rows_cols(bf16, d, batch, rows), 0x7fffffff, 0, 0, true, 0, 1};
+  const int span = rows_span(g, p.cols, max_len, window, n_first), rt = rows_per_tile(g, p.cols);
   const int few = ROWS_FEW / g;
   const bool prompts = bf16 && rows > few;
   if (prompts) {
@@ -125,9 +132,9 @@ inline RowsPlan rows_plan(bool bf16, int nkv, int g, int batch, int rows, int sp
     }
     if (batch == 1) return p;     // the kernel of prompts takes a lone sequence however short it is
   }
-  long n = rows_segments(nkv, g, batch, rows);
-  // short sequences among prompts have few / rows_per_tile tiles at most
-  const long top = prompts ? (long)batch * ((few + rows_per_tile(g) - 1) / rows_per_tile(g)) * nkv : n;
+  long n = rows_segments(nkv, g, p.cols, batch, rows);
+  // short sequences among prompts have few / rt tiles at most
+  const long top = prompts ? (long)batch * ((few + rt - 1) / rt) * nkv : n;
   n = n < top ? n : top;
   p.segments = (int)n;
   p.direct = span <= CACHE_DIRECT || n >= ROWS_DIRECT_SEGMENTS;
@@ -142,7 +149,7 @@ inline size_t rows_part_bytes(size_t parts, int d) {
 }
 inline size_t rows_scratch(int g, int d, const RowsPlan &p) {
   if (p.direct || !p.segments) return 0;
-  return rows_part_bytes((size_t)cache_partials(p.waves, p.segments) * rows_per_tile(g) * g, d);
+  return rows_part_bytes((size_t)cache_partials(p.waves, p.segments) * rows_per_tile(g, p.cols) * g, d);
 }
 inline size_t prompt_scratch(int nq, int d, int rows, const RowsPlan &p) {
   return p.prompt_segments && p.splits > 1 ? rows_part_bytes((size_t)p.splits * rows * nq, d) : 0;
@@ -153,9 +160,12 @@ inline size_t prompt_scratch(int nq, int d, int rows, const RowsPlan &p) {
 inline size_t rows_scratch_up_to(bool bf16, int nkv, int g, int d, int batch, int rows, int max_len, int waves) {
   size_t bytes = 0;
   if (max_len > CACHE_DIRECT) {
-    const long n = rows_segments(nkv, g, batch, rows);
-    const int most = (int)(n < ROWS_DIRECT_SEGMENTS ? n : ROWS_DIRECT_SEGMENTS - 1);
-    bytes += rows_part_bytes((size_t)cache_partials(waves, most) * rows_per_tile(g) * g, d);
+    for (int cols = 16; cols <= rows_cols(bf16, d, 0, rows); cols += 16) {   // (a smaller batch may have wider tiles)
+      const long n = rows_segments(nkv, g, cols, batch, rows);
+      const int most = (int)(n < ROWS_DIRECT_SEGMENTS ? n : ROWS_DIRECT_SEGMENTS - 1);
+      const size_t need = rows_part_bytes((size_t)cache_partials(waves, most) * rows_per_tile(g, cols) * g, d);
+      bytes = need > bytes ? need : bytes;
+    }
   }
   if (bf16 && max_len >= 2 * PROMPT_PART) {
     const long fill = (long)PROMPT_FILL * prompt_rows(g) / nkv + 1, all = 2 * fill + (rows < fill ? rows : fill);

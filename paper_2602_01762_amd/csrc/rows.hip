@@ -4,12 +4,11 @@
 // with a window W those from v - W on and the first n_first.
 //
 // The rows of a sequence are cut into tiles whose (row, head) pairs of one KV head
-// are the 16 columns of a matrix-core tile.  A segment is a tile of one KV head;
+// are the 16 columns of a matrix-core tile, or of two.  A segment is a tile of one KV head;
 // it walks the slots that any of its rows sees as "places": the first ones, then
 // those from the first row's window on.
 #include "cache.h"
 #include "cache_device.h"
-#include <type_traits>
 
 namespace prism {
 
@@ -46,7 +45,7 @@ __device__ __forceinline__ RowWalk row_walk(const RowsAttend &a) {
   const long v0 = (long)L + a.v.n_new;
   if (w.n > 0 && (L < 0 || v0 + w.n - 1 > a.v.max_len)) atomicOr(a.err, ERRF_CAPACITY);
   w.v0 = L < 0 ? NO_SLOTS : (int)min(v0, (long)a.v.max_len);
-  const int rt = rows_per_tile(a.g);
+  const int rt = rows_per_tile(a.g, a.cols);
   w.tiles = w.n > a.few ? 0 : (w.n + rt - 1) / rt;   // (k_rows_prompt's)
   if (a.direct) {
     w.count = 1;                           // an empty segment writes its zeros itself
@@ -96,7 +95,7 @@ __device__ __forceinline__ RowSegment row_segment_at(const RowsAttend &a, const 
   s.index = __builtin_amdgcn_readlane(w.seg_end, s.b) - tiles * a.v.nkv + run.head;
   s.j = run.head / tiles;
   s.tile = run.head - s.j * tiles;
-  const int rt = rows_per_tile(a.g);
+  const int rt = rows_per_tile(a.g, a.cols);
   s.i0 = s.tile * rt;
   s.rows = min(rt, __builtin_amdgcn_readlane(w.n, s.b) - s.i0);
   s.r = __builtin_amdgcn_readlane(w.r0, s.b) + s.i0;
@@ -160,32 +159,21 @@ struct Loader {
   }
 };
 // A value that is not finite must not meet the probability 0 of a column that does
-// not see it (0 times it is NaN).  Masked tiles that hold one multiply their values
-// with 0 in its place, and count what each column sees of them by a second product
-// (the prompts' kernel, whose registers have no room for it, keeps masks in LDS):
-// operands 1 for +inf, 128 for -inf, 2^14 for NaN, times 1 where the column sees
-// the place, exact for the up to 64 places of a tile.
-constexpr float ODD_POS = 1.f, ODD_NEG = 128.f, ODD_NAN = 16384.f;
-__device__ __forceinline__ void split_odd(float v, float &fin, float &code) {
-  const bool odd = !(fabsf(v) < INFINITY);
-  fin = odd ? 0.f : v;
-  code = !odd ? 0.f : v != v ? ODD_NAN : v > 0.f ? ODD_POS : ODD_NEG;
+// not see it (0 times it is NaN).  Of a masked tile that holds one, the values that
+// are not finite become 0 in LDS, and masks keep their places, for each dim those of
+// +inf, -inf and NaN; what a column sees of them is added to its outputs behind the
+// product.
+typedef uint64_t OddMask[3];
+template <typename T>
+__device__ __forceinline__ void take_odd(T *v, OddMask &m, int s) {
+  const float x = Ty<T>::ld(v, 0);
+  if (fabsf(x) < INFINITY) return;
+  atomicOr((unsigned long long *)&m[x != x ? 2 : x < 0.f], 1ull << s);
+  *v = 0;
 }
-template <int N>
-__device__ __forceinline__ void split_odd_bf16(const uint32_t (&v)[N], uint32_t (&fin)[N], uint32_t (&code)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float a, b, x, y;
-    split_odd(__uint_as_float(v[i] << 16), a, x);
-    split_odd(__uint_as_float(v[i] & 0xffff0000u), b, y);
-    fin[i] = pack_upper(a, b);
-    code[i] = pack_upper(x, y);
-  }
-}
-// What the counted values add to a sum.
-__device__ __forceinline__ float odd_sum(float n) {
-  const int c = (int)n, pos = c & 127, neg = (c >> 7) & 127;
-  return c >> 14 || (pos && neg) ? NAN : pos ? INFINITY : neg ? -INFINITY : 0.f;
+__device__ __forceinline__ float odd_sum(const OddMask &m, uint64_t see) {
+  const bool pos = m[0] & see, neg = m[1] & see, nan = m[2] & see;
+  return nan || (pos && neg) ? NAN : pos ? INFINITY : neg ? -INFINITY : 0.f;
 }
 
 // A wave takes tiles of TS places, as in the attention of one row per sequence
@@ -194,7 +182,7 @@ __device__ __forceinline__ float odd_sum(float n) {
 // holding one column's softmax state.  A column is a (row, head) pair, so a tile's
 // rows share what is loaded; where not every row sees every place of a tile, the
 // scores are masked place by place.
-template <typename T, int D, bool Q8, int NW>
+template <typename T, int D, bool Q8, int NT, int NW>
 __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_attend(RowsAttend a) {
   using M = Tile<T, D>;
   using Ld = Loader<T, D, Q8>;
@@ -208,17 +196,29 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
   const KvArgs &kv = a.v.kv;
   const RowWalk wk = row_walk(a);
   if (wk.bad) return;
-  const int rt = rows_per_tile(g), columns = rt * g, crow = col / g, chead = col - crow * g;
+  constexpr int NC = 16 * NT;                                // columns of the tile: n * 16 + col
+  const int columns = NC / g * g;
+  int crow[NT], chead[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    crow[n] = (16 * n + col) / g;
+    chead[n] = 16 * n + col - crow[n] * g;
+  }
   int u = blockIdx.x * wk.per;
   const int last = min(wk.total, u + wk.per);
   while (u < last) {
     const RowSegment sg = row_segment_at(a, wk, u, last);
     u += sg.granules;
-    const bool used = col < columns && crow < sg.rows;
-    const size_t hi = (size_t)(sg.r + crow) * a.nq + sg.j * g + chead;   // this column's row of q and out (used)
-    // what this column sees: slots below vis, from win on or below n_first
-    const int vis = used ? visible_of(sg.v0, sg.i0 + crow, a.v.max_len) : 0;
-    const int win = a.window ? vis - a.window : 0;
+    // of this lane's columns: whether there is a row, and what it sees: slots below
+    // vis, from win on or below n_first
+    bool used[NT];
+    int vis[NT], win[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      used[n] = 16 * n + col < columns && crow[n] < sg.rows;
+      vis[n] = used[n] ? visible_of(sg.v0, sg.i0 + crow[n], a.v.max_len) : 0;
+      win[n] = a.window ? vis[n] - a.window : 0;
+    }
     const int vis_min = visible_of(sg.v0, sg.i0, a.v.max_len);           // slots below it every row sees, if
     const int win_max = a.window ? visible_of(sg.v0, sg.i0 + sg.rows - 1, a.v.max_len) - a.window : 0;   // from here on
     const int32_t *table = kv.block_table + (size_t)sg.b * kv.mbps;
@@ -257,14 +257,20 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
         vr[i] = *(const u32x4 *)((const char *)kv.v_pool + at);
       }
     };
-    float m_run = -INFINITY, l_run = 0.f;
-    f32x4 o[ND];
+    float m_run[NT], l_run[NT];
+    f32x4 o[NT][ND];
+    u32x4 qf[NT][NK];
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    u32x4 qf[NK];
+    for (int n = 0; n < NT; ++n) {
+      m_run[n] = -INFINITY;
+      l_run[n] = 0.f;
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk)
-      qf[kk] = used ? *(const u32x4 *)((const T *)a.q + hi * D + (4 * kk + q4) * E) : u32x4{0, 0, 0, 0};
+      for (int dt = 0; dt < ND; ++dt) o[n][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const size_t hi = (size_t)(sg.r + crow[n]) * a.nq + sg.j * g + chead[n];
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk)
+        qf[n][kk] = used[n] ? *(const u32x4 *)((const T *)a.q + hi * D + (4 * kk + q4) * E) : u32x4{0, 0, 0, 0};
+    }
     constexpr int STEP = NW * TS;
     const int t0 = sg.p0 + wave * TS;
     int c1 = 0, b1 = 0;
@@ -311,151 +317,165 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
         load(row.row);
       }
       wave_lds_sync();
-      // scores S[place 16 st + 4 q4 + i][column col]
-      f32x4 sc[NS];
+      // scores S[place 16 st + 4 q4 + i][column 16 n + col]
+      f32x4 sc[NT][NS];
 #pragma unroll
       for (int st = 0; st < NS; ++st) {
-        sc[st] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk)
-          sc[st] = Ty<T>::mma(*(const u32x4 *)(s_k + M::at(16 * st + col, 4 * kk + q4)), qf[kk], sc[st]);
+        for (int n = 0; n < NT; ++n) sc[n][st] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+          const u32x4 kf = *(const u32x4 *)(s_k + M::at(16 * st + col, 4 * kk + q4));
+#pragma unroll
+          for (int n = 0; n < NT; ++n) sc[n][st] = Ty<T>::mma(kf, qf[n][kk], sc[n][st]);
+        }
       }
-      uint32_t sees = 0;                                   // bit 4 st + i: this column sees that place
-      float mx = -INFINITY;
+      uint32_t sees[NT];                                   // bit 4 st + i: the column sees that place
       const uint64_t mine = mask >> (4 * q4);              // from this lane's first place on
 #pragma unroll
-      for (int st = 0; st < NS; ++st)
+      for (int n = 0; n < NT; ++n) {
+        float mx = -INFINITY;
+        sees[n] = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          bool see = (uint32_t)(mine >> (16 * st)) & (1u << i);
-          if (!whole) {
-            const int slot = slot_of(t + 4 * q4 + 16 * st + i);
-            see &= slot < vis && (slot >= win || slot < a.n_first);
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            bool see = (uint32_t)(mine >> (16 * st)) & (1u << i);
+            if (!whole) {
+              const int slot = slot_of(t + 4 * q4 + 16 * st + i);
+              see &= slot < vis[n] && (slot >= win[n] || slot < a.n_first);
+            }
+            sees[n] |= (uint32_t)see << (4 * st + i);
+            sc[n][st][i] = see ? sc[n][st][i] * a.scale : -INFINITY;
+            mx = fmaxf(mx, sc[n][st][i]);
           }
-          sees |= (uint32_t)see << (4 * st + i);
-          sc[st][i] = see ? sc[st][i] * a.scale : -INFINITY;
-          mx = fmaxf(mx, sc[st][i]);
+        mx = fmaxf(mx, xor16_f(mx));
+        mx = fmaxf(mx, xor32_f(mx));
+        const float mn = fmaxf(m_run[n], mx);
+        // nothing but -inf so far: subtract 0, so that every p is 0 (a NaN score
+        // still makes its p, and with it the sum and the output, NaN)
+        const float ms = mn == -INFINITY ? 0.f : mn;
+        const float al = __builtin_amdgcn_exp2f(m_run[n] - ms);
+        m_run[n] = mn;
+        float ls = 0.f;
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sc[n][st][i] = __builtin_amdgcn_exp2f(sc[n][st][i] - ms);
+            ls += sc[n][st][i];
+          }
+        ls += xor16_f(ls);
+        ls += xor32_f(ls);
+        l_run[n] = l_run[n] * al + ls;
+        if (__ballot(al != 1.f)) {
+#pragma unroll
+          for (int dt = 0; dt < ND; ++dt) o[n][dt] *= al;
         }
-      mx = fmaxf(mx, xor16_f(mx));
-      mx = fmaxf(mx, xor32_f(mx));
-      const float mn = fmaxf(m_run, mx);
-      // nothing but -inf so far: subtract 0, so that every p is 0 (a NaN score
-      // still makes its p, and with it the sum and the output, NaN)
-      const float ms = mn == -INFINITY ? 0.f : mn;
-      const float al = __builtin_amdgcn_exp2f(m_run - ms);
-      m_run = mn;
-      float ls = 0.f;
-#pragma unroll
-      for (int st = 0; st < NS; ++st)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          sc[st][i] = __builtin_amdgcn_exp2f(sc[st][i] - ms);
-          ls += sc[st][i];
-        }
-      ls += xor16_f(ls);
-      ls += xor32_f(ls);
-      l_run = l_run * al + ls;
-      if (__ballot(al != 1.f)) {
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) o[dt] *= al;
       }
-      // O[dim 16 dt + 4 q4 + i][column col]
+      // O[dim 16 dt + 4 q4 + i][column 16 n + col]
       constexpr int NP = sizeof(T) == 2 && NS > 1 ? 2 : 1;   // groups of 16 places per bf16 MFMA (32 places, or 16)
-      auto product = [&](auto masked) {
-        constexpr bool ODD = decltype(masked)::value;
-        f32x4 count[ODD ? ND : 1];
-        if constexpr (ODD) {
-#pragma unroll
-          for (int dt = 0; dt < ND; ++dt) count[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      OddMask *masks = (OddMask *)s_k;                     // [D], over the keys, whose scores are done
+      static_assert(D * sizeof(OddMask) <= TILE, "masks fit the K tile");
+      if (odd) {
+        wave_lds_sync();
+        for (int i = lane; i < 3 * D; i += 64) masks[i / 3][i % 3] = 0;
+        wave_lds_sync();
+        for (int i = lane; i < TS * D; i += 64) {
+          const int p = i / D, dim = i % D;
+          take_odd((T *)(s_v + M::at(p, dim / E)) + dim % E, masks[dim], p);
         }
+        wave_lds_sync();
+      }
 #pragma unroll
-        for (int st = 0; st < NS; st += NP) {
-          if constexpr (sizeof(T) == 2) {
-            uint32_t hi3[2 * NP], mid[2 * NP], lo[2 * NP], one[2 * NP];
+      for (int st = 0; st < NS; st += NP) {
+        if constexpr (sizeof(T) == 2) {
+          uint32_t hi[NT][2 * NP], mid[NT][2 * NP], lo[NT][2 * NP];
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int x = 0; x < NP; ++x) {
               uint32_t h[2], m[2], l[2];
-              split_bf16(sc[st + x], h, m, l);
+              split_bf16(sc[n][st + x], h, m, l);
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
-                hi3[2 * x + y] = h[y];
-                mid[2 * x + y] = m[y];
-                lo[2 * x + y] = l[y];
-                const uint32_t b = sees >> (4 * (st + x) + 2 * y);
-                one[2 * x + y] = (b & 1 ? 0x3f80u : 0u) | (b & 2 ? 0x3f800000u : 0u);
+                hi[n][2 * x + y] = h[y];
+                mid[n][2 * x + y] = m[y];
+                lo[n][2 * x + y] = l[y];
               }
             }
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) {
-              uint32_t v[2 * NP];
+          for (int dt = 0; dt < ND; ++dt) {
+            uint32_t v[2 * NP];
 #pragma unroll
-              for (int x = 0; x < NP; ++x) {
-                const char *pv = s_v + M::at(16 * (st + x) + 4 * q4 + (col >> 2), 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
-                const uint2 r = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
-                v[2 * x] = r.x;
-                v[2 * x + 1] = r.y;
-              }
-              uint32_t code[2 * NP];
-              if constexpr (ODD) {
-                uint32_t fin[2 * NP];
-                split_odd_bf16<2 * NP>(v, fin, code);
-#pragma unroll
-                for (int x = 0; x < 2 * NP; ++x) v[x] = fin[x];
-              }
-              // k = 8 q4 + e: places 16 st + 4 q4 + e, then the same of st + 1, in both operands
-              auto mma = [&](const uint32_t(&x)[2 * NP], const uint32_t(&y)[2 * NP], f32x4 acc) {
-                if constexpr (NP == 2)
-                  return Ty<T>::mma(u32x4{x[0], x[1], x[2], x[3]}, u32x4{y[0], y[1], y[2], y[3]}, acc);
-                else
-                  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, uint2{x[0], x[1]}),
-                                                                  __builtin_bit_cast(s16x4, uint2{y[0], y[1]}), acc, 0, 0, 0);
-              };
-              o[dt] = mma(v, hi3, o[dt]);
-              o[dt] = mma(v, mid, o[dt]);
-              o[dt] = mma(v, lo, o[dt]);
-              if constexpr (ODD) count[dt] = mma(code, one, count[dt]);
+            for (int x = 0; x < NP; ++x) {
+              const char *pv = s_v + M::at(16 * (st + x) + 4 * q4 + (col >> 2), 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
+              const uint2 r = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
+              v[2 * x] = r.x;
+              v[2 * x + 1] = r.y;
             }
-          } else {
-            // step i: place 4 q4 + i of each lane row
+            // k = 8 q4 + e: places 16 st + 4 q4 + e, then the same of st + 1, in both operands
+            auto mma = [&](const uint32_t(&x)[2 * NP], const uint32_t(&y)[2 * NP], f32x4 acc) {
+              if constexpr (NP == 2)
+                return Ty<T>::mma(u32x4{x[0], x[1], x[2], x[3]}, u32x4{y[0], y[1], y[2], y[3]}, acc);
+              else
+                return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, uint2{x[0], x[1]}),
+                                                                __builtin_bit_cast(s16x4, uint2{y[0], y[1]}), acc, 0, 0, 0);
+            };
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const char *pv = s_v + M::at(16 * st + 4 * q4 + i, 4 * dt + (col >> 2)) + 4 * (col & 3);
-                float v = *(const float *)pv, code;
-                if constexpr (ODD) {
-                  float fin;
-                  split_odd(v, fin, code);
-                  v = fin;
-                }
-                o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[st][i], o[dt], 0, 0, 0);
-                if constexpr (ODD)
-                  count[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(code, (sees >> (4 * st + i)) & 1 ? 1.f : 0.f, count[dt], 0, 0, 0);
-              }
+            for (int n = 0; n < NT; ++n) {
+              o[n][dt] = mma(v, hi[n], o[n][dt]);
+              o[n][dt] = mma(v, mid[n], o[n][dt]);
+              o[n][dt] = mma(v, lo[n], o[n][dt]);
+            }
           }
-        }
-        if constexpr (ODD) {
+        } else {
+          // step i: place 4 q4 + i of each lane row
 #pragma unroll
           for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[dt][i] += odd_sum(count[dt][i]);
+            for (int i = 0; i < 4; ++i) {
+              const char *pv = s_v + M::at(16 * st + 4 * q4 + i, 4 * dt + (col >> 2)) + 4 * (col & 3);
+              const float v = *(const float *)pv;
+#pragma unroll
+              for (int n = 0; n < NT; ++n) o[n][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[n][st][i], o[n][dt], 0, 0, 0);
+            }
         }
-      };
-      if (odd) product(std::true_type{});
-      else product(std::false_type{});
+      }
+      if (odd) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          // the places that this column sees, those of its four lanes
+          uint64_t see = 0;
+#pragma unroll
+          for (int st = 0; st < NS; ++st) see |= (uint64_t)((sees[n] >> (4 * st)) & 15) << (16 * st + 4 * q4);
+          see |= __shfl_xor(see, 16, 64);
+          see |= __shfl_xor(see, 32, 64);
+#pragma unroll
+          for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              o[n][dt][i] += odd_sum(masks[16 * dt + 4 * q4 + i], see);
+              __builtin_amdgcn_sched_barrier(0);            // few registers rather than overlap
+            }
+        }
+      }
       wave_lds_sync();                                 // reads done before the next tile's writes
     }
     if constexpr (NW > 1) {
-      __shared__ float s_m[NW][16], s_l[NW][16];
-      float *so = (float *)s_k;                        // this wave's outputs [16][D]: within its K and V tiles
-      static_assert(2 * TILE >= 16 * D * (int)sizeof(float), "outputs of a wave fit its tiles");
-      if (used) {
+      __shared__ float s_m[NW][NC], s_l[NW][NC];
+      float *so = (float *)s_k;                        // this wave's outputs [NC][D]: within its K and V tiles
+      static_assert(2 * TILE >= NC * D * (int)sizeof(float), "outputs of a wave fit its tiles");
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(so + col * D + 16 * dt + 4 * q4) = o[dt];
-      }
-      if (q4 == 0) {
-        s_m[wave][col] = m_run;
-        s_l[wave][col] = l_run;
+      for (int n = 0; n < NT; ++n) {
+        if (used[n]) {
+#pragma unroll
+          for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(so + (16 * n + col) * D + 16 * dt + 4 * q4) = o[n][dt];
+        }
+        if (q4 == 0) {
+          s_m[wave][16 * n + col] = m_run[n];
+          s_l[wave][16 * n + col] = l_run[n];
+        }
       }
       __syncthreads();
       for (int e = threadIdx.x; e < sg.rows * g * D / 4; e += 64 * NW) {
@@ -477,13 +497,16 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
       }
       return;                                          // one segment per workgroup
     }
-    if (!used) continue;
-    const size_t part = (size_t)cache_partial(blockIdx.x, sg.index) * columns + col;
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(a.po + part * D + 16 * dt + 4 * q4) = o[dt];
-    if (q4 == 0) {
-      a.pm[part] = m_run;
-      a.pl[part] = l_run;
+    for (int n = 0; n < NT; ++n) {
+      if (!used[n]) continue;
+      const size_t part = (size_t)cache_partial(blockIdx.x, sg.index) * columns + 16 * n + col;
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) *(f32x4 *)(a.po + part * D + 16 * dt + 4 * q4) = o[n][dt];
+      if (q4 == 0) {
+        a.pm[part] = m_run[n];
+        a.pl[part] = l_run[n];
+      }
     }
   }
 }
@@ -496,7 +519,7 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttend a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const RowWalk w = row_walk(a);
   if (w.bad) return;
-  const int rt = rows_per_tile(a.g), columns = rt * a.g;
+  const int rt = rows_per_tile(a.g, a.cols), columns = rt * a.g;
   // the column of this group of threads (whole waves), the same in each of its lanes
   const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * (256 / TH) + tid / TH), t = tid % TH;
   const int seg = id / columns, col = id - seg * columns;
@@ -598,7 +621,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
   constexpr int BN = PT::BN, NS = BN / 32, NK = D / 16, ND = D / 32;
   constexpr int LPR = Q8 ? D / 16 : D / 8, RPI = 256 / LPR, NI = (BN + RPI - 1) / RPI;   // lanes per stored row, rows per load, loads
   __shared__ __attribute__((aligned(16))) char s_k[2][PT::BYTES], s_v[2][PT::BYTES];
-  __shared__ uint64_t s_mask[D][3];                         // places with +inf, -inf, NaN in each dim
+  __shared__ OddMask s_mask[D];
   __shared__ int s_odd[3];                                  // of the tiles in turn: whether a masked one holds
                                                             // what is not finite
   const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, half = lane >> 5, g = a.g, nkv = a.v.nkv;
@@ -796,11 +819,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
       lds_barrier();
       for (int i = tid; i < BN * D; i += 256) {
         const int s = i / D, dim = i % D;
-        uint16_t *v = (uint16_t *)(s_v[buf] + PT::v_at(s, dim >> 3) + 2 * (dim & 7));
-        const uint32_t x = *v;
-        if ((x & 0x7f80u) != 0x7f80u) continue;
-        atomicOr((unsigned long long *)&s_mask[dim][(x & 0x7fu) ? 2 : x >> 15], 1ull << s);
-        *v = 0;
+        take_odd((bf16_t *)(s_v[buf] + PT::v_at(s, dim >> 3)) + (dim & 7), s_mask[dim], s);
       }
       lds_barrier();
     }
@@ -810,6 +829,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
     if (!skip) {
       // scores S[place 32 st + 8 jj + 4 half + i][column lane % 32]
       f32x16 sc[NS];
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int st = 0; st < NS; ++st) {
 #pragma unroll
@@ -820,6 +840,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
               __builtin_bit_cast(bf16x8, *(const u32x4 *)(bk + get_k[kk % KA] + PT::step(32 * st, 16 * (kk / KA)))),
               __builtin_bit_cast(bf16x8, qf[kk]), sc[st], 0, 0, 0);
       }
+      __builtin_amdgcn_s_setprio(0);
       uint32_t sees = ~0u;                                  // bit 16 st + i
       if (!whole) {
         sees = 0;
@@ -860,6 +881,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
           l_run += sc[st][i];
         }
       // O[dim 32 dt + 8 jj + 4 half + i][column lane % 32]
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int x = 0; x < 2 * NS; ++x) {                    // places 16 x .. 16 x + 15
         u32x4 pb;
@@ -877,6 +899,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
               __builtin_bit_cast(bf16x8, u32x4{v[0].x, v[0].y, v[1].x, v[1].y}), __builtin_bit_cast(bf16x8, pb), o[dt], 0, 0, 0);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
       if (odd) {
         // the places that this column sees, those of both halves of the lanes
         uint64_t see = 0;
@@ -889,9 +912,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
         for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const uint64_t(&m)[3] = s_mask[32 * dt + 8 * (i >> 2) + 4 * half + (i & 3)];
-            const bool pos = m[0] & see, neg = m[1] & see, nan = m[2] & see;
-            o[dt][i] += nan || (pos && neg) ? NAN : pos ? INFINITY : neg ? -INFINITY : 0.f;
+            o[dt][i] += odd_sum(s_mask[32 * dt + 8 * (i >> 2) + 4 * half + (i & 3)], see);
             __builtin_amdgcn_sched_barrier(0);              // few registers rather than overlap
           }
       }
@@ -971,14 +992,17 @@ static void rows_d(const RowsAttend &a, hipStream_t s) {
   if (!a.segments) return;
   constexpr int NW = D * sizeof(T) > 512 ? 2 : 4;      // 64 KB of LDS
   const dim3 g(a.waves);
-  if (a.direct) {
-    hipLaunchKernelGGL((k_rows_attend<T, D, Q8, NW>), g, dim3(64 * NW), 0, s, a);
-    return;
+  const bool wide = a.cols == 32;
+  if constexpr (sizeof(T) == 2 && D <= 128) {
+    if (wide && a.direct) hipLaunchKernelGGL((k_rows_attend<T, D, Q8, 2, NW>), g, dim3(64 * NW), 0, s, a);
+    else if (wide) hipLaunchKernelGGL((k_rows_attend<T, D, Q8, 2, 1>), g, dim3(64), 0, s, a);
   }
-  hipLaunchKernelGGL((k_rows_attend<T, D, Q8, 1>), g, dim3(64), 0, s, a);
+  if (!wide && a.direct) hipLaunchKernelGGL((k_rows_attend<T, D, Q8, 1, NW>), g, dim3(64 * NW), 0, s, a);
+  else if (!wide) hipLaunchKernelGGL((k_rows_attend<T, D, Q8, 1, 1>), g, dim3(64), 0, s, a);
+  if (a.direct) return;
   // partials of a segment on average: few, and a wave adds a column's
   const bool few = a.waves / a.segments <= 16;
-  const long columns = (long)a.segments * rows_per_tile(a.g) * a.g;
+  const long columns = (long)a.segments * rows_per_tile(a.g, a.cols) * a.g;
   if (few) hipLaunchKernelGGL((k_rows_join<T, D, 64>), dim3((columns + 3) / 4), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((k_rows_join<T, D, 256>), dim3(columns), dim3(256), 0, s, a);
 }

@@ -224,8 +224,6 @@ int main() {
     const int top = 1 << (rand() % 12), max_len = 1 + rand() % (1 << (rand() % 18 + 1));
     long T = 0;
     std::vector<int> counts;
-    const int rt = rows_per_tile(g);
-    if (rt < 1 || rt * g > 16) return 1;
     for (int b = 0; b < B; ++b) {
       const int n = rand() % 4 ? rand() % (top + 1) : 0;
       T += n;
@@ -235,9 +233,10 @@ int main() {
     if (T < 1) T = 1;
     const int window = rand() % 2 ? 1 + rand() % 5000 : 0, n_first = rand() % 40, waves = cache_waves(d * 2);
     const bool bf16 = rand() % 2;
-    const int span = rows_span(g, max_len, window, n_first);
+    const RowsPlan p = rows_plan(bf16, nkv, g, d, B, (int)T, max_len, window, n_first, waves);
+    const int span = rows_span(g, p.cols, max_len, window, n_first), rt = rows_per_tile(g, p.cols);
     if (span < 1 || span > max_len) return 2;
-    const RowsPlan p = rows_plan(bf16, nkv, g, B, (int)T, span, waves);
+    if (rt < 1 || rt * g > p.cols || (p.cols != 16 && p.cols != 32)) return 1;
     long few = 0, many = 0;                       // segments of each kernel
     int longest = 0;
     for (int b = 0; b < B; ++b) {

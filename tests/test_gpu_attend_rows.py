@@ -464,12 +464,12 @@ def test_refusals():
         with pytest.raises(PrismError) as e:
             call()
         assert e.value.status == -1 and str(e.value), i
-    out, scratch = torch.empty_like(q), torch.empty(1 << 24, dtype=torch.uint8, device=DEV)
+    out, scratch = torch.empty_like(q), torch.empty(1 << 26, dtype=torch.uint8, device=DEV)
     kv8 = c.kv8()
     io = B.prism_cache_row_attention()
     io.kv, io.rows, io.d_q, io.d_out = ctypes.addressof(kv), 2, B.ptr(q), B.ptr(out)
     io.d_scratch, io.scratch_bytes = B.ptr(scratch), B.prism_cache_rows_scratch(c.dr.ctx, 2, 2, 0)
-    assert 0 < io.scratch_bytes <= 1 << 24
+    assert 0 < io.scratch_bytes <= 1 << 26
     B.prism_cache_attend_rows(c.dr.ctx, io)
     for field, value in (("scratch_bytes", 16), ("d_scratch", 0), ("d_q", 0), ("d_q", B.ptr(q) + 2),
                          ("d_out", B.ptr(out) + 8), ("kv", None), ("kv8", ctypes.addressof(kv8)), ("rows", 3)):

@@ -106,7 +106,7 @@ def append(c, counts, positions=None, gains=True, pad=0, std=1.5, offsets=True, 
     torch.cuda.synchronize()
     x, got = f64(qkv), f64(out)
     gains64 = [None if t is None else f64(t) for t in g]
-    half = 2.0 ** -8 if c.dt == torch.bfloat16 else 2.0 ** -24
+    half = 2.0 ** -8 if c.dt == torch.bfloat16 else 0.0
     r0 = 0
     for b, n in enumerate(counts):
         rows = np.zeros((2, n, c.nkv, c.d))
@@ -115,7 +115,12 @@ def append(c, counts, positions=None, gains=True, pad=0, std=1.5, offsets=True, 
             with np.errstate(invalid="ignore"):
                 q, rows[0, i], rows[1, i] = C8.append_row(x[r0 + i], c.nq, c.nkv, p, 1e4, float(np.float32(EPS)), *gains64)
             top = np.abs(q).max(axis=1, keepdims=True)
-            lim = half * np.abs(q) + (2.0 ** -44 + p * 2.0 ** -50) * top
+            y = x[r0 + i, : c.nq]
+            if gains64[0] is not None:
+                y = y / np.sqrt(np.mean(y * y, -1, keepdims=True) + EPS) * gains64[0]
+            pair = np.abs(y[:, : c.d // 2]) + np.abs(y[:, c.d // 2:])
+            lim = half * np.abs(q) + (c.d / 2 + 10) * 2.0 ** -24 * (np.concatenate([pair, pair], -1) + np.abs(q))
+            lim = lim + p * 2.0 ** -50 * top
             over = float(np.max(np.abs(got[r0 + i] - q) / lim))
             assert over <= 1, (b, i, over)
         for w in range(2):
