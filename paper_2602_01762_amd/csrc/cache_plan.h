@@ -105,7 +105,7 @@ constexpr int ROWS_DIRECT_SEGMENTS = 2048;
 // kernel of prompts, in tiles of PROMPT_COLUMNS; where those are fewer than
 // PROMPT_FILL over all KV heads, each is split along its places into at most
 // PROMPT_SPLITS parts of PROMPT_PART at least, up to twice PROMPT_FILL in all.
-constexpr int ROWS_FEW = 32, PROMPT_COLUMNS = 128;
+constexpr int ROWS_FEW = 32, PROMPT_COLUMNS = 128, PROMPT_LEAST = 512;
 constexpr int PROMPT_FILL = 256, PROMPT_SPLITS = 16, PROMPT_PART = 256;
 constexpr int prompt_rows(int g) { return PROMPT_COLUMNS / g; }
 struct RowsPlan {
@@ -115,12 +115,12 @@ struct RowsPlan {
   bool direct;
   int prompt_segments, splits;    // of the other (0: not needed)
 };
-inline RowsPlan rows_plan(bool bf16, int nkv, int g, int d, int batch, int rows, int max_len, int window, int n_first,
-                          int waves) {
+inline RowsPlan rows_plan(bool bf16, int nkv, int g, int d, int batch, int rows, bool one_each, int max_len, int window,
+                          int n_first, int waves) {
   RowsPlan p{rows_cols(bf16, d, batch, rows), 0x7fffffff, 0, 0, true, 0, 1};
   const int span = rows_span(g, p.cols, max_len, window, n_first), rt = rows_per_tile(g, p.cols);
   const int few = ROWS_FEW / g;
-  const bool prompts = bf16 && rows > few;
+  const bool prompts = bf16 && !one_each && rows > few && (batch == 1 || (long)rows * g > PROMPT_LEAST);
   if (prompts) {
     const long tiles = (long)rows / prompt_rows(g) + batch, full = (rows + prompt_rows(g) - 1l) / prompt_rows(g) * nkv;
     p.few = few;

@@ -116,6 +116,13 @@ struct Loader {
   static constexpr int SZ = Q8 ? 1 : (int)sizeof(T);                    // bytes of a stored value
   static constexpr int LPR = D * SZ / 16, RPI = 64 / LPR;               // lanes per row, rows per load
   static constexpr int NI = Tile<T, D>::TS / RPI;                       // loads per tile
+  // byte of piece c of row s of the values' tile: in bf16 the transposing read takes
+  // two pieces of 8 rows at a time, which this puts in all 64 banks
+  __device__ static int v_at(int s, int c) {
+    constexpr int L = Tile<T, D>::LPR;
+    if constexpr (sizeof(T) == 4) return Tile<T, D>::at(s, c);
+    return (s * L + (c ^ (L >= 16 ? 2 * (s & 7) : L == 8 ? s & 6 : (s >> 1) & 2))) * 16;
+  }
   // whether one of the values of a piece is an infinity or a NaN
   __device__ static bool odd(u32x4 x) {
     bool r = false;
@@ -133,10 +140,11 @@ struct Loader {
     return r;
   }
   // piece li of row s of a tile to LDS
+  template <bool V>
   __device__ static void put(char *tile, int s, int li, u32x4 x, float scale) {
-    using M = Tile<T, D>;
+    auto at = [](int s, int c) { return V ? v_at(s, c) : Tile<T, D>::at(s, c); };
     if constexpr (!Q8) {
-      *(u32x4 *)(tile + M::at(s, li)) = x;
+      *(u32x4 *)(tile + at(s, li)) = x;
     } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -146,14 +154,14 @@ struct Loader {
           y[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[2 * h + i], scale, false));
           y[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[2 * h + i], scale, true));
         }
-        *(u32x4 *)(tile + M::at(s, 2 * li + h)) = y;
+        *(u32x4 *)(tile + at(s, 2 * li + h)) = y;
       }
     } else {
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)x[h], scale, false);
         const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)x[h], scale, true);
-        *(f32x4 *)(tile + M::at(s, 4 * li + h)) = f32x4{lo[0], lo[1], hi[0], hi[1]};
+        *(f32x4 *)(tile + at(s, 4 * li + h)) = f32x4{lo[0], lo[1], hi[0], hi[1]};
       }
     }
   }
@@ -253,8 +261,8 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
       for (int i = 0; i < NI; ++i) {
         const uint32_t r = __shfl(row, i * RPI + grp, 64);
         const size_t at = (size_t)(r == NO_ROW ? 0 : r) * (D * Ld::SZ) + 16 * li;   // a masked place reads row 0
-        kr[i] = *(const u32x4 *)((const char *)kv.k_pool + at);
-        vr[i] = *(const u32x4 *)((const char *)kv.v_pool + at);
+        kr[i] = stream16((const char *)kv.k_pool + at);
+        vr[i] = stream16((const char *)kv.v_pool + at);
       }
     };
     float m_run[NT], l_run[NT];
@@ -306,8 +314,8 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int s = i * RPI + grp;
-        Ld::put(s_k, s, li, kr[i], Q8 ? __shfl(row.ks, s, 64) : 1.f);
-        Ld::put(s_v, s, li, vr[i], Q8 ? __shfl(row.vs, s, 64) : 1.f);
+        Ld::template put<false>(s_k, s, li, kr[i], Q8 ? __shfl(row.ks, s, 64) : 1.f);
+        Ld::template put<true>(s_v, s, li, vr[i], Q8 ? __shfl(row.vs, s, 64) : 1.f);
       }
       if (t + STEP < sg.p1) {
         row = Row{NO_ROW, 1.f, 1.f};
@@ -383,7 +391,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
         wave_lds_sync();
         for (int i = lane; i < TS * D; i += 64) {
           const int p = i / D, dim = i % D;
-          take_odd((T *)(s_v + M::at(p, dim / E)) + dim % E, masks[dim], p);
+          take_odd((T *)(s_v + Ld::v_at(p, dim / E)) + dim % E, masks[dim], p);
         }
         wave_lds_sync();
       }
@@ -409,7 +417,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
             uint32_t v[2 * NP];
 #pragma unroll
             for (int x = 0; x < NP; ++x) {
-              const char *pv = s_v + M::at(16 * (st + x) + 4 * q4 + (col >> 2), 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
+              const char *pv = s_v + Ld::v_at(16 * (st + x) + 4 * q4 + (col >> 2), 2 * dt + ((col & 3) >> 1)) + 8 * (col & 1);
               const uint2 r = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)pv));
               v[2 * x] = r.x;
               v[2 * x + 1] = r.y;
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
           for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const char *pv = s_v + M::at(16 * st + 4 * q4 + i, 4 * dt + (col >> 2)) + 4 * (col & 3);
+              const char *pv = s_v + Ld::v_at(16 * st + 4 * q4 + i, 4 * dt + (col >> 2)) + 4 * (col & 3);
               const float v = *(const float *)pv;
 #pragma unroll
               for (int n = 0; n < NT; ++n) o[n][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[n][st][i], o[n][dt], 0, 0, 0);
@@ -829,7 +837,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
     if (!skip) {
       // scores S[place 32 st + 8 jj + 4 half + i][column lane % 32]
       f32x16 sc[NS];
-      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int st = 0; st < NS; ++st) {
 #pragma unroll
@@ -840,7 +847,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
               __builtin_bit_cast(bf16x8, *(const u32x4 *)(bk + get_k[kk % KA] + PT::step(32 * st, 16 * (kk / KA)))),
               __builtin_bit_cast(bf16x8, qf[kk]), sc[st], 0, 0, 0);
       }
-      __builtin_amdgcn_s_setprio(0);
       uint32_t sees = ~0u;                                  // bit 16 st + i
       if (!whole) {
         sees = 0;
@@ -881,7 +887,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
           l_run += sc[st][i];
         }
       // O[dim 32 dt + 8 jj + 4 half + i][column lane % 32]
-      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int x = 0; x < 2 * NS; ++x) {                    // places 16 x .. 16 x + 15
         u32x4 pb;
@@ -899,7 +904,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
               __builtin_bit_cast(bf16x8, u32x4{v[0].x, v[0].y, v[1].x, v[1].y}), __builtin_bit_cast(bf16x8, pb), o[dt], 0, 0, 0);
         }
       }
-      __builtin_amdgcn_s_setprio(0);
       if (odd) {
         // the places that this column sees, those of both halves of the lanes
         uint64_t see = 0;

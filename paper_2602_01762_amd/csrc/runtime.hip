@@ -1836,7 +1836,7 @@ prism_status prism_cache_attend_rows(prism_ctx *c, const prism_cache_row_attenti
   if ((long)io->rows * c->nq >= 1l << 30) return fail(c, PRISM_ERR_SHAPE, "%d rows of %d heads", io->rows, c->nq);
   CHECK(check_rows(c, io->d_q, "d_q"));
   CHECK(check_rows(c, io->d_out, "d_out"));
-  const RowsPlan p = rows_plan(c->bf16, c->nkv, g, c->d, B, io->rows, len, io->window, io->n_first,
+  const RowsPlan p = rows_plan(c->bf16, c->nkv, g, c->d, B, io->rows, !io->d_offsets, len, io->window, io->n_first,
                                cache_waves(c->d * c->esz));
   const size_t first = rows_scratch(g, c->d, p), second = prompt_scratch(c->nq, c->d, io->rows, p);
   CHECK(check_scratch(c, io->d_scratch, io->scratch_bytes, first + second));

@@ -233,7 +233,7 @@ int main() {
     if (T < 1) T = 1;
     const int window = rand() % 2 ? 1 + rand() % 5000 : 0, n_first = rand() % 40, waves = cache_waves(d * 2);
     const bool bf16 = rand() % 2;
-    const RowsPlan p = rows_plan(bf16, nkv, g, d, B, (int)T, max_len, window, n_first, waves);
+    const RowsPlan p = rows_plan(bf16, nkv, g, d, B, (int)T, false, max_len, window, n_first, waves);
     const int span = rows_span(g, p.cols, max_len, window, n_first), rt = rows_per_tile(g, p.cols);
     if (span < 1 || span > max_len) return 2;
     if (rt < 1 || rt * g > p.cols || (p.cols != 16 && p.cols != 32)) return 1;
