@@ -256,6 +256,8 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
       return r;
     };
     u32x4 kr[NI], vr[NI];
+    // nontemporal: where tiles of a sequence share its slots that costs at most 3%
+    // (1000 fp32 rows of 32 heads), where each slot is read once it gives 3 to 8
     auto load = [&](uint32_t row) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
@@ -284,8 +286,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
     int c1 = 0, b1 = 0;
     Row row{NO_ROW, 1.f, 1.f};
     if (t0 < sg.p1) {
-      const int c0 = column(t0 + lane);
-      const int b0 = block(c0);
+      const int c0 = column(t0 + lane), b0 = block(c0);
       c1 = column(t0 + STEP + lane);
       b1 = block(c1);
       if (lane < TS) row = row_of(t0 + lane, c0, b0);
@@ -342,23 +343,26 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
       const uint64_t mine = mask >> (4 * q4);              // from this lane's first place on
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
+        sees[n] = ~0u;
+        if (!whole || mask != FULL) {
+          sees[n] = 0;
+#pragma unroll
+          for (int st = 0; st < NS; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int slot = slot_of(t + 4 * q4 + 16 * st + i);
+              const bool see = ((uint32_t)(mine >> (16 * st)) & (1u << i)) && slot < vis[n] && (slot >= win[n] || slot < a.n_first);
+              sees[n] |= (uint32_t)see << (4 * st + i);
+              sc[n][st][i] = see ? sc[n][st][i] : -INFINITY;
+            }
+        }
         float mx = -INFINITY;
-        sees[n] = 0;
 #pragma unroll
         for (int st = 0; st < NS; ++st)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            bool see = (uint32_t)(mine >> (16 * st)) & (1u << i);
-            if (!whole) {
-              const int slot = slot_of(t + 4 * q4 + 16 * st + i);
-              see &= slot < vis[n] && (slot >= win[n] || slot < a.n_first);
-            }
-            sees[n] |= (uint32_t)see << (4 * st + i);
-            sc[n][st][i] = see ? sc[n][st][i] * a.scale : -INFINITY;
-            mx = fmaxf(mx, sc[n][st][i]);
-          }
+          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[n][st][i]);
         mx = fmaxf(mx, xor16_f(mx));
-        mx = fmaxf(mx, xor32_f(mx));
+        mx = fmaxf(mx, xor32_f(mx)) * a.scale;
         const float mn = fmaxf(m_run[n], mx);
         // nothing but -inf so far: subtract 0, so that every p is 0 (a NaN score
         // still makes its p, and with it the sum and the output, NaN)
@@ -370,7 +374,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
         for (int st = 0; st < NS; ++st)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            sc[n][st][i] = __builtin_amdgcn_exp2f(sc[n][st][i] - ms);
+            sc[n][st][i] = __builtin_amdgcn_exp2f(fmaf(sc[n][st][i], a.scale, -ms));
             ls += sc[n][st][i];
           }
         ls += xor16_f(ls);

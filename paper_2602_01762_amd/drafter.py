@@ -544,7 +544,7 @@ class Drafter:
             io.d_out = out.data_ptr()
         else:
             io.d_out = self._expect(out, "out", shape, dt)
-        sums = torch.empty(shape[:2], dtype=torch.float32, device=self.device) if lse else None
+        sums = q.new_empty(shape[:2], dtype=torch.float32) if lse else None
         io.d_lse = None if sums is None else sums.data_ptr()
         io.scratch_bytes, scratch = self._scratch(None, nb, max_len, q, T)
         io.d_scratch = None if scratch is None else scratch.data_ptr()
