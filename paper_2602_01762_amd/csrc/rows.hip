@@ -184,6 +184,25 @@ __device__ __forceinline__ float odd_sum(const OddMask &m, uint64_t see) {
   return nan || (pos && neg) ? NAN : pos ? INFINITY : neg ? -INFINITY : 0.f;
 }
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+}
+// Four probabilities as hi + lo: the first 8 bits, cut off, and what is left rounded to
+// 8 (2^-16 of the value at most), neither negative, nor 0 but for p = 0, as in
+// split_bf16.
+__device__ __forceinline__ void pair_bf16(const f32x4 &p, uint32_t (&hi)[2], uint32_t (&lo)[2]) {
+  float l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    l[i] = fmaxf(p[i] - __uint_as_float(__float_as_uint(p[i]) & 0xffff0000u), fminf(p[i], 0x1p-126f));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    hi[i] = pack_upper(p[2 * i], p[2 * i + 1]);
+    lo[i] = pack_bf16(l[2 * i], l[2 * i + 1]);
+  }
+}
+
 // A wave takes tiles of TS places, as in the attention of one row per sequence
 // (cache.hip): rows loaded whole, into operand order through LDS, scores as MFMAs of
 // 16 places x 16 columns, outputs as MFMAs of 16 dims x 16 columns, each lane
@@ -408,12 +427,13 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
 #pragma unroll
             for (int x = 0; x < NP; ++x) {
               uint32_t h[2], m[2], l[2];
-              split_bf16(sc[n][st + x], h, m, l);
+              if constexpr (NT == 1) split_bf16(sc[n][st + x], h, m, l);
+              else pair_bf16(sc[n][st + x], h, m);
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
                 hi[n][2 * x + y] = h[y];
                 mid[n][2 * x + y] = m[y];
-                lo[n][2 * x + y] = l[y];
+                if constexpr (NT == 1) lo[n][2 * x + y] = l[y];
               }
             }
 #pragma unroll
@@ -438,7 +458,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
             for (int n = 0; n < NT; ++n) {
               o[n][dt] = mma(v, hi[n], o[n][dt]);
               o[n][dt] = mma(v, mid[n], o[n][dt]);
-              o[n][dt] = mma(v, lo[n], o[n][dt]);
+              if constexpr (NT == 1) o[n][dt] = mma(v, lo[n], o[n][dt]);
             }
           }
         } else {
@@ -604,11 +624,7 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttend a) {
 // of two LDS buffers, one tile ahead of the products, their loads two tiles ahead
 // and block-table lookups three: one barrier per tile.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr float PROMPT_SLACK = 8.f;
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-}
 // LDS written by the workgroup is there, with global loads still in flight
 __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
