@@ -80,9 +80,9 @@ __device__ __forceinline__ float to_odd(double x) {
 // between keeps the side (to_odd).  Queries, which have no such borders, in fp32.  Up to 16 new rows of a block stay in registers
 // between the maximum and the codes; of more (larger blocks), the rows are read
 // twice.
-constexpr int APPEND8_ROWS = 16;
+constexpr int APPEND8_ROWS = 16, APPEND8_FILL = 1024;
 template <typename T, int D>
-__global__ __launch_bounds__(512) void k_cache8_append(Cache8Append a) {
+__global__ __launch_bounds__(256) void k_cache8_append(Cache8Append a) {
   constexpr int LPH = D / 16, HPW = 64 / LPH, IT = (APPEND8_ROWS + HPW - 1) / HPW;
   const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, NW = blockDim.x >> 6;
   __shared__ double cs[APPEND8_ROWS][D / 2], sn[APPEND8_ROWS][D / 2];
@@ -269,8 +269,8 @@ static void append8_d(const Cache8Append &a, int d, hipStream_t s) {
   // blocks that can receive rows: each row one, each sequence ceil((at + n) / bs)
   long blocks = a.rows;
   if (a.offsets) blocks = min(blocks, (long)a.rows / bs + 2 * B);
-  const int nw = min(8, nh);
-  const int share = (int)max(1l, min((long)(nh + nw - 1) / nw, 1024 / max(1l, blocks)));
+  const int nw = min(4, nh);
+  const int share = (int)max(1l, min((long)(nh + nw - 1) / nw, APPEND8_FILL / max(1l, blocks)));
   const dim3 g(blocks, share), t(64 * nw);
   if (d == 32) hipLaunchKernelGGL((k_cache8_append<T, 32>), g, t, 0, s, a);
   else if (d == 64) hipLaunchKernelGGL((k_cache8_append<T, 64>), g, t, 0, s, a);
