@@ -102,12 +102,15 @@ inline int rows_span(int g, int cols, int max_len, int window, int n_first) {
 // chip by themselves; else equal runs of granules for all waves, as above.
 constexpr int ROWS_DIRECT_SEGMENTS = 2048;
 // In bf16 contexts, sequences of more rows than ROWS_FEW columns hold go to the
-// kernel of prompts, in tiles of PROMPT_COLUMNS; where those are fewer than
-// PROMPT_FILL over all KV heads, each is split along its places into at most
-// PROMPT_SPLITS parts of PROMPT_PART at least, up to twice PROMPT_FILL in all.
-constexpr int ROWS_FEW = 32, PROMPT_COLUMNS = 128, PROMPT_LEAST = 512;
-constexpr int PROMPT_FILL = 256, PROMPT_SPLITS = 16, PROMPT_PART = 256;
-constexpr int prompt_rows(int g) { return PROMPT_COLUMNS / g; }
+// kernel of prompts, in tiles of prompt_columns, 32 to a wave: 256 (with 128, two
+// workgroups to a CU: one prompt of 8192 rows, 32 heads, 692 us, so 634), and 128 where
+// a wave of outputs takes more than a quarter of a SIMD's registers.  Where tiles are
+// fewer than PROMPT_FILL over all KV heads, each is split along its places into at
+// most PROMPT_SPLITS parts of PROMPT_PART at least, up to twice PROMPT_FILL in all.
+constexpr int ROWS_FEW = 32, PROMPT_LEAST = 512;
+constexpr int PROMPT_FILL = 128, PROMPT_SPLITS = 16, PROMPT_PART = 256;
+constexpr int prompt_columns(int d) { return d == 256 ? 128 : 256; }
+constexpr int prompt_rows(int g, int d) { return prompt_columns(d) / g; }
 struct RowsPlan {
   int cols;                       // columns of a tile of the first kernel
   int few;                        // rows of a sequence that the first kernel takes
@@ -122,7 +125,7 @@ inline RowsPlan rows_plan(bool bf16, int nkv, int g, int d, int batch, int rows,
   const int few = ROWS_FEW / g;
   const bool prompts = bf16 && !one_each && rows > few && (batch == 1 || (long)rows * g > PROMPT_LEAST);
   if (prompts) {
-    const long tiles = (long)rows / prompt_rows(g) + batch, full = (rows + prompt_rows(g) - 1l) / prompt_rows(g) * nkv;
+    const long tiles = (long)rows / prompt_rows(g, d) + batch, full = (rows + prompt_rows(g, d) - 1l) / prompt_rows(g, d) * nkv;
     p.few = few;
     p.prompt_segments = (int)((tiles < rows ? tiles : rows) * nkv);
     if (full < PROMPT_FILL) {
@@ -168,7 +171,7 @@ inline size_t rows_scratch_up_to(bool bf16, int nkv, int g, int d, int batch, in
     }
   }
   if (bf16 && max_len >= 2 * PROMPT_PART) {
-    const long fill = (long)PROMPT_FILL * prompt_rows(g) / nkv + 1, all = 2 * fill + (rows < fill ? rows : fill);
+    const long fill = (long)PROMPT_FILL * prompt_rows(g, d) / nkv + 1, all = 2 * fill + (rows < fill ? rows : fill);
     const long each = (long)PROMPT_SPLITS * rows;
     bytes += rows_part_bytes((size_t)(all < each ? all : each) * nkv * g, d);
   }

@@ -611,7 +611,7 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttend a) {
 
 // ---------------------------------------------------------------- prompts
 // Sequences of more than a.few rows in bf16 contexts.  A workgroup takes a tile of
-// PROMPT_COLUMNS (row, head) pairs of one KV head, 32 columns a wave, and walks its
+// prompt_columns (row, head) pairs of one KV head, 32 columns a wave, and walks its
 // places BN at a time: S = K Q^T and O = V^T P as MFMAs of 32 x 32, so that a lane
 // holds one column's probabilities just where the second product takes them.
 // Probabilities are rounded to bf16 for it (2^-9 of each on average over a sum of
@@ -644,10 +644,10 @@ struct PromptTile {
   __device__ static constexpr int step(int rows, int pieces) { return (rows * LPR + pieces) * 16; }
 };
 template <int D, bool Q8>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAttend a) {
+__global__ __launch_bounds__(2 * prompt_columns(D), D == 256 ? 1 : 2) void k_rows_prompt(RowsAttend a) {
   using PT = PromptTile<D>;
   constexpr int BN = PT::BN, NS = BN / 32, NK = D / 16, ND = D / 32;
-  constexpr int LPR = Q8 ? D / 16 : D / 8, RPI = 256 / LPR, NI = (BN + RPI - 1) / RPI;   // lanes per stored row, rows per load, loads
+  constexpr int LPR = Q8 ? D / 16 : D / 8, RPI = 2 * prompt_columns(D) / LPR, NI = (BN + RPI - 1) / RPI;   // lanes per stored row, rows per load, loads
   __shared__ __attribute__((aligned(16))) char s_k[2][PT::BYTES], s_v[2][PT::BYTES];
   __shared__ OddMask s_mask[D];
   __shared__ int s_odd[3];                                  // of the tiles in turn: whether a masked one holds
@@ -661,7 +661,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
   {
     const RowWalk w = row_walk(a);
     if (w.bad) return;
-    const int tiles = w.n > a.few ? (w.n + prompt_rows(g) - 1) / prompt_rows(g) : 0;
+    const int tiles = w.n > a.few ? (w.n + prompt_rows(g, D) - 1) / prompt_rows(g, D) : 0;
     const uint32_t end = wave_scan((uint32_t)(lane < kv.n_seq ? tiles * nkv : 0));
     b = __popcll(__ballot(end <= blockIdx.x));
     if (b >= kv.n_seq) return;
@@ -670,8 +670,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
     tile = nt - 1 - at / nkv;
     j = at % nkv;
     sg.v0 = __builtin_amdgcn_readlane(w.v0, b);
-    sg.i0 = tile * prompt_rows(g);
-    sg.rows = min(prompt_rows(g), __builtin_amdgcn_readlane(w.n, b) - sg.i0);
+    sg.i0 = tile * prompt_rows(g, D);
+    sg.rows = min(prompt_rows(g, D), __builtin_amdgcn_readlane(w.n, b) - sg.i0);
     sg.r = __builtin_amdgcn_readlane(w.r0, b) + sg.i0;
   }
   int places;
@@ -684,10 +684,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
 
   // this lane's column, and what the wave's columns see
   const int cid = 32 * wave + (lane & 31), crow = cid / g, chead = cid - crow * g;
-  const bool used = crow < sg.rows && crow < prompt_rows(g);
+  const bool used = crow < sg.rows && crow < prompt_rows(g, D);
   const size_t hi = (size_t)(sg.r + crow) * a.nq + j * g + chead;
   const int vis = used ? visible_of(sg.v0, sg.i0 + crow, a.v.max_len) : 0, win = a.window ? vis - a.window : 0;
-  const int row_a = 32 * wave / g, row_b = min(sg.rows, prompt_rows(g)) - 1;
+  const int row_a = 32 * wave / g, row_b = min(sg.rows, prompt_rows(g, D)) - 1;
   const bool some = row_a <= row_b;
   const int vis_a = visible_of(sg.v0, sg.i0 + row_a, a.v.max_len);
   const int vis_b = visible_of(sg.v0, sg.i0 + min(row_b, (32 * wave + 31) / g), a.v.max_len);
@@ -843,9 +843,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
     const bool odd = s_odd[turn] != 0;
     const char *bk = s_k[buf], *bv = s_v[buf];
     if (odd) {                                              // the same for the workgroup
-      for (int i = tid; i < 3 * D; i += 256) s_mask[i / 3][i % 3] = 0;
+      for (int i = tid; i < 3 * D; i += 2 * prompt_columns(D)) s_mask[i / 3][i % 3] = 0;
       lds_barrier();
-      for (int i = tid; i < BN * D; i += 256) {
+      for (int i = tid; i < BN * D; i += 2 * prompt_columns(D)) {
         const int s = i / D, dim = i % D;
         take_odd((bf16_t *)(s_v[buf] + PT::v_at(s, dim >> 3)) + (dim & 7), s_mask[dim], s);
       }
@@ -858,15 +858,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_rows_prompt(RowsAtten
       // scores S[place 32 st + 8 jj + 4 half + i][column lane % 32]
       f32x16 sc[NS];
 #pragma unroll
-      for (int st = 0; st < NS; ++st) {
+      for (int st = 0; st < NS; ++st)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[st][i] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk)
+      for (int kk = 0; kk < NK; ++kk)
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
           sc[st] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
               __builtin_bit_cast(bf16x8, *(const u32x4 *)(bk + get_k[kk % KA] + PT::step(32 * st, 16 * (kk / KA)))),
               __builtin_bit_cast(bf16x8, qf[kk]), sc[st], 0, 0, 0);
-      }
       uint32_t sees = ~0u;                                  // bit 16 st + i
       if (!whole) {
         sees = 0;
@@ -1006,7 +1007,7 @@ static void rows_d(const RowsAttend &a, hipStream_t s) {
     if (a.prompt_segments) {
       RowsAttend p = a;
       p.few = a.segments ? a.few : 0;                      // alone it takes every sequence
-      hipLaunchKernelGGL((k_rows_prompt<D, Q8>), dim3(p.prompt_segments, p.splits), dim3(256), 0, s, p);
+      hipLaunchKernelGGL((k_rows_prompt<D, Q8>), dim3(p.prompt_segments, p.splits), dim3(2 * prompt_columns(D)), 0, s, p);
       if (p.splits > 1) {
         const long per = 256 / (D / 4), n = (long)p.rows * p.nq;
         hipLaunchKernelGGL((k_prompt_join<D>), dim3((n + per - 1) / per), dim3(256), 0, s, p, p.splits);

@@ -240,13 +240,13 @@ int main() {
     long few = 0, many = 0;                       // segments of each kernel
     int longest = 0;
     for (int b = 0; b < B; ++b) {
-      if (counts[b] > p.few) many += (counts[b] + prompt_rows(g) - 1) / prompt_rows(g) * nkv;
+      if (counts[b] > p.few) many += (counts[b] + prompt_rows(g, d) - 1) / prompt_rows(g, d) * nkv;
       else few += (counts[b] + rt - 1) / rt * nkv;
       longest = counts[b] > longest ? counts[b] : longest;
     }
     if (!p.segments) {                            // the prompts' kernel alone: one sequence
       if (B != 1 || !p.prompt_segments) return 3;
-      many = (longest + prompt_rows(g) - 1) / prompt_rows(g) * nkv;
+      many = (longest + prompt_rows(g, d) - 1) / prompt_rows(g, d) * nkv;
       few = 0;
     }
     if (few > p.segments || many > p.prompt_segments) return 4;
