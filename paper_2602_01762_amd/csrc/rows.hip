@@ -351,11 +351,25 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
       for (int st = 0; st < NS; ++st) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) sc[n][st] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (sizeof(T) == 4) {
+          // four sums of a quarter of the dims each: a single one of d terms in fp32 is
+          // twice as far off (1.2e-6 of the outputs with d = 256)
+          f32x4 part[3] = {};
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk) {
-          const u32x4 kf = *(const u32x4 *)(s_k + M::at(16 * st + col, 4 * kk + q4));
+          for (int kk = 0; kk < NK; ++kk) {
+            const f32x4 kf = *(const f32x4 *)(s_k + M::at(16 * st + col, 4 * kk + q4)), q = __builtin_bit_cast(f32x4, qf[0][kk]);
+            sc[0][st] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[0], q[0], sc[0][st], 0, 0, 0);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) sc[n][st] = Ty<T>::mma(kf, qf[n][kk], sc[n][st]);
+            for (int x = 0; x < 3; ++x) part[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[x + 1], q[x + 1], part[x], 0, 0, 0);
+          }
+          sc[0][st] = (sc[0][st] + part[0]) + (part[1] + part[2]);
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < NK; ++kk) {
+            const u32x4 kf = *(const u32x4 *)(s_k + M::at(16 * st + col, 4 * kk + q4));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sc[n][st] = Ty<T>::mma(kf, qf[n][kk], sc[n][st]);
+          }
         }
       }
       uint32_t sees[NT];                                   // bit 4 st + i: the column sees that place
