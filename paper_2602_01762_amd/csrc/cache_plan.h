@@ -84,14 +84,17 @@ inline size_t cache_attend_scratch_up_to(int batch, int nkv, int g, int d, int s
 // Attention of several rows per sequence.  A wave's tile has `cols` columns, (row,
 // head) pairs of a KV head: 16, and 32 where the rows are more than the sequences and
 // two tiles of outputs fit the registers (six rows of 4 heads over 8-bit caches of
-// 512 .. 16384 slots, 16 sequences: 105 us with 16, PENDING with 32).
+// 512 .. 16384 slots, 16 sequences: 105 us with 16 columns, 72 with 32).
 constexpr int rows_per_tile(int g, int cols) { return cols / g; }
 constexpr int rows_cols(bool bf16, int d, int batch, int rows) { return bf16 && d <= 128 && rows > batch ? 32 : 16; }
-// The tiles (segments, over all KV heads) that T rows of B sequences can make: a
-// sequence's last one may be short.
+// The tiles of `per` rows that T rows of B sequences can make at most: the sum of
+// ceil(n / per), a sequence's last one may be short.
+inline long rows_tiles(int per, int batch, int rows) {
+  const long tiles = ((long)rows + (long)batch * (per - 1)) / per;
+  return tiles < rows ? tiles : rows;
+}
 inline long rows_segments(int nkv, int g, int cols, int batch, int rows) {
-  const long tiles = (long)rows / rows_per_tile(g, cols) + batch;
-  return (tiles < rows ? tiles : rows) * nkv;
+  return rows_tiles(rows_per_tile(g, cols), batch, rows) * nkv;
 }
 // Places of a segment at most.
 inline int rows_span(int g, int cols, int max_len, int window, int n_first) {
@@ -102,12 +105,20 @@ inline int rows_span(int g, int cols, int max_len, int window, int n_first) {
 // chip by themselves; else equal runs of granules for all waves, as above.
 constexpr int ROWS_DIRECT_SEGMENTS = 2048;
 // In bf16 contexts, sequences of more rows than ROWS_FEW columns hold go to the
-// kernel of prompts, in tiles of prompt_columns, 32 to a wave: 256 (with 128, two
-// workgroups to a CU: one prompt of 8192 rows, 32 heads, 692 us, so 634), and 128 where
-// a wave of outputs takes more than a quarter of a SIMD's registers.  Where tiles are
-// fewer than PROMPT_FILL over all KV heads, each is split along its places into at
-// most PROMPT_SPLITS parts of PROMPT_PART at least, up to twice PROMPT_FILL in all.
-constexpr int ROWS_FEW = 32, PROMPT_LEAST = 512;
+// kernel of prompts (4096 slots, 4 query heads per KV head, one sequence: 16 rows 26 us
+// in tiles and 28 as a prompt, 32 rows 31 and 31, 64 rows 47 and 39; 32 sequences of 12
+// rows in 8 bits 129 and 185; one query head per KV head, 64 rows 48 and 31).  A call whose
+// rows are one each, or no more than PROMPT_LEAST columns in several sequences, does
+// without it: its launch costs 9 us where no sequence is that long, and a lone one
+// of so many takes about 1.5 times as long in tiles.
+//   Its tiles have prompt_columns, 32 to a wave: 256 (with 128, two workgroups to a CU:
+// one prompt of 8192 rows, 32 heads, 692 us, so 634), and 128 where a wave's outputs take
+// more than a quarter of a SIMD's registers.  Where tiles are fewer than PROMPT_FILL
+// over all KV heads, each is split along its places into at most PROMPT_SPLITS parts
+// of PROMPT_PART at least, up to twice PROMPT_FILL in all (64 rows over 32768 slots:
+// 102 us, unsplit 1170).  The bound of the tiles is exact for one sequence: 8 workgroups of
+// 24 without work made 128 rows there 186 us instead of 110.
+constexpr int ROWS_FEW = 48, PROMPT_LEAST = 1024;
 constexpr int PROMPT_FILL = 128, PROMPT_SPLITS = 16, PROMPT_PART = 256;
 constexpr int prompt_columns(int d) { return d == 256 ? 128 : 256; }
 constexpr int prompt_rows(int g, int d) { return prompt_columns(d) / g; }
@@ -125,9 +136,13 @@ inline RowsPlan rows_plan(bool bf16, int nkv, int g, int d, int batch, int rows,
   const int few = ROWS_FEW / g;
   const bool prompts = bf16 && !one_each && rows > few && (batch == 1 || (long)rows * g > PROMPT_LEAST);
   if (prompts) {
-    const long tiles = (long)rows / prompt_rows(g, d) + batch, full = (rows + prompt_rows(g, d) - 1l) / prompt_rows(g, d) * nkv;
+    // tiles to expect: full ones, and one at least for each sequence if those have
+    // enough rows on average
+    long full = (rows + prompt_rows(g, d) - 1l) / prompt_rows(g, d);
+    if (rows / batch > few && full < batch) full = batch;
+    full *= nkv;
     p.few = few;
-    p.prompt_segments = (int)((tiles < rows ? tiles : rows) * nkv);
+    p.prompt_segments = (int)(rows_tiles(prompt_rows(g, d), batch, rows) * nkv);
     if (full < PROMPT_FILL) {
       const long most = (2 * PROMPT_FILL + full - 1) / full, parts = span / PROMPT_PART;
       const long n = most < parts ? most : parts;
