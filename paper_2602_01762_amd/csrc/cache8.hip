@@ -62,12 +62,14 @@ __device__ __forceinline__ void shrink_rows(uint8_t *codes, int n, int d, int ol
   }
 }
 // fp64 to fp32, cut off, and the last bit set where anything was: a rounding of
-// that to fewer bits is the rounding of the fp64 value.
+// that to fewer bits is the rounding of the fp64 value.  A finite value beyond fp32
+// is cut off to its largest one (whose last bit is set), which has the same scale
+// and code.
 __device__ __forceinline__ float to_odd(double x) {
   const float f = (float)x;
   uint32_t u = __float_as_uint(f);
-  if ((double)f == x || !(fabsf(f) < INFINITY)) return f;
-  if (fabs((double)f) > fabs(x)) --u;        // cut off (f is not 0 then)
+  if ((double)f == x || x != x) return f;
+  if (fabs((double)f) > fabs(x)) --u;        // cut off (f is not 0 then; the one below infinity is the largest)
   return __uint_as_float(u | 1u);
 }
 

@@ -193,6 +193,21 @@ def test_append_what_is_not_finite():
     c.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_keys_beyond_the_largest_fp32(dtype):
+    """Two finite channels of 3e38 that a rotation adds to 4.2e38: a finite key, so the
+    largest code over the largest scale (448 * 2^119), of either sign."""
+    c = Cache8(4, 2, 64, dtype, 16, [0, 3], 2)
+    # heads 4, 5 are keys; at position 7 the first pair turns by 7 rad: cos 0.75, sin 0.66
+    append(c, [2, 1], gains=False, positions=[7, 7],
+           put=[(0, 4, 0, 3e38), (0, 4, 32, -3e38), (2, 5, 0, -3e38), (2, 5, 32, 3e38)])
+    v, s = values(c.k8), c.scales.cpu().numpy()
+    a, b = int(c.table8_h[0, 0]), int(c.table8_h[1, 0])
+    assert v[a, 0, 0, 0] == 448.0 and s[a, 0, 0] == 2.0 ** 119
+    assert v[b, 1, 3, 0] == -448.0 and s[b, 1, 0] == 2.0 ** 119
+    c.close()
+
+
 def test_keys_next_to_a_border():
     """Keys that lie halfway between two codes, and next to it, without a rotation
     (position 0) and gains: ties go to the even code, the others to the nearer."""
