@@ -538,6 +538,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_rows_a
           l += s_l[w][c] * wt;
           y += *(const f32x4 *)((const float *)sh[w] + 4 * e) * wt;
         }
+        if (l == 0.f) y = f32x4{0.f, 0.f, 0.f, 0.f};   // (0 times a value that is not finite)
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
         const size_t at = (size_t)(sg.r + c / g) * a.nq + sg.j * g + c % g;
@@ -984,7 +985,9 @@ __global__ __launch_bounds__(2 * prompt_columns(D), D == 256 ? 1 : 2) void k_row
   for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
     for (int jj = 0; jj < 4; ++jj) {
-      const float z[4] = {o[dt][4 * jj] * inv, o[dt][4 * jj + 1] * inv, o[dt][4 * jj + 2] * inv, o[dt][4 * jj + 3] * inv};
+      // (an output is not finite with l = 0 where a value is not)
+      const float z[4] = {l == 0.f ? 0.f : o[dt][4 * jj] * inv, l == 0.f ? 0.f : o[dt][4 * jj + 1] * inv,
+                          l == 0.f ? 0.f : o[dt][4 * jj + 2] * inv, l == 0.f ? 0.f : o[dt][4 * jj + 3] * inv};
       store_n<bf16_t, 4>((bf16_t *)a.out + hi * D + 32 * dt + 8 * jj + 4 * half, z);
     }
   if (a.lse && half == 0) a.lse[hi] = l == 0.f ? -INFINITY : (m_run + log2f(l)) * LN2;

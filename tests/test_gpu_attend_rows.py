@@ -311,6 +311,24 @@ def test_infinite_values_that_are_seen(n):
     c.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,counts", [([80, 80], [1, 1]), ([80, 80], [5, 3]), ([80], [90]), ([1500, 80], [5, 3]), ([1500], [90])])
+def test_values_that_are_not_finite_behind_scores_of_minus_infinity(lens, counts, dtype):
+    """A row whose every score is -inf gives zeros, whatever its values are; in tiles
+    that one workgroup walks, in prompts, and joined."""
+    c, q, off = setup((4, 2, 64, dtype), 16, lens, counts, False)
+    q = q.abs() + 0.5
+    for b, n in enumerate(counts):
+        blocks = [int(x) for x in c.table_h[b]]
+        c.k[blocks, 0] = float("-inf")
+        for s, dim, x in ((0, 0, "inf"), (17, 1, "-inf"), (40, 2, "nan"), (lens[b], 3, "inf")):
+            c.v[int(c.table_h[b, s // 16]), 0, s % 16, dim] = float(x)
+    r = c.dr.cache_attend_rows(c.kv(), q, offsets=off, n_new=1, lse=True)
+    assert bool((r["out"][:, :2] == 0).all()) and bool(torch.isneginf(r["lse"][:, :2]).all())
+    assert bool(torch.isfinite(r["out"]).all())
+    c.close()
+
+
 # ------------------------------------------------------------------- together
 @pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (32, 8, 128, "bf16"), (4, 1, 128, "f32")])
 def test_a_cache_in_eight_bits_from_prompt_to_drafting(heads):
