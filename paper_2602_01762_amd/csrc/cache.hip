@@ -486,6 +486,7 @@ __global__ __launch_bounds__(64 * NW, D * sizeof(T) > 512 ? 1 : 2) void k_cache_
           l += s_l[w][h] * wt;
           y += *(const f32x4 *)((const float *)sh_k[w] + 4 * e) * wt;
         }
+        if (l == 0.f) y = f32x4{0.f, 0.f, 0.f, 0.f};   // (0 times a value that is not finite)
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
         store_n<T, 4>((T *)a.out + ((size_t)sg.b * a.nq + sg.j * g) * D + 4 * e, z);

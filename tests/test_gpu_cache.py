@@ -515,6 +515,27 @@ def test_attend_infinite_values(heads, lens):
     c.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L", [1, 80, 3000])
+def test_attend_values_that_are_not_finite_behind_scores_of_minus_infinity(L, dtype):
+    """A sequence whose every score is -inf gives zeros, whatever its values are: by
+    one workgroup, joined, with slot weights (which receive nothing)."""
+    c = Cache(4, 2, 64, dtype, 16, [L, L], -(-L // 16))
+    q = c.normal((2, 4, 64)).abs() + 0.5                     # positive: the sign of k decides
+    blocks = [int(x) for x in c.table_h[0]]
+    c.k[blocks, 0] = float("-inf")
+    for s, dim, x in ((0, 0, "inf"), (L // 2, 1, "-inf"), (L - 1, 2, "nan")):
+        c.v[int(c.table_h[0, s // 16]), 0, s % 16, dim] = float(x)
+    w = c.weights()
+    w0 = w.clone()
+    for kw in (dict(), dict(max_len=L), dict(weights=w)):
+        r = c.dr.cache_attend(c.kv(), q, lse=True, **kw)
+        assert bool((r["out"][0, :2] == 0).all()) and bool(torch.isneginf(r["lse"][0, :2]).all())
+        assert bool(torch.isfinite(r["out"]).all()) and bool(torch.isfinite(r["lse"][1]).all())
+    assert torch.equal(w[blocks, 0], w0[blocks, 0])
+    c.close()
+
+
 def test_attend_rows_beyond_four_gigabytes():
     """Blocks at the end of pools of more than 2^32 bytes."""
     nkv, d, bs = 8, 128, 16
