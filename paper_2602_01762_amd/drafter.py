@@ -284,7 +284,7 @@ class Drafter:
     @staticmethod
     def _kind(kv, cls):
         """A call's sequences, of the cache it works on."""
-        if type(kv) is not cls:
+        if not isinstance(kv, cls):
             raise TypeError("a %s is needed, not %s" % (cls.__name__, type(kv).__name__))
         return kv
 
@@ -526,7 +526,7 @@ class Drafter:
         dt, T = self._dt, q.shape[0]
         shape = (T, self._nq, self._d)
         io = self._io[6]
-        if type(kv) is B.prism_cache8:
+        if isinstance(kv, B.prism_cache8):
             io.kv, io.kv8 = None, ctypes.addressof(kv)
         else:
             io.kv, io.kv8 = ctypes.addressof(self._kind(kv, B.prism_batch)), None

@@ -169,6 +169,49 @@ def test_calls_refuse_other_tensors():
             call()
 
 
+def test_calls_take_subclasses_of_their_structs(monkeypatch):
+    """A program's own descriptions, derived from the binding's, reach the library."""
+    class Batch(B.prism_batch):
+        pass
+
+    class Held(B.prism_cache8):
+        pass
+
+    def as_a(cls, kv):
+        own = cls.from_buffer_copy(kv)
+        own.__dict__.update(kv.__dict__)
+        return own
+
+    dr = _fake()
+    kv, kv8 = as_a(Batch, _kv(dr)), as_a(Held, _kv8(dr))
+    bf = dict(dtype=torch.bfloat16)
+    q, qkv, w = torch.zeros(3, 4, 32, **bf), torch.zeros(3, 256, **bf), torch.zeros(9, 2, 16)
+    summary, table = torch.zeros(9, 2, 2, 32, **bf), torch.zeros(3, 5, dtype=torch.int32)
+    monkeypatch.setattr(Drafter, "_stream", lambda self: 0)
+    calls = {name: [] for name in B.EXPORTS if name.startswith("prism_cache")}
+    for name, got in calls.items():
+        if name.endswith("scratch"):
+            monkeypatch.setattr(B, name, lambda *a: 16)
+        else:
+            monkeypatch.setattr(B, name, lambda ctx, io, *a, got=got: got.append(io))
+    dr.cache_append(kv, qkv)
+    assert calls["prism_cache_append"][0].kv == ctypes.addressof(kv)
+    dr.cache_attend(kv, q)
+    dr.cache_summarize(kv, summary)
+    dr.cache_select(kv, q, summary, 1)
+    dr.cache_evict(kv, table, w, 1)
+    dr.cache8_append(kv8, qkv)
+    dr.cache8_pack(kv8, kv)
+    dr.cache8_unpack(kv8, kv)
+    io = dr._io[6]
+    dr.cache_attend_rows(kv8, q)
+    assert io.kv is None and io.kv8 == ctypes.addressof(kv8)
+    dr.cache_attend_rows(kv, q)
+    assert io.kv == ctypes.addressof(kv) and io.kv8 is None
+    assert all(len(got) == (2 if name == "prism_cache_attend_rows" else 1)
+               for name, got in calls.items() if not name.endswith("scratch"))
+
+
 STRUCTS = ("prism_cache8", "prism_cache8_rows", "prism_cache8_move", "prism_cache_row_attention")
 
 
