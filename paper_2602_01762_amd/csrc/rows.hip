@@ -637,7 +637,8 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttend a) {
 // unrounded): in three parts they would double the work of the larger product.
 //   The maximum that is subtracted follows the scores only when one is 2^8 above
 // it: sums and outputs are fp32, so nothing is lost, and outputs are seldom
-// rescaled.
+// rescaled.  Each column decides for itself, so that no other row's scores change
+// how its probabilities are rounded.
 //   Rows of K and V go through registers (8-bit ones become bf16 on the way) to one
 // of two LDS buffers, one tile ahead of the products, their loads two tiles ahead
 // and block-table lookups three: one barrier per tile.
@@ -910,10 +911,10 @@ __global__ __launch_bounds__(2 * prompt_columns(D), D == 256 ? 1 : 2) void k_row
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[st][i]);
       mx = fmaxf(mx, xor32_f(mx)) * a.scale;
-      if (__ballot(mx > m_run + PROMPT_SLACK)) {            // (from -inf: any score that is not)
-        const float mn = fmaxf(m_run, mx);
-        const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - mn);
-        m_run = mn;
+      const bool up = mx > m_run + PROMPT_SLACK;            // (from -inf: any score that is not)
+      if (__ballot(up)) {
+        const float al = up ? __builtin_amdgcn_exp2f(m_run - mx) : 1.f;
+        m_run = up ? mx : m_run;
         l_run *= al;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)

@@ -329,6 +329,25 @@ def test_values_that_are_not_finite_behind_scores_of_minus_infinity(lens, counts
     c.close()
 
 
+@pytest.mark.parametrize("eight", [False, True])
+def test_other_rows_do_not_reach_a_prompt(eight):
+    """Other queries in other rows, of the same sequence and of another one, change no
+    bit of a row's output."""
+    for lens, counts, changed in (([100], [200], slice(1, None, 2)), ([0, 50], [150, 201], slice(0, 150)),
+                                  ([0, 2500], [150, 201], slice(0, 150))):
+        c, q, off = setup((8, 2, 64, "bf16"), 16, lens, counts, eight)
+        kv = sequences(c, eight)
+        kept = torch.ones(q.shape[0], dtype=torch.bool, device=DEV)
+        kept[changed] = False
+        was = c.dr.cache_attend_rows(kv, q, offsets=off, n_new=1, lse=True)
+        q[changed] *= 30
+        now = c.dr.cache_attend_rows(kv, q, offsets=off, n_new=1, lse=True)
+        for x in ("out", "lse"):
+            assert torch.equal(was[x][kept], now[x][kept]), (x, lens)
+            assert not torch.equal(was[x][~kept], now[x][~kept])
+        c.close()
+
+
 # ------------------------------------------------------------------- together
 @pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (32, 8, 128, "bf16"), (4, 1, 128, "f32")])
 def test_a_cache_in_eight_bits_from_prompt_to_drafting(heads):
