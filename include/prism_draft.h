@@ -650,9 +650,11 @@ prism_status prism_cache_rows_scratch(prism_ctx *ctx, int32_t batch, int32_t row
  * token, drafts to be scored, prompts, in one batch.  A row that sees nothing, or
  * whose every score is -inf, gives zeros and a log-sum of -inf.  What a row does
  * not see does not reach it, also where it is infinite or NaN; infinite values as
- * in prism_cache_attend.  Rows behind the last sequence are left alone.  A
- * malformed d_offsets raises PRISM_ERR_INVALID_ARG in prism_device_status and
- * writes nothing. */
+ * in prism_cache_attend, but for a probability below 2^-118.  Sums are fp32 with
+ * weights up to 1: finite values whose largest magnitude times the slots that a row
+ * sees is below 2^128 give finite outputs.  Rows behind the last sequence are left
+ * alone.  A malformed d_offsets raises PRISM_ERR_INVALID_ARG in
+ * prism_device_status and writes nothing. */
 prism_status prism_cache_attend_rows(prism_ctx *ctx, const prism_cache_row_attention *io,
                                      void *stream);
 

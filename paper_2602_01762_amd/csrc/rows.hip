@@ -635,10 +635,12 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttend a) {
 // Probabilities are rounded to bf16 for it (2^-9 of each on average over a sum of
 // many, as much as the rounding of the output; the sum of a row takes them
 // unrounded): in three parts they would double the work of the larger product.
-//   The maximum that is subtracted follows the scores only when one is 2^8 above
-// it: sums and outputs are fp32, so nothing is lost, and outputs are seldom
-// rescaled.  Each column decides for itself, so that no other row's scores change
-// how its probabilities are rounded.
+//   What is subtracted from the scores lies up to 2^8 above the largest so far and
+// follows only a score that passes it, so that outputs are seldom rescaled and no
+// probability is above 1: as in the tiles of rows, sums leave fp32's range where the
+// values times the slots do.  Below 2^-118 of the largest a probability may be 0.
+// Each column decides for itself, so that no other row's scores change how its
+// probabilities are rounded.
 //   Rows of K and V go through registers (8-bit ones become bf16 on the way) to one
 // of two LDS buffers, one tile ahead of the products, their loads two tiles ahead
 // and block-table lookups three: one barrier per tile.
@@ -730,7 +732,8 @@ __global__ __launch_bounds__(2 * prompt_columns(D), D == 256 ? 1 : 2) void k_row
   for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;                     // l_run: over this lane's half of the places
+  float m_run = -INFINITY;                                  // what is subtracted
+  float l_run = 0.f;                                        // over this lane's half of the places
 
   // Loads: a lane of each wave looks up one place of a tile, and takes piece li of
   // row grp of each pass.
@@ -911,10 +914,10 @@ __global__ __launch_bounds__(2 * prompt_columns(D), D == 256 ? 1 : 2) void k_row
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[st][i]);
       mx = fmaxf(mx, xor32_f(mx)) * a.scale;
-      const bool up = mx > m_run + PROMPT_SLACK;            // (from -inf: any score that is not)
+      const bool up = mx > m_run;                           // (from -inf: any score that is not)
       if (__ballot(up)) {
-        const float al = up ? __builtin_amdgcn_exp2f(m_run - mx) : 1.f;
-        m_run = up ? mx : m_run;
+        const float ms = mx + PROMPT_SLACK, al = up ? __builtin_amdgcn_exp2f(m_run - ms) : 1.f;
+        m_run = up ? ms : m_run;
         l_run *= al;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)

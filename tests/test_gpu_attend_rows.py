@@ -348,6 +348,25 @@ def test_other_rows_do_not_reach_a_prompt(eight):
         c.close()
 
 
+@pytest.mark.parametrize("L", [200, 3000])
+def test_large_values_of_a_prompt(L):
+    """Values of 1e37 on 20 slots whose score lies 2^7.9 above those before them: their
+    average is finite, and so is every sum that leads to it."""
+    c, q, off = setup((4, 1, 64, "bf16"), 16, [L], [64], False)
+    c.k.zero_()
+    c.v.zero_()
+    q.zero_()
+    q[:, :, 0] = 8.0
+    for s in range(130, 150):
+        blk = int(c.table_h[0, s // 16])
+        c.k[blk, 0, s % 16, 0] = 7.9 * np.log(2.0)                # the score, 8 k / sqrt(64)
+        c.v[blk, 0, s % 16] = 1e37
+    r = c.dr.cache_attend_rows(c.kv(), q, offsets=off, n_new=1, lse=True)
+    assert bool(torch.isfinite(r["out"]).all()) and float(r["out"].float().min()) > 5e36 * min(1.0, 1000 / L)
+    check(c, q, [64], r, rounded=True)
+    c.close()
+
+
 # ------------------------------------------------------------------- together
 @pytest.mark.parametrize("heads", [(8, 2, 64, "bf16"), (32, 8, 128, "bf16"), (4, 1, 128, "f32")])
 def test_a_cache_in_eight_bits_from_prompt_to_drafting(heads):
