@@ -68,6 +68,25 @@ def make(case, eight, **kw):
     return setup(heads, bs, lens, counts, eight, columns=R.columns_of(bs, lens, counts), **kw)
 
 
+# ------------------------------------------------------- tiles, at their own precision
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("heads,bs,lens,counts", [
+    (R.SMALL, 1, [300, 0, 65, 511], [1, 70, 6, 40]), (R.SMALL, 12, [300, 0, 65, 511], [1, 70, 6, 40]),
+    (R.SMALL, 256, [300, 0, 65, 511], [1, 70, 6, 40]), (R.MANY, 16, [3000, 100], [60, 50]), (R.NARROW, 7, [200, 30, 0], [9, 0, 33]),
+    (R.SMALL, 16, [5000, 1023, 2048, 0], [3, 1, 6, 2]), (R.ODD, 16, [700, 3000, 1], [6, 12, 16]), (R.WIDE, 16, [700, 90], [33, 12]),
+    ((4, 1, 128, "f32"), 16, [300, 0, 2000], [1, 70, 33]),
+])
+def test_rows_in_tiles(heads, bs, lens, counts, eight):
+    """Probabilities in two parts or three, wherever no prompt is: their low parts
+    are not lost."""
+    c, q, off = make((heads, bs, lens, counts), eight)
+    for window, n_first in ((0, 0), (90, 5)):
+        assert not R.plan(heads, len(lens), sum(counts), bs * c.columns, window, n_first).prompt_segments
+        r = c.dr.cache_attend_rows(sequences(c, eight), q, offsets=off, n_new=1, window=window, n_first=n_first, lse=True)
+        check(c, q, counts, r, eight, window=window, n_first=n_first)
+    c.close()
+
+
 # ------------------------------------------------------------------ prompts
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("case", R.BLOCKS)
