@@ -278,3 +278,78 @@ def test_a_prompt_appended_in_eight_bits_and_attended_to(case):
             c.exp_h = np.where(np.isnan(s), -999, np.log2(np.where(s > 0, s, 1.0)).astype(np.int64))
         check(c, q, counts, r, True, window=window, n_first=n_first)
     c.close()
+
+
+# ------------------------------------------------- streams and scratch
+def on_side(fill, call):
+    """call() on a stream of its own, behind work that keeps that stream busy and then
+    writes the call's input: a launch on another stream would not wait for it."""
+    side = torch.cuda.Stream()
+    busy = torch.randn((4096, 4096), device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(8):                                  # a few ms
+            busy = busy @ busy * 1e-2
+        fill()
+        r = call()
+    side.synchronize()
+    torch.cuda.synchronize()
+    return r
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("case", R.STREAMS + [(R.SMALL, 16, [700, 90], [1, 1]), (R.SMALL, 16, [700, 90], [7, 3])])
+def test_attention_waits_for_its_stream(case, eight):
+    c, q, off = make(case, eight)
+    kv, src = sequences(c, eight), q.clone()
+    want = c.dr.cache_attend_rows(kv, q, offsets=off, n_new=1, lse=True)
+    q.zero_()
+    got = on_side(lambda: q.copy_(src), lambda: c.dr.cache_attend_rows(kv, q, offsets=off, n_new=1, lse=True))
+    assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
+    c.close()
+
+
+def test_the_8_bit_cache_waits_for_its_stream():
+    a, b = (Cache8(8, 2, 64, "bf16", 16, [0, 70, 33], 8, seed=3) for _ in range(2))
+    rows = a.normal((3, 12 * 64), 2.0)
+    start = torch.tensor([0, 5, 33], dtype=torch.int32, device=DEV)
+    off = torch.arange(4, dtype=torch.int32, device=DEV)
+
+    def step(c, qkv):
+        q = c.dr.cache8_append(c.kv8(), qkv, offsets=off)
+        c.dr.cache8_unpack(c.kv8(), c.kv(), start=start, n_new=1)
+        c.dr.cache8_pack(c.kv8(), c.kv(), start=start, n_new=1)
+        return q
+
+    want = step(a, rows)
+    src = torch.zeros_like(rows)
+    got = on_side(lambda: src.copy_(rows), lambda: step(b, src))
+    assert torch.equal(got, want)
+    for x, y in ((a.k, b.k), (a.v, b.v), (a.k8, b.k8), (a.v8, b.v8), (a.scales, b.scales)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    a.close()
+    b.close()
+
+
+def test_nothing_is_written_behind_the_scratch():
+    """Sized for the largest call, for each batch, and to the byte that a call asks for."""
+    from paper_2602_01762_amd import binding as B
+    heads, bs, lens, counts = R.SCRATCH
+    c, q, off = make(R.SCRATCH, False)
+    most = B.prism_cache_rows_scratch(c.dr.ctx, 4, sum(counts), 0)
+    for nb in (4, 3, 2, 1):
+        kv = c.dr.cache(c.lens[:nb], c.k, c.v, c.table[:nb])
+        T = sum(counts[:nb])
+        for n in {most, B.prism_cache_rows_scratch(c.dr.ctx, nb, T, 0)}:
+            for window, n_first in ((0, 0), (600, 3)):
+                out = torch.empty((T, c.nq, c.d), dtype=c.dt, device=DEV)
+                scratch = torch.full((n + 4096,), 0xa5, dtype=torch.uint8, device=DEV)
+                io = B.prism_cache_row_attention()
+                io.kv, io.rows, io.d_offsets, io.n_new = ctypes.addressof(kv), T, B.ptr(off), 1
+                io.window, io.n_first, io.d_q, io.d_out = window, n_first, B.ptr(q), B.ptr(out)
+                io.d_scratch, io.scratch_bytes = B.ptr(scratch), n
+                B.prism_cache_attend_rows(c.dr.ctx, io)
+                assert bool((scratch[n:] == 0xa5).all())
+                want = c.dr.cache_attend_rows(kv, q[:T], offsets=off[: nb + 1], n_new=1, window=window, n_first=n_first)
+                assert torch.equal(out, want["out"])
+    c.close()
