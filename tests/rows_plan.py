@@ -78,5 +78,9 @@ GRAPH_WINDOWS = [(0, 0), (100, 4)]
 INFINITE = [((4, 2, 64, "bf16"), 16, [80, 80], [300, 300])]
 STREAMS = [(SMALL, 16, [700, 90], [260, 40]), (SMALL, 16, [3000], [100])]
 EIGHT = [(SMALL, 16, [0, 0, 0], [300, 33, 1])]
+# other numbers of new rows; many sequences; the end of the largest capacity, 2^20 slots
+NEW = [(SMALL, 16, [0, 100], [200, 90]), ((5, 1, 128, "bf16"), 16, [60], [70]), ((8, 1, 64, "bf16"), 16, [0, 3], [130, 20])]
+CROWD = [((6, 2, 32, "bf16"), 16, [(b * 131) % 500 for b in range(64)], [(b * 7) % 40 for b in range(64)])]
+LONG = [(NARROW, 7, [2 ** 20 - 44], [20])]
 # a batch that needs the scratch of both kernels
 SCRATCH = (SMALL, 16, [900, 40, 1500, 700], [60, 1, 9, 230])

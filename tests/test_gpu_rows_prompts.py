@@ -110,6 +110,44 @@ def test_windows_split_over_their_length(case, eight):
     c.close()
 
 
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("case", R.NEW)
+def test_numbers_of_new_rows(case, eight):
+    """Rows that see the slots before them only (the first of an empty sequence sees
+    nothing), and rows with others in the cache behind them."""
+    heads, bs, lens, counts = case
+    c, q, off = setup(heads, bs, lens, [n + 9 for n in counts], eight)
+    q = q[: sum(counts)].contiguous()
+    off = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device=DEV)
+    for n_new in (0, 2, 9):
+        for window, n_first in ((0, 0), (30, 2)):
+            kw = dict(n_new=n_new, window=window, n_first=n_first)
+            check(c, q, counts, c.dr.cache_attend_rows(sequences(c, eight), q, offsets=off, lse=True, **kw), eight, **kw)
+    c.close()
+
+
+@pytest.mark.parametrize("case", R.CROWD)
+def test_many_sequences(case):
+    c, q, off = make(case, True)
+    for window, n_first in ((0, 0), (200, 3)):
+        r = c.dr.cache_attend_rows(c.kv8(), q, offsets=off, n_new=1, window=window, n_first=n_first, lse=True)
+        check(c, q, case[3], r, True, window=window, n_first=n_first)
+    c.close()
+
+
+@pytest.mark.parametrize("n", [1, 5, 20])
+@pytest.mark.parametrize("case", R.LONG)
+def test_the_end_of_the_largest_capacity(case, n):
+    """Slots up to 2^20, in blocks of 7: by tiles and as a prompt."""
+    heads, bs, lens, (most,) = case
+    c, q, off = make(case, False)
+    q, off = q[:n].contiguous(), torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    for window, n_first in ((0, 0), (9000, 5)):
+        r = c.dr.cache_attend_rows(c.kv(), q, offsets=off, n_new=1 + most - n, window=window, n_first=n_first, lse=True)
+        check(c, q, [n], r, n_new=1 + most - n, window=window, n_first=n_first)
+    c.close()
+
+
 # slots, and whether some row sees none of them: among the first ones that every row
 # sees too; that only the first rows still see; that only later rows see
 BAD = [({0: [101, 63, 2, 103], 1: [32, 33, 1]}, False), ({0: [63, 62], 1: [32, 33]}, True), ({0: [101, 103], 1: [60, 61]}, True)]

@@ -11,7 +11,8 @@ def _plan(case, window=(0, 0)):
 
 @pytest.mark.parametrize("cases,windows", [
     (R.BLOCKS, R.BLOCK_WINDOWS), (R.SPLIT, R.SPLIT_WINDOWS), (R.HIDDEN, [R.HIDDEN_WINDOW]), (R.FLAGS, [(0, 0)]),
-    (R.GRAPHS, R.GRAPH_WINDOWS), (R.INFINITE, [(0, 0)]), (R.STREAMS, [(0, 0)]), (R.EIGHT, [(0, 0)]), ([R.SCRATCH], [(0, 0)]),
+    (R.GRAPHS, R.GRAPH_WINDOWS), (R.INFINITE, [(0, 0)]), (R.STREAMS, [(0, 0)]), (R.EIGHT, [(0, 0)]),
+    (R.NEW, [(0, 0), (30, 2)]), (R.CROWD, [(0, 0), (200, 3)]), (R.LONG, [(0, 0), (9000, 5)]), ([R.SCRATCH], [(0, 0)]),
 ])
 def test_prompts_go_by_their_kernel(cases, windows):
     for case in cases:
