@@ -652,9 +652,12 @@ prism_status prism_cache_rows_scratch(prism_ctx *ctx, int32_t batch, int32_t row
  * not see does not reach it, also where it is infinite or NaN; infinite values as
  * in prism_cache_attend, but for a probability below 2^-118.  Sums are fp32 with
  * weights up to 1: finite values whose largest magnitude times the slots that a row
- * sees is below 2^128 give finite outputs.  Rows behind the last sequence are left
- * alone.  A malformed d_offsets raises PRISM_ERR_INVALID_ARG in
- * prism_device_status and writes nothing. */
+ * sees is below 2^128 give finite outputs.  In bf16 contexts the product with V takes
+ * the probabilities of prompts rounded to bf16, those of other rows to 2^-16 or
+ * better (a prompt: more than 48 / g rows, of g query heads per KV head, in a batch
+ * of more than 1024 / g rows, or a lone sequence whose buffer has more); log-sums
+ * have them unrounded.  Rows behind the last sequence are left alone.  A malformed
+ * d_offsets raises PRISM_ERR_INVALID_ARG in prism_device_status and writes nothing. */
 prism_status prism_cache_attend_rows(prism_ctx *ctx, const prism_cache_row_attention *io,
                                      void *stream);
 

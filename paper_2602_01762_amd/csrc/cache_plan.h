@@ -105,10 +105,12 @@ inline int rows_span(int g, int cols, int max_len, int window, int n_first) {
 // chip by themselves; else equal runs of granules for all waves, as above.
 constexpr int ROWS_DIRECT_SEGMENTS = 2048;
 // In bf16 contexts, sequences of more rows than ROWS_FEW columns hold go to the
-// kernel of prompts (4096 slots, 4 query heads per KV head, one sequence: 16 rows 26 us
-// in tiles and 28 as a prompt, 32 rows 31 and 31, 64 rows 47 and 39; 32 sequences of 12
-// rows in 8 bits 129 and 185; one query head per KV head, 64 rows 48 and 31).  A call whose
-// rows are one each, or no more than PROMPT_LEAST columns in several sequences, does
+// kernel of prompts.  In tiles and as a prompt, over 4096 slots: 4 query heads per KV
+// head, one sequence, 16 rows 26 and 28 us, 32 rows 31 and 31, 64 rows 47 and 39; one
+// query head per KV head, 64 rows 48 and 31; 32 sequences of 12 rows in 8 bits 129 and
+// 185.  So they meet at 128 columns with 4 heads and below 64 with one, and the limit
+// is below both: with 4 heads, 13 .. 31 rows of a lone sequence lose up to 2 us, and
+// the low bits of their probabilities.  A call whose rows are one each, or no more than PROMPT_LEAST columns in several sequences, does
 // without it: its launch costs 9 us where no sequence is that long, and a lone one
 // of so many takes about 1.5 times as long in tiles.
 //   Its tiles have prompt_columns, 32 to a wave: 256 (with 128, two workgroups to a CU:

@@ -644,9 +644,9 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsAttend a) {
 //   Rows of K and V go through registers (8-bit ones become bf16 on the way) to one
 // of two LDS buffers, one tile ahead of the products, their loads two tiles ahead
 // and block-table lookups three: one barrier per tile.
-//   8192 rows of 32 heads: 633 us, 869 TFLOP/s, 71% of what a large product of the
+//   8192 rows of 32 heads: 630 us, 873 TFLOP/s, 72% of what a large product of the
 // vendor's library reaches here; the matrix units are busy 33% of the cycles, the
-// vector units 39%, and a wave waits 36% of its time, so their overlap bounds it.
+// vector units 40%, and a wave waits 36% of its time, so their overlap bounds it.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float PROMPT_SLACK = 8.f;
 // LDS written by the workgroup is there, with global loads still in flight

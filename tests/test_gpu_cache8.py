@@ -5,9 +5,10 @@ normalised and rotated go through some tens of fp64 operations, so a key is off 
 less than 2^-44 of its head's largest magnitude, and takes another code than the
 oracle's only next to the border of two.  That an input lies there is a matter of
 10^-11 for each (2^-44 of magnitudes of some 2^2 against steps of 2^-9 or more of
-the scale, twice), and inputs are seeded.  Queries: fp64 arithmetic, and one
-rounding to the context's type, half a step, 2^-8 of the value in bf16, 2^-24 in
-fp32.
+the scale, twice), and inputs are seeded.  Queries are normalised and rotated in
+fp32: (d / 2 + 10) 2^-24 of the two channels of a pair together and of the value (the
+mean of d squares, halved by the root, and some ten operations behind it), and in
+bf16 one rounding more, half a step, 2^-8 of the value.
 """
 import numpy as np
 import pytest
